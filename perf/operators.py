@@ -229,6 +229,7 @@ def prepare(case, seed):
         s["weights"] = torch.empty(t, k, dtype=torch.float32, device=dev)
         s["plan"] = torch.empty(abi.sparoa_expert_plan_words(t, k, e), dtype=torch.int32,
                                 device=dev)
+        s["views"] = abi.expert_plan_views(s["plan"], t, k, e)
         s["ws"] = scratch(abi.sparoa_expert_route_workspace_size(s["desc"]))
     elif case["kind"] == "experts":
         t, e, k = case["tokens"], case["experts"], case["top_k"]
@@ -262,11 +263,9 @@ def run(state):
 
 
 def _own_route(s):
-    abi, c = s["abi"], s["case"]
-    abi.sparoa_expert_route(s["desc"], s["logits"], s["bias"], s["valid"], s["idx"], s["weights"],
-                            s["plan"], s["ws"])
-    return s["idx"], s["weights"], abi.expert_plan_views(s["plan"], c["tokens"], c["top_k"],
-                                                         c["experts"])
+    s["abi"].sparoa_expert_route(s["desc"], s["logits"], s["bias"], s["valid"], s["idx"],
+                                 s["weights"], s["plan"], s["ws"])
+    return s["idx"], s["weights"], s["views"]
 
 
 def _own_experts(s):
