@@ -59,7 +59,15 @@ typedef enum {
 
 typedef enum { SPAROA_F32 = 0, SPAROA_F16 = 1, SPAROA_BF16 = 2 } sparoa_dtype;
 
-typedef enum { SPAROA_ACT_NONE = 0, SPAROA_ACT_RELU = 1, SPAROA_ACT_RELU6 = 2 } sparoa_act;
+/* SILU (v / (1 + exp(-v))) and GELU (v (1 + erf(v / sqrt 2)) / 2) are for
+ * sparoa_expert_ffn; the other calls take NONE, RELU and RELU6. */
+typedef enum {
+  SPAROA_ACT_NONE = 0,
+  SPAROA_ACT_RELU = 1,
+  SPAROA_ACT_RELU6 = 2,
+  SPAROA_ACT_SILU = 3,
+  SPAROA_ACT_GELU = 4
+} sparoa_act;
 
 /* bit 0 = skip zero blocks, bit 1 = bandwidth-bound kernel. */
 typedef enum {
@@ -552,6 +560,111 @@ sparoa_status sparoa_conv2d_noalloc(const sparoa_conv_desc *desc, sparoa_path pa
 sparoa_status sparoa_maxpool2d(const void *x, sparoa_dtype dtype, int64_t n, int64_t c,
                                int64_t h, int64_t w, int64_t k, int64_t s, int64_t p, void *y,
                                hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Routing of tokens to experts, and the plan that groups their slots.
+ *
+ * sparoa_expert_route: logits [tokens][experts] (dtype) of a router, for
+ * every token t:
+ *   s_e   = softmax(l)_e or sigmoid(l_e)
+ *   key_e = s_e + bias_e          (bias fp32 [experts], nullable: it balances
+ *                                  the choice and joins no weight)
+ *   groups > 1: the experts are `groups` runs of experts / groups; a group
+ *   scores the sum of its group_best (1 or 2) largest keys, and only the
+ *   top_groups best groups' experts stay;
+ *   the top_k experts of the largest keys, in that order, ties to the lowest
+ *   expert (groups: to the lowest group), are idx[t][0 .. top_k);
+ *   weights[t][j] = s of choice j, over the choices' sum if `renormalise`
+ *   (0 where that sum is 0), times scale.
+ * A logit that is NaN or -inf, or a key that is, is never chosen and joins no
+ * sum; token_mask (nullable, [tokens]): a zero byte marks a token that is
+ * routed nowhere (padding).  Where fewer than top_k experts can be chosen the
+ * remaining idx are -1 and their weights 0.  A logit of +inf takes the whole
+ * softmax, shared with its equals.  Scores, keys and sums are fp32 (scores
+ * that differ by less than their key can hold tie).
+ *
+ * The plan (int32, sparoa_expert_plan_words words; E = experts, S = tokens *
+ * top_k, slot s = t * top_k + j):
+ *   [0, E]          offsets: expert e's slots are order[offsets[e] ..
+ *                   offsets[e + 1])
+ *   [E + 1]         number of experts with a slot, then their ids, ascending
+ *   [H, H + S)      order: slots sorted by expert, ascending within one (a
+ *                   stable sort); -1 past offsets[E];  H = 2 E + 2 rounded up
+ *                   to a multiple of 4
+ *   [H + S', +S)    place: slot s is order[place[s]], or -1; S' = S rounded
+ *                   up to a multiple of 4
+ * plan is nullable (routing only).  sparoa_expert_plan makes the plan of
+ * given idx (a value outside [0, E) is no expert).  Equal choices give an
+ * equal plan.  Workspace: the *_workspace_size bytes, contents on entry do
+ * not matter (a routing without plan takes none).
+ * Errors: INVALID_ARG for null logits/idx/weights (plan: null idx/plan), sizes
+ * <= 0, top_k > experts, groups that do not divide experts, top_groups outside
+ * [1, groups], group_best outside {1, 2}, more choices than the kept groups'
+ * experts, an unknown score or dtype, a scale that is not finite; UNSUPPORTED
+ * for experts > 512, top_k > 32, groups > 64, tokens * top_k > 2^30 or a
+ * misaligned pointer; WORKSPACE.
+ * ---------------------------------------------------------------------- */
+typedef enum { SPAROA_SCORE_SOFTMAX = 0, SPAROA_SCORE_SIGMOID = 1 } sparoa_score;
+
+typedef struct {
+  int64_t tokens, experts, top_k, groups, top_groups, group_best;
+  sparoa_dtype dtype;
+  sparoa_score score;
+  int renormalise;
+  float scale;
+} sparoa_expert_route_desc;
+
+sparoa_status sparoa_expert_plan_words(int64_t tokens, int64_t top_k, int64_t experts,
+                                       int64_t *words);
+sparoa_status sparoa_expert_route_workspace_size(const sparoa_expert_route_desc *desc,
+                                                 size_t *bytes);
+sparoa_status sparoa_expert_route(const sparoa_expert_route_desc *desc, const void *logits,
+                                  const float *bias, const uint8_t *token_mask, int32_t *idx,
+                                  float *weights, int32_t *plan, void *workspace, size_t ws_bytes,
+                                  hipStream_t stream);
+sparoa_status sparoa_expert_plan_workspace_size(int64_t tokens, int64_t top_k, int64_t experts,
+                                                size_t *bytes);
+sparoa_status sparoa_expert_plan(int64_t tokens, int64_t top_k, int64_t experts,
+                                 const int32_t *idx, int32_t *plan, void *workspace,
+                                 size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * The norm between two blocks, fused with the first block's gate and the
+ * residual's scale.  For every row (a token) of `cols` features:
+ *   v  = post(y)                    norm behind the block, or y itself
+ *   r' = residual_scale * r + gate * v          -> r_out
+ *   n  = pre(r')                    norm before the next block -> n_out
+ * with rms(v) = v / sqrt(mean(v^2) + eps) * w + b and
+ * layer(v) = (v - mean v) / sqrt(mean((v - mean v)^2) + eps) * w + b.
+ *   y [rows][cols] (nullable: v = 0), r [rows][cols] (nullable: r' = gate v);
+ *   not both null.  gate [ceil(rows / gate_rows)][cols], nullable (= 1): row i
+ *   takes gate row i / gate_rows (gate_rows = rows: one gate per channel;
+ *   rows of a sample: one per sample).  Weights and biases [cols], nullable
+ *   (1 and 0); a post or pre of NORM_NONE ignores its own, and pre NORM_NONE
+ *   ignores n_out.  r_out is nullable where n_out is written.
+ *   Statistics, r' and the products are fp32; each output is rounded once
+ *   (n is computed from r' before its rounding).  A NaN or infinity stays in
+ *   its row.
+ *   Aliasing: r_out may be r or y, and n_out may be r or y, whole; no other
+ *   overlap.
+ * Errors: INVALID_ARG for rows, cols or gate_rows <= 0, an unknown norm or
+ * dtype, eps < 0 or not finite, a residual_scale that is not finite, y and r
+ * both null, no output to write; UNSUPPORTED for misaligned pointers or
+ * cols > 2^31 - 1.
+ * ---------------------------------------------------------------------- */
+typedef enum { SPAROA_NORM_NONE = 0, SPAROA_NORM_RMS = 1, SPAROA_NORM_LAYER = 2 } sparoa_norm;
+
+typedef struct {
+  int64_t rows, cols, gate_rows;
+  sparoa_dtype dtype;
+  sparoa_norm post, pre;
+  float eps, residual_scale;
+} sparoa_block_norm_desc;
+
+sparoa_status sparoa_block_norm(const sparoa_block_norm_desc *desc, const void *y,
+                                const void *post_w, const void *post_b, const void *gate,
+                                const void *r, const void *pre_w, const void *pre_b, void *r_out,
+                                void *n_out, hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -15,13 +15,16 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libsparoa.so")
 
 F32, F16, BF16 = 0, 1, 2
-ACT_NONE, ACT_RELU, ACT_RELU6 = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_RELU6, ACT_SILU, ACT_GELU = 0, 1, 2, 3, 4
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
 PATH_DENSE_MFMA, PATH_SKIP_MFMA, PATH_DENSE_BW, PATH_SKIP_BW = 0, 1, 2, 3
 ROUTE_BLOCK, ROUTE_ELEMENT = 0, 1
 PATH_NAMES = {0: "dense_mfma", 1: "skip_mfma", 2: "dense_bw", 3: "skip_bw"}
 COMMIT_WORDS_BYTES = 2048   # SPAROA_COMMIT_WORDS_BYTES
 
 _TORCH_DT = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+_DT_TORCH = {code: dt for dt, code in _TORCH_DT.items()}
 
 EXPORTS = [
     "sparoa_abi_version", "sparoa_status_string", "sparoa_last_error", "sparoa_mask_words",
@@ -35,6 +38,8 @@ EXPORTS = [
     "sparoa_fc_measured", "sparoa_conv2d_routed_measured", "sparoa_fc_routed_measured",
     "sparoa_conv2d_split", "sparoa_fc_split", "sparoa_measure_sparsity_preset",
     "sparoa_conv2d_noalloc", "sparoa_conv2d_reads_mask", "sparoa_conv2d_routed_reads_mask",
+    "sparoa_block_norm", "sparoa_expert_plan_words", "sparoa_expert_route_workspace_size",
+    "sparoa_expert_route", "sparoa_expert_plan_workspace_size", "sparoa_expert_plan",
 ]
 
 
@@ -84,6 +89,20 @@ class FcOp(ctypes.Structure):
                 ("counts", ctypes.c_void_p), ("mask", ctypes.c_void_p), ("y", ctypes.c_void_p),
                 ("workspace", ctypes.c_void_p), ("ws_bytes", ctypes.c_size_t),
                 ("path", ctypes.c_void_p), ("thr", Thresholds)]
+
+
+class ExpertRouteDesc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("experts", ctypes.c_int64),
+                ("top_k", ctypes.c_int64), ("groups", ctypes.c_int64),
+                ("top_groups", ctypes.c_int64), ("group_best", ctypes.c_int64),
+                ("dtype", ctypes.c_int), ("score", ctypes.c_int), ("renormalise", ctypes.c_int),
+                ("scale", ctypes.c_float)]
+
+
+class BlockNormDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("gate_rows", ctypes.c_int64),
+                ("dtype", ctypes.c_int), ("post", ctypes.c_int), ("pre", ctypes.c_int),
+                ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float)]
 
 
 def _load():
@@ -153,6 +172,13 @@ def _load():
         "sparoa_fc_routed_measured": (ctypes.c_int, [P(FcDesc), P(Thresholds), vp, vp, vp, vp, vp,
                                                      vp, ctypes.c_int, vp, vp, vp, sz, vp, vp, vp,
                                                      vp, vp]),
+        "sparoa_expert_plan_words": (ctypes.c_int, [i64, i64, i64, P(i64)]),
+        "sparoa_expert_route_workspace_size": (ctypes.c_int, [P(ExpertRouteDesc), P(sz)]),
+        "sparoa_expert_route": (ctypes.c_int, [P(ExpertRouteDesc), vp, vp, vp, vp, vp, vp, vp, sz,
+                                               vp]),
+        "sparoa_expert_plan_workspace_size": (ctypes.c_int, [i64, i64, i64, P(sz)]),
+        "sparoa_expert_plan": (ctypes.c_int, [i64, i64, i64, vp, vp, vp, sz, vp]),
+        "sparoa_block_norm": (ctypes.c_int, [P(BlockNormDesc)] + [vp] * 10),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -186,6 +212,18 @@ def _stream(stream):
             return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
         return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else None
     return stream if isinstance(stream, int) else stream.cuda_stream
+
+
+def _whole(t, dtype, numel, name):
+    """The pointer of a dense device tensor of `dtype` with `numel` elements
+    (None stays None): what the kernels would read elsewhere is refused here."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != numel or not t.is_contiguous() or not t.is_cuda:
+        raise SparoaError(1, f"{name}: a contiguous {dtype} device tensor of {numel} elements is "
+                             f"wanted, got {t.dtype} {tuple(t.shape)} with strides {t.stride()} "
+                             f"on {t.device}")
+    return t.data_ptr()
 
 
 def dtype_code(t):
@@ -508,3 +546,88 @@ def sparoa_fc_ops_run(op_array, sparsity_thr=None, intensity_thr=None, mode=ROUT
     if events is not None:
         ev = (ctypes.c_void_p * len(events))(*[e.cuda_event for e in events])
     _check(_L.sparoa_fc_ops_run(op_array, len(op_array), t, ev, _stream(stream)))
+
+# ------------------------------------- transformer-block operators (see sparoa.h)
+
+def _scratch(t):
+    """Pointer and bytes of a workspace tensor (or None)."""
+    if t is None:
+        return None, 0
+    if not t.is_contiguous() or not t.is_cuda:
+        raise SparoaError(1, "workspace: a contiguous device tensor is wanted")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def expert_route_desc(tokens, experts, top_k, dtype=F32, score=SCORE_SOFTMAX, groups=1,
+                      top_groups=1, group_best=1, renormalise=False, scale=1.0):
+    if isinstance(dtype, torch.dtype):
+        dtype = dtype_code(dtype)
+    return ExpertRouteDesc(tokens, experts, top_k, groups, top_groups, group_best, dtype, score,
+                           int(renormalise), scale)
+
+
+def sparoa_expert_plan_words(tokens, top_k, experts):
+    w = ctypes.c_int64()
+    _check(_L.sparoa_expert_plan_words(tokens, top_k, experts, ctypes.byref(w)))
+    return w.value
+
+
+def expert_plan_views(plan, tokens, top_k, experts):
+    """(offsets [experts + 1], order [tokens * top_k], place [tokens * top_k]) of a plan."""
+    slots, head = tokens * top_k, -(-(2 * experts + 2) // 4) * 4
+    at = head + -(-slots // 4) * 4
+    return plan[:experts + 1], plan[head:head + slots], plan[at:at + slots]
+
+
+def sparoa_expert_route_workspace_size(desc):
+    s = ctypes.c_size_t()
+    _check(_L.sparoa_expert_route_workspace_size(ctypes.byref(desc), ctypes.byref(s)))
+    return s.value
+
+
+def sparoa_expert_route(desc, logits, bias, token_mask, idx, weights, plan=None, workspace=None,
+                        stream=None):
+    """Chosen experts, their weights and (plan not None) the dispatch plan."""
+    t, e, slots = desc.tokens, desc.experts, desc.tokens * desc.top_k
+    words = 0 if plan is None else sparoa_expert_plan_words(t, desc.top_k, e)
+    ws, ws_bytes = _scratch(workspace)
+    _check(_L.sparoa_expert_route(
+        ctypes.byref(desc), _whole(logits, _DT_TORCH.get(desc.dtype), t * e, "logits"),
+        _whole(bias, torch.float32, e, "bias"), _whole(token_mask, torch.uint8, t, "token_mask"),
+        _whole(idx, torch.int32, slots, "idx"), _whole(weights, torch.float32, slots, "weights"),
+        _whole(plan, torch.int32, words, "plan"), ws, ws_bytes, _stream(stream)))
+
+
+def sparoa_expert_plan_workspace_size(tokens, top_k, experts):
+    s = ctypes.c_size_t()
+    _check(_L.sparoa_expert_plan_workspace_size(tokens, top_k, experts, ctypes.byref(s)))
+    return s.value
+
+
+def sparoa_expert_plan(tokens, top_k, experts, idx, plan, workspace, stream=None):
+    """The dispatch plan of given choices idx [tokens, top_k]."""
+    ws, ws_bytes = _scratch(workspace)
+    _check(_L.sparoa_expert_plan(
+        tokens, top_k, experts, _whole(idx, torch.int32, tokens * top_k, "idx"),
+        _whole(plan, torch.int32, sparoa_expert_plan_words(tokens, top_k, experts), "plan"),
+        ws, ws_bytes, _stream(stream)))
+
+
+def block_norm_desc(rows, cols, dtype=BF16, post=NORM_NONE, pre=NORM_RMS, eps=1e-6,
+                    gate_rows=None, residual_scale=1.0):
+    """gate_rows: rows that share a gate row (default: all of them)."""
+    if isinstance(dtype, torch.dtype):
+        dtype = dtype_code(dtype)
+    return BlockNormDesc(rows, cols, rows if gate_rows is None else gate_rows, dtype, post, pre,
+                         eps, residual_scale)
+
+
+def sparoa_block_norm(desc, y, post_w, post_b, gate, r, pre_w, pre_b, r_out, n_out, stream=None):
+    """r_out = residual_scale r + gate post(y), n_out = pre(r_out)."""
+    dt, c, n = _DT_TORCH.get(desc.dtype), desc.cols, desc.rows * desc.cols
+    gates = -(-desc.rows // max(1, desc.gate_rows)) * c
+    _check(_L.sparoa_block_norm(
+        ctypes.byref(desc), _whole(y, dt, n, "y"), _whole(post_w, dt, c, "post_w"),
+        _whole(post_b, dt, c, "post_b"), _whole(gate, dt, gates, "gate"), _whole(r, dt, n, "r"),
+        _whole(pre_w, dt, c, "pre_w"), _whole(pre_b, dt, c, "pre_b"),
+        _whole(r_out, dt, n, "r_out"), _whole(n_out, dt, n, "n_out"), _stream(stream)))

@@ -9,7 +9,9 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libsparoa.so")
-SOURCES = ["abi.cpp", "measure.hip", "gemm.hip", "fc_bw.hip", "direct.hip", "noalloc.hip", "pointwise.hip"]
+SOURCES = ["abi.cpp", "measure.hip", "gemm.hip", "fc_bw.hip", "direct.hip", "noalloc.hip",
+           "pointwise.hip", "block_abi.cpp", "norm.hip",
+           "expert_route.hip"]
 OBJDIR = os.path.join(PKG, "_build")
 
 FLAGS = [

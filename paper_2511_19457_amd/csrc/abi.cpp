@@ -101,6 +101,8 @@ sparoa_status hip_fail(hipError_t e, const char *what) {
   return SPAROA_ERR_HIP;
 }
 
+void clear_error() { g_last_error.clear(); }
+
 }  // namespace sparoa
 
 using namespace sparoa;

@@ -1,0 +1,177 @@
+// extern "C" entry points of the transformer-block operators: argument
+// validation and dispatch.
+#include <cmath>
+
+#include "block.h"
+
+using namespace sparoa;
+
+namespace {
+
+bool dtype_ok(int d) { return d == SPAROA_F32 || d == SPAROA_F16 || d == SPAROA_BF16; }
+
+bool norm_ok(int n) {
+  return n == SPAROA_NORM_NONE || n == SPAROA_NORM_RMS || n == SPAROA_NORM_LAYER;
+}
+
+sparoa_status check_ptrs16(std::initializer_list<const void *> ps) {
+  for (const void *p : ps)
+    if (p && !aligned16(p)) return fail(SPAROA_ERR_UNSUPPORTED, "pointer not 16-byte aligned");
+  return SPAROA_OK;
+}
+
+// a * b * c fits 62 bits (every size positive).
+bool product_ok(int64_t a, int64_t b, int64_t c = 1) {
+  int64_t p;
+  return !__builtin_mul_overflow(a, b, &p) && !__builtin_mul_overflow(p, c, &p) &&
+         p <= INT64_MAX / 8;
+}
+
+sparoa_status check_plan(int64_t tokens, int64_t top_k, int64_t experts) {
+  if (tokens <= 0 || top_k <= 0 || experts <= 0)
+    return fail(SPAROA_ERR_INVALID_ARG, "experts: sizes must be > 0");
+  if (experts > 512 || top_k > 32 || tokens > (1 << 30) / top_k)
+    return fail(SPAROA_ERR_UNSUPPORTED,
+                "experts: more than 512 experts, 32 choices or 2^30 slots");
+  return SPAROA_OK;
+}
+
+sparoa_status check_route(const sparoa_expert_route_desc *d) {
+  if (!d) return fail(SPAROA_ERR_INVALID_ARG, "null expert_route descriptor");
+  if (!dtype_ok(d->dtype)) return fail(SPAROA_ERR_INVALID_ARG, "unknown dtype");
+  if (d->score != SPAROA_SCORE_SOFTMAX && d->score != SPAROA_SCORE_SIGMOID)
+    return fail(SPAROA_ERR_INVALID_ARG, "expert_route: unknown score");
+  if (d->tokens <= 0 || d->top_k <= 0 || d->experts <= 0)
+    return fail(SPAROA_ERR_INVALID_ARG, "expert_route: sizes must be > 0");
+  if (d->groups <= 0 || d->experts % d->groups || d->top_groups < 1 ||
+      d->top_groups > d->groups || (d->group_best != 1 && d->group_best != 2))
+    return fail(SPAROA_ERR_INVALID_ARG, "expert_route: bad groups");
+  if (d->top_k > d->experts / d->groups * d->top_groups)
+    return fail(SPAROA_ERR_INVALID_ARG, "expert_route: more choices than experts to choose from");
+  if (!std::isfinite(d->scale))
+    return fail(SPAROA_ERR_INVALID_ARG, "expert_route: the scale must be finite");
+  if (d->groups > 64) return fail(SPAROA_ERR_UNSUPPORTED, "expert_route: more than 64 groups");
+  return check_plan(d->tokens, d->top_k, d->experts);
+}
+
+int64_t round4(int64_t n) { return (n + 3) / 4 * 4; }
+// Words before the plan's order, and before its place.
+int64_t plan_order(int64_t experts) { return round4(2 * experts + 2); }
+int64_t plan_place(int64_t experts, int64_t slots) { return plan_order(experts) + round4(slots); }
+
+void set_plan(RouteArgs &a, int32_t *plan) {
+  a.plan = plan;
+  a.order = plan ? plan + plan_order(a.experts) : nullptr;
+  a.place = plan ? plan + plan_place(a.experts, a.tokens * a.top_k) : nullptr;
+}
+
+}  // namespace
+
+extern "C" {
+
+// ---------------------------------------------------------- expert routing
+
+sparoa_status sparoa_expert_plan_words(int64_t tokens, int64_t top_k, int64_t experts,
+                                       int64_t *words) {
+  clear_error();
+  if (!words) return fail(SPAROA_ERR_INVALID_ARG, "null result pointer");
+  sparoa_status st = check_plan(tokens, top_k, experts);
+  if (st != SPAROA_OK) return st;
+  *words = plan_place(experts, tokens * top_k) + round4(tokens * top_k);
+  return SPAROA_OK;
+}
+
+sparoa_status sparoa_expert_route_workspace_size(const sparoa_expert_route_desc *d,
+                                                 size_t *bytes) {
+  clear_error();
+  if (!bytes) return fail(SPAROA_ERR_INVALID_ARG, "null result pointer");
+  sparoa_status st = check_route(d);
+  if (st != SPAROA_OK) return st;
+  *bytes = expert_plan_workspace(d->tokens, d->experts);
+  return SPAROA_OK;
+}
+
+sparoa_status sparoa_expert_plan_workspace_size(int64_t tokens, int64_t top_k, int64_t experts,
+                                                size_t *bytes) {
+  clear_error();
+  if (!bytes) return fail(SPAROA_ERR_INVALID_ARG, "null result pointer");
+  sparoa_status st = check_plan(tokens, top_k, experts);
+  if (st != SPAROA_OK) return st;
+  *bytes = expert_plan_workspace(tokens, experts);
+  return SPAROA_OK;
+}
+
+sparoa_status sparoa_expert_route(const sparoa_expert_route_desc *d, const void *logits,
+                                  const float *bias, const uint8_t *token_mask, int32_t *idx,
+                                  float *weights, int32_t *plan, void *workspace, size_t ws_bytes,
+                                  hipStream_t stream) {
+  clear_error();
+  sparoa_status st = check_route(d);
+  if (st != SPAROA_OK) return st;
+  if (!logits || !idx || !weights)
+    return fail(SPAROA_ERR_INVALID_ARG, "expert_route: null logits, idx or weights");
+  st = check_ptrs16({logits, bias, token_mask, idx, weights, plan, workspace});
+  if (st != SPAROA_OK) return st;
+  if (plan && (!workspace || ws_bytes < expert_plan_workspace(d->tokens, d->experts)))
+    return fail(SPAROA_ERR_WORKSPACE, "expert_route: workspace too small");
+  RouteArgs a{};
+  a.logits = logits, a.bias = bias, a.token_mask = token_mask, a.idx = idx, a.weights = weights;
+  a.tokens = d->tokens, a.experts = (int)d->experts, a.top_k = (int)d->top_k;
+  a.groups = (int)d->groups, a.top_groups = (int)d->top_groups;
+  a.group_best = (int)d->group_best, a.score = d->score, a.renormalise = d->renormalise != 0;
+  a.by_score = bias || (d->groups > 1 && d->group_best == 2);
+  a.scale = d->scale;
+  a.counts = reinterpret_cast<uint32_t *>(workspace);
+  set_plan(a, plan);
+  return launch_expert_route(a, d->dtype, stream);
+}
+
+sparoa_status sparoa_expert_plan(int64_t tokens, int64_t top_k, int64_t experts,
+                                 const int32_t *idx, int32_t *plan, void *workspace,
+                                 size_t ws_bytes, hipStream_t stream) {
+  clear_error();
+  sparoa_status st = check_plan(tokens, top_k, experts);
+  if (st != SPAROA_OK) return st;
+  if (!idx || !plan) return fail(SPAROA_ERR_INVALID_ARG, "expert_plan: null idx or plan");
+  st = check_ptrs16({idx, plan, workspace});
+  if (st != SPAROA_OK) return st;
+  if (!workspace || ws_bytes < expert_plan_workspace(tokens, experts))
+    return fail(SPAROA_ERR_WORKSPACE, "expert_plan: workspace too small");
+  RouteArgs a{};
+  a.idx = const_cast<int32_t *>(idx);   // (only read)
+  a.tokens = tokens, a.experts = (int)experts, a.top_k = (int)top_k;
+  a.counts = reinterpret_cast<uint32_t *>(workspace);
+  set_plan(a, plan);
+  return launch_expert_plan(a, stream);
+}
+
+// ------------------------------------------------------------- block norm
+
+sparoa_status sparoa_block_norm(const sparoa_block_norm_desc *d, const void *y,
+                                const void *post_w, const void *post_b, const void *gate,
+                                const void *r, const void *pre_w, const void *pre_b, void *r_out,
+                                void *n_out, hipStream_t stream) {
+  clear_error();
+  if (!d) return fail(SPAROA_ERR_INVALID_ARG, "null block_norm descriptor");
+  if (!dtype_ok(d->dtype)) return fail(SPAROA_ERR_INVALID_ARG, "unknown dtype");
+  if (d->rows <= 0 || d->cols <= 0 || d->gate_rows <= 0 || !product_ok(d->rows, d->cols))
+    return fail(SPAROA_ERR_INVALID_ARG, "block_norm: sizes must be > 0");
+  if (!norm_ok(d->post) || !norm_ok(d->pre))
+    return fail(SPAROA_ERR_INVALID_ARG, "block_norm: unknown norm");
+  if (!(d->eps >= 0.f) || !std::isfinite(d->eps) || !std::isfinite(d->residual_scale))
+    return fail(SPAROA_ERR_INVALID_ARG, "block_norm: eps must be finite and >= 0, the scale finite");
+  if (!y && !r) return fail(SPAROA_ERR_INVALID_ARG, "block_norm: y and r both null");
+  const bool norms = d->pre != SPAROA_NORM_NONE;
+  if (norms ? !n_out : !r_out)
+    return fail(SPAROA_ERR_INVALID_ARG, norms ? "block_norm: null n_out"
+                                              : "block_norm: null r_out and no norm to write");
+  if (d->cols > INT32_MAX)
+    return fail(SPAROA_ERR_UNSUPPORTED, "block_norm: more than 2^31 - 1 columns");
+  sparoa_status st = check_ptrs16({y, post_w, post_b, gate, r, pre_w, pre_b, r_out, n_out});
+  if (st != SPAROA_OK) return st;
+  NormArgs a{y, post_w, post_b, gate, r, pre_w, pre_b, r_out, n_out, d->rows, d->cols,
+             d->gate_rows, d->post, d->pre, d->eps, d->residual_scale};
+  return launch_block_norm(a, d->dtype, stream);
+}
+
+}  // extern "C"

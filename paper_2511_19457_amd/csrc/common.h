@@ -16,6 +16,7 @@ namespace sparoa {
 // Thread-local error message plumbing (defined in abi.cpp).
 sparoa_status fail(sparoa_status s, const std::string &msg);
 sparoa_status hip_fail(hipError_t e, const char *what);
+void clear_error();
 
 #define SPAROA_HIP_CHECK(call)                                  \
   do {                                                          \

@@ -1,0 +1,255 @@
+// The norm between two blocks: r' = c r + gate * post(y), n = pre(r').
+//
+// One pass over memory: a row's elements stay in registers (fp32) from their
+// load to both stores, so y and r are read once and r' and n written once.
+// Sums run over lanes by cross-lane adds and, where a row takes several
+// waves, once more through LDS; the layer norm's variance is taken from the
+// registers around the mean (no E[v^2] - mean^2).
+// Bound by HBM: 4 cols sizeof(dtype) bytes a row.
+#include <algorithm>
+
+#include "block.h"
+#include "dtype.h"
+
+namespace sparoa {
+namespace {
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+  return v;
+}
+
+// Sum over the TPR threads of a row; red: one float per wave of the
+// work-group, two halves used in turn so that one barrier per sum is enough.
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float (*red)[16], int &turn) {
+  v = wave_sum(v);
+  if constexpr (TPR > 64) {
+    constexpr int W = TPR / 64;
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) red[turn][wave] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) v += red[turn][i];
+    turn ^= 1;
+  }
+  return v;
+}
+
+// A row in registers: TPR threads, VPT vectors of 16 bytes each (cols a
+// multiple of a vector).  TPR = 64: a wave per row, four rows a work-group.
+template <int DT, int TPR, int VPT>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_rows_kernel(NormArgs a) {
+  using E = Elem<DT>;
+  using raw = typename E::raw;
+  constexpr int V = 16 / E::size;
+  constexpr int RPW = TPR >= 256 ? 1 : 256 / TPR;   // rows per work-group
+  __shared__ float red[2][16];
+  const int t = TPR >= 256 ? threadIdx.x : threadIdx.x % TPR;
+  const int cols = (int)a.cols, nv = cols / V;
+  int turn = 0;
+  const float inv = 1.f / (float)cols;
+
+  union Q {
+    uint4 q;
+    raw e[V];
+  };
+  auto load = [&](Q (&d)[VPT], const void *p, int64_t at) __attribute__((always_inline)) {
+    const raw *src = reinterpret_cast<const raw *>(p) + at;
+#pragma unroll
+    for (int u = 0; u < VPT; ++u)   // (lanes past the row read its last vector, unused)
+      d[u].q = *reinterpret_cast<const uint4 *>(src + min(t + u * TPR, nv - 1) * V);
+  };
+  // (whole waves leave the loop, and RPW > 1 has no barrier)
+  for (int64_t row = (int64_t)blockIdx.x * RPW + (TPR >= 256 ? 0 : threadIdx.x / TPR);
+       row < a.rows; row += (int64_t)gridDim.x * RPW) {
+    const int64_t base = row * a.cols;
+    Q yq[VPT], rq[VPT], w[VPT];
+    if (a.y) load(yq, a.y, base);
+    if (a.r) load(rq, a.r, base);
+
+    float v[VPT][V];
+#pragma unroll
+    for (int u = 0; u < VPT; ++u) {
+      const bool in = t + u * TPR < nv;
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[u][e] = (a.y && in) ? E::to_f32(yq[u].e[e]) : 0.f;
+    }
+    // v <- norm(v) * weight + bias
+    auto normalise = [&](int kind, const void *wp, const void *bp) __attribute__((always_inline)) {
+      if (wp) load(w, wp, 0);
+      Q b[VPT];
+      if (bp) load(b, bp, 0);
+      if (kind == SPAROA_NORM_LAYER) {
+        float s = 0.f;
+#pragma unroll
+        for (int u = 0; u < VPT; ++u)
+#pragma unroll
+          for (int e = 0; e < V; ++e) s += v[u][e];
+        const float mean = row_sum<TPR>(s, red, turn) * inv;
+#pragma unroll
+        for (int u = 0; u < VPT; ++u) {
+          const bool in = t + u * TPR < nv;
+#pragma unroll
+          for (int e = 0; e < V; ++e) v[u][e] = in ? v[u][e] - mean : 0.f;
+        }
+      }
+      float s = 0.f;
+#pragma unroll
+      for (int u = 0; u < VPT; ++u)
+#pragma unroll
+        for (int e = 0; e < V; ++e) s += v[u][e] * v[u][e];
+      const float k = 1.f / sqrtf(row_sum<TPR>(s, red, turn) * inv + a.eps);
+#pragma unroll
+      for (int u = 0; u < VPT; ++u)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          v[u][e] *= k;
+          if (wp) v[u][e] *= E::to_f32(w[u].e[e]);
+          if (bp) v[u][e] += E::to_f32(b[u].e[e]);
+        }
+    };
+    auto store = [&](void *p) __attribute__((always_inline)) {
+      raw *dst = reinterpret_cast<raw *>(p) + base;
+#pragma unroll
+      for (int u = 0; u < VPT; ++u) {
+        Q o;
+#pragma unroll
+        for (int e = 0; e < V; ++e) o.e[e] = E::from_f32(v[u][e]);
+        if (t + u * TPR < nv) *reinterpret_cast<uint4 *>(dst + (t + u * TPR) * V) = o.q;
+      }
+    };
+
+    if (a.y && a.post != SPAROA_NORM_NONE) normalise(a.post, a.post_w, a.post_b);
+    if (a.gate) {
+      load(w, a.gate, row / a.gate_rows * a.cols);
+#pragma unroll
+      for (int u = 0; u < VPT; ++u)
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[u][e] *= E::to_f32(w[u].e[e]);
+    }
+    if (a.r) {
+#pragma unroll
+      for (int u = 0; u < VPT; ++u)
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[u][e] = fmaf(a.scale, E::to_f32(rq[u].e[e]), v[u][e]);
+    }
+    // lanes past the row hold what their clamped loads gave them: cleared
+#pragma unroll
+    for (int u = 0; u < VPT; ++u) {
+      const bool in = t + u * TPR < nv;
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[u][e] = in ? v[u][e] : 0.f;
+    }
+    if (a.r_out) store(a.r_out);
+    if (a.pre != SPAROA_NORM_NONE) {
+      normalise(a.pre, a.pre_w, a.pre_b);
+      store(a.n_out);
+    }
+  }
+}
+
+// Any row length and alignment: element by element, a work-group per row, its
+// elements read again for each statistic and computed again for the stores,
+// which come last (so outputs may take an input's place).
+template <int DT>
+__global__ __launch_bounds__(256) void norm_any_kernel(NormArgs a) {
+  using E = Elem<DT>;
+  using raw = typename E::raw;
+  __shared__ float red[2][16];
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const int64_t base = row * a.cols;
+    const raw *y = a.y ? reinterpret_cast<const raw *>(a.y) + base : nullptr;
+    const raw *r = a.r ? reinterpret_cast<const raw *>(a.r) + base : nullptr;
+    const raw *g = a.gate ? reinterpret_cast<const raw *>(a.gate) + row / a.gate_rows * a.cols
+                          : nullptr;
+    const raw *pw = reinterpret_cast<const raw *>(a.post_w);
+    const raw *pb = reinterpret_cast<const raw *>(a.post_b);
+    const raw *nw = reinterpret_cast<const raw *>(a.pre_w);
+    const raw *nb = reinterpret_cast<const raw *>(a.pre_b);
+    const float inv = 1.f / (float)a.cols;
+    // mean (layer) and 1 / deviation of f(0 .. cols - 1)
+    auto stats = [&](int kind, auto f, float &mean, float &k) {
+      mean = 0.f;
+      if (kind == SPAROA_NORM_LAYER) {
+        float s = 0.f;
+        for (int64_t c = threadIdx.x; c < a.cols; c += 256) s += f(c);
+        mean = row_sum<256>(s, red, turn) * inv;
+      }
+      float s = 0.f;
+      for (int64_t c = threadIdx.x; c < a.cols; c += 256) {
+        const float d = f(c) - mean;
+        s += d * d;
+      }
+      k = 1.f / sqrtf(row_sum<256>(s, red, turn) * inv + a.eps);
+    };
+    const bool post = y && a.post != SPAROA_NORM_NONE;
+    float m0 = 0.f, k0 = 1.f, m1 = 0.f, k1 = 1.f;
+    if (post) stats(a.post, [&](int64_t c) { return E::to_f32(y[c]); }, m0, k0);
+    auto joined = [&](int64_t c) {
+      float v = y ? E::to_f32(y[c]) : 0.f;
+      if (post) {
+        v = (v - m0) * k0;
+        if (pw) v *= E::to_f32(pw[c]);
+        if (pb) v += E::to_f32(pb[c]);
+      }
+      if (g) v *= E::to_f32(g[c]);
+      return r ? fmaf(a.scale, E::to_f32(r[c]), v) : v;
+    };
+    const bool pre = a.pre != SPAROA_NORM_NONE;
+    if (pre) stats(a.pre, joined, m1, k1);
+    raw *ro = a.r_out ? reinterpret_cast<raw *>(a.r_out) + base : nullptr;
+    raw *no = reinterpret_cast<raw *>(a.n_out) + base;
+    for (int64_t c = threadIdx.x; c < a.cols; c += 256) {
+      const float v = joined(c);
+      if (ro) ro[c] = E::from_f32(v);
+      if (!pre) continue;
+      float n = (v - m1) * k1;
+      if (nw) n *= E::to_f32(nw[c]);
+      if (nb) n += E::to_f32(nb[c]);
+      no[c] = E::from_f32(n);
+    }
+  }
+}
+
+template <int DT>
+void launch_dt(const NormArgs &a, hipStream_t stream) {
+  constexpr int V = 16 / Elem<DT>::size;
+  const int64_t nv = a.cols / V;
+  // (a grid has under 2^32 threads: longer inputs loop)
+  const dim3 rows((unsigned)std::min<int64_t>(a.rows, 1 << 20));
+  const dim3 rows4((unsigned)std::min<int64_t>(cdiv(a.rows, 4), 1 << 20));
+  if (a.cols % V || nv > 8192)
+    norm_any_kernel<DT><<<rows, 256, 0, stream>>>(a);
+  else if (nv <= 64)
+    norm_rows_kernel<DT, 64, 1><<<rows4, 256, 0, stream>>>(a);
+  else if (nv <= 128)
+    norm_rows_kernel<DT, 64, 2><<<rows4, 256, 0, stream>>>(a);
+  else if (nv <= 256)
+    norm_rows_kernel<DT, 256, 1><<<rows, 256, 0, stream>>>(a);
+  else if (nv <= 512)
+    norm_rows_kernel<DT, 256, 2><<<rows, 256, 0, stream>>>(a);
+  else if (nv <= 1024)
+    norm_rows_kernel<DT, 256, 4><<<rows, 256, 0, stream>>>(a);
+  else if (nv <= 2048)
+    norm_rows_kernel<DT, 1024, 2><<<rows, 1024, 0, stream>>>(a);
+  else
+    norm_rows_kernel<DT, 1024, 8><<<rows, 1024, 0, stream>>>(a);
+}
+
+}  // namespace
+
+sparoa_status launch_block_norm(const NormArgs &a, sparoa_dtype dt, hipStream_t stream) {
+  switch (dt) {
+    case SPAROA_F32: launch_dt<SPAROA_F32>(a, stream); break;
+    case SPAROA_F16: launch_dt<SPAROA_F16>(a, stream); break;
+    default: launch_dt<SPAROA_BF16>(a, stream); break;
+  }
+  SPAROA_LAUNCH_CHECK("block_norm");
+  return SPAROA_OK;
+}
+
+}  // namespace sparoa
