@@ -629,6 +629,79 @@ sparoa_status sparoa_expert_plan(int64_t tokens, int64_t top_k, int64_t experts,
                                  size_t ws_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------------------
+ * The experts' products: the FFN of every token's chosen experts,
+ *   y[t] = residual[t] + sum_j weights[t][j] (w_down_e u + b_down_e),
+ *   u    = act(w_up_e x[t] + b_up_e)                          (gated = 0)
+ *        = act(gate) * up, [gate; up] = w_up_e x[t] + b_up_e  (gated = 1)
+ * over the choices j of token t, e the expert of choice j.
+ *   x [tokens][hidden]; w_up [experts][inner or 2 inner][hidden] (gated: the
+ *   gate's rows, then the up rows); w_down [experts][hidden][inner]; biases
+ *   b_up [experts][inner or 2 inner] and b_down [experts][hidden] (both, if
+ *   has_bias); weights fp32 [tokens][top_k]; plan: of sparoa_expert_route or
+ *   sparoa_expert_plan with the same tokens, top_k and experts; residual
+ *   (nullable) and y [tokens][hidden] (y may be residual; no other overlap).
+ *   A slot whose expert is -1 is not computed and its weight not looked at; a
+ *   token without experts gives residual, or 0.
+ *   Products accumulate in fp32; u is rounded to dtype once (the second
+ *   product's operand), the slots' down products stay fp32 and so does their
+ *   weighted sum, in the order of j; y is rounded once.
+ *   act: NONE, RELU, RELU6, SILU or GELU.
+ *   Kernels: few rows an expert stream its weights (each byte read once for
+ *   up to 64 rows); many run tiles through LDS.  Only experts with a row are
+ *   read.
+ *   Workspace: sparoa_expert_ffn_workspace_size bytes (u and the down
+ *   products, tokens * top_k rows); contents on entry do not matter.
+ * Errors: those of the plan's sizes; INVALID_ARG for hidden or inner <= 0, null
+ * x/w_up/w_down/weights/plan/y, biases that do not match has_bias, an unknown
+ * act; UNSUPPORTED for misaligned pointers, x or one expert's matrix of 2 GiB
+ * or more (split the tokens); WORKSPACE.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  int64_t tokens, top_k, experts, hidden, inner;
+  sparoa_dtype dtype;
+  int gated, has_bias;
+} sparoa_expert_ffn_desc;
+
+sparoa_status sparoa_expert_ffn_workspace_size(const sparoa_expert_ffn_desc *desc, size_t *bytes);
+sparoa_status sparoa_expert_ffn(const sparoa_expert_ffn_desc *desc, sparoa_act act, const void *x,
+                                const void *w_up, const void *b_up, const void *w_down,
+                                const void *b_down, const float *weights, const int32_t *plan,
+                                const void *residual, void *y, void *workspace, size_t ws_bytes,
+                                hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * FC with low-rank adapters of many requests:
+ *   y[i] = act(w x[i] + bias + scale_a b_a (a_a x[i]) + residual[i]),
+ *   a = adapter_ids[i]; a value outside [0, adapters) is no adapter.
+ *   x [m][k], w [n][k], bias [n], residual and y [m][n] as for sparoa_fc_dense;
+ *   lora_a [adapters][rank][k], lora_b [adapters][n][rank] (dtype), scale fp32
+ *   [adapters], adapter_ids int32 [m].  Rows of one adapter need not be
+ *   consecutive (they cost least when they are).  Adapters of smaller rank
+ *   are padded with zero rows of lora_a.
+ *   a_a x accumulates in fp32, is scaled in fp32 and kept in fp32 where the
+ *   weights are streamed, else rounded to dtype once for the second product.
+ *   act: NONE, RELU or RELU6.
+ *   Workspace: sparoa_fc_adapted_workspace_size bytes; contents on entry do
+ *   not matter.
+ * Errors: INVALID_ARG for sizes <= 0, null x/w/lora_a/lora_b/scale/
+ * adapter_ids/y, bias that does not match has_bias, an unknown act or dtype;
+ * UNSUPPORTED for misaligned pointers, rank > 512, rows of x or a matrix of
+ * 2 GiB or more; WORKSPACE.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  int64_t m, k, n, adapters, rank;
+  sparoa_dtype dtype;
+  int has_bias;
+} sparoa_fc_adapted_desc;
+
+sparoa_status sparoa_fc_adapted_workspace_size(const sparoa_fc_adapted_desc *desc, size_t *bytes);
+sparoa_status sparoa_fc_adapted(const sparoa_fc_adapted_desc *desc, sparoa_act act, const void *x,
+                                const void *w_nk, const void *bias, const void *lora_a,
+                                const void *lora_b, const float *scale,
+                                const int32_t *adapter_ids, const void *residual, void *y,
+                                void *workspace, size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------
  * The norm between two blocks, fused with the first block's gate and the
  * residual's scale.  For every row (a token) of `cols` features:
  *   v  = post(y)                    norm behind the block, or y itself

@@ -40,6 +40,8 @@ EXPORTS = [
     "sparoa_conv2d_noalloc", "sparoa_conv2d_reads_mask", "sparoa_conv2d_routed_reads_mask",
     "sparoa_block_norm", "sparoa_expert_plan_words", "sparoa_expert_route_workspace_size",
     "sparoa_expert_route", "sparoa_expert_plan_workspace_size", "sparoa_expert_plan",
+    "sparoa_expert_ffn_workspace_size", "sparoa_expert_ffn", "sparoa_fc_adapted_workspace_size",
+    "sparoa_fc_adapted",
 ]
 
 
@@ -97,6 +99,19 @@ class ExpertRouteDesc(ctypes.Structure):
                 ("top_groups", ctypes.c_int64), ("group_best", ctypes.c_int64),
                 ("dtype", ctypes.c_int), ("score", ctypes.c_int), ("renormalise", ctypes.c_int),
                 ("scale", ctypes.c_float)]
+
+
+class ExpertFfnDesc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("top_k", ctypes.c_int64),
+                ("experts", ctypes.c_int64), ("hidden", ctypes.c_int64),
+                ("inner", ctypes.c_int64), ("dtype", ctypes.c_int), ("gated", ctypes.c_int),
+                ("has_bias", ctypes.c_int)]
+
+
+class FcAdaptedDesc(ctypes.Structure):
+    _fields_ = [("m", ctypes.c_int64), ("k", ctypes.c_int64), ("n", ctypes.c_int64),
+                ("adapters", ctypes.c_int64), ("rank", ctypes.c_int64), ("dtype", ctypes.c_int),
+                ("has_bias", ctypes.c_int)]
 
 
 class BlockNormDesc(ctypes.Structure):
@@ -178,6 +193,12 @@ def _load():
                                                vp]),
         "sparoa_expert_plan_workspace_size": (ctypes.c_int, [i64, i64, i64, P(sz)]),
         "sparoa_expert_plan": (ctypes.c_int, [i64, i64, i64, vp, vp, vp, sz, vp]),
+        "sparoa_expert_ffn_workspace_size": (ctypes.c_int, [P(ExpertFfnDesc), P(sz)]),
+        "sparoa_expert_ffn": (ctypes.c_int, [P(ExpertFfnDesc), ctypes.c_int] + [vp] * 10 +
+                              [sz, vp]),
+        "sparoa_fc_adapted_workspace_size": (ctypes.c_int, [P(FcAdaptedDesc), P(sz)]),
+        "sparoa_fc_adapted": (ctypes.c_int, [P(FcAdaptedDesc), ctypes.c_int] + [vp] * 10 +
+                              [sz, vp]),
         "sparoa_block_norm": (ctypes.c_int, [P(BlockNormDesc)] + [vp] * 10),
     }
     for name, (res, args) in sig.items():
@@ -611,6 +632,63 @@ def sparoa_expert_plan(tokens, top_k, experts, idx, plan, workspace, stream=None
         tokens, top_k, experts, _whole(idx, torch.int32, tokens * top_k, "idx"),
         _whole(plan, torch.int32, sparoa_expert_plan_words(tokens, top_k, experts), "plan"),
         ws, ws_bytes, _stream(stream)))
+
+
+def expert_ffn_desc(tokens, top_k, experts, hidden, inner, dtype=BF16, gated=False,
+                    has_bias=False):
+    if isinstance(dtype, torch.dtype):
+        dtype = dtype_code(dtype)
+    return ExpertFfnDesc(tokens, top_k, experts, hidden, inner, dtype, int(gated), int(has_bias))
+
+
+def sparoa_expert_ffn_workspace_size(desc):
+    s = ctypes.c_size_t()
+    _check(_L.sparoa_expert_ffn_workspace_size(ctypes.byref(desc), ctypes.byref(s)))
+    return s.value
+
+
+def sparoa_expert_ffn(desc, act, x, w_up, b_up, w_down, b_down, weights, plan, residual, y,
+                      workspace, stream=None):
+    """The FFN of every token's experts, weighted and summed (see sparoa.h)."""
+    d, dt = desc, _DT_TORCH.get(desc.dtype)
+    rows, tok = d.experts * d.inner * (2 if d.gated else 1), d.tokens * d.hidden
+    ws, ws_bytes = _scratch(workspace)
+    _check(_L.sparoa_expert_ffn(
+        ctypes.byref(d), act, _whole(x, dt, tok, "x"), _whole(w_up, dt, rows * d.hidden, "w_up"),
+        _whole(b_up, dt, rows, "b_up"),
+        _whole(w_down, dt, d.experts * d.hidden * d.inner, "w_down"),
+        _whole(b_down, dt, d.experts * d.hidden, "b_down"),
+        _whole(weights, torch.float32, d.tokens * d.top_k, "weights"),
+        _whole(plan, torch.int32, sparoa_expert_plan_words(d.tokens, d.top_k, d.experts), "plan"),
+        _whole(residual, dt, tok, "residual"), _whole(y, dt, tok, "y"), ws, ws_bytes,
+        _stream(stream)))
+
+
+def fc_adapted_desc(m, k, n, adapters, rank, dtype=BF16, has_bias=False):
+    if isinstance(dtype, torch.dtype):
+        dtype = dtype_code(dtype)
+    return FcAdaptedDesc(m, k, n, adapters, rank, dtype, int(has_bias))
+
+
+def sparoa_fc_adapted_workspace_size(desc):
+    s = ctypes.c_size_t()
+    _check(_L.sparoa_fc_adapted_workspace_size(ctypes.byref(desc), ctypes.byref(s)))
+    return s.value
+
+
+def sparoa_fc_adapted(desc, act, x, w_nk, bias, lora_a, lora_b, scale, adapter_ids, residual, y,
+                      workspace, stream=None):
+    """FC with the low-rank adapter of each row's request (see sparoa.h)."""
+    d, dt = desc, _DT_TORCH.get(desc.dtype)
+    ws, ws_bytes = _scratch(workspace)
+    _check(_L.sparoa_fc_adapted(
+        ctypes.byref(d), act, _whole(x, dt, d.m * d.k, "x"), _whole(w_nk, dt, d.n * d.k, "w_nk"),
+        _whole(bias, dt, d.n, "bias"), _whole(lora_a, dt, d.adapters * d.rank * d.k, "lora_a"),
+        _whole(lora_b, dt, d.adapters * d.n * d.rank, "lora_b"),
+        _whole(scale, torch.float32, d.adapters, "scale"),
+        _whole(adapter_ids, torch.int32, d.m, "adapter_ids"),
+        _whole(residual, dt, d.m * d.n, "residual"), _whole(y, dt, d.m * d.n, "y"), ws, ws_bytes,
+        _stream(stream)))
 
 
 def block_norm_desc(rows, cols, dtype=BF16, post=NORM_NONE, pre=NORM_RMS, eps=1e-6,

@@ -38,4 +38,46 @@ sparoa_status launch_expert_route(RouteArgs a, sparoa_dtype dt, hipStream_t stre
 sparoa_status launch_expert_plan(RouteArgs a, hipStream_t stream);
 size_t expert_plan_workspace(int64_t tokens, int64_t experts);
 
+// Products of gathered or consecutive rows with the weights of their segment
+// (rows_gemm.hip): y[p] = epilogue(W_s x[p]), rows p of segment s.
+//   experts: segments are the plan's experts, weights w + s * w_stride;
+//            up: x rows gathered through order; down: consecutive.
+//   fc:      one segment of `rows` consecutive rows, low-rank adapters.
+struct RowsArgs {
+  const void *x, *w, *bias, *residual;
+  void *y;
+  int64_t rows;                // slots (experts) or rows (fc)
+  int64_t x_bytes;             // gathered x: bytes of the whole of it (< 2^31)
+  int64_t ldx, ldy;            // elements per row of x and y
+  int n, k;                    // output columns, depth
+  int64_t w_stride;            // elements between segments' weights
+  int w_rows;                  // weight rows of a segment (2 n: gate rows, then up rows)
+  int act;
+  // experts
+  const int32_t *plan, *order; // order: gather through it (null: consecutive)
+  int experts, top_k;
+  // adapters: y += h[row] b[ids[row]]^T before bias and activation
+  const int32_t *ids;          // [rows]; outside [0, adapters): none
+  const void *h, *b;           // h [rows][ldh], b [adapters][n][rank]
+  const float *scale;          // (shrink: h = scale_a A_a x)
+  int adapters, rank, ldh;
+  int h_f32;                   // h is fp32 whatever the dtype
+};
+enum RowsMode { kRowsUp, kRowsUpGated, kRowsDown, kRowsFc, kRowsShrink };
+sparoa_status launch_rows(RowsMode mode, const RowsArgs &a, sparoa_dtype dt, hipStream_t stream);
+// Whether the tile kernel (16-bit h) serves an adapted FC of these sizes.
+bool fc_adapted_tiles(int64_t m, int64_t k, int64_t n, int64_t rank, sparoa_dtype dt);
+
+// y[t] = residual[t] + sum_j weights[t][j] z[place[t][j]]
+struct CombineArgs {
+  const float *z;              // the down products, fp32
+  const void *residual;
+  const float *weights;
+  const int32_t *place;
+  void *y;
+  int64_t tokens, hidden, ldz;
+  int top_k;
+};
+sparoa_status launch_combine(const CombineArgs &a, sparoa_dtype dt, hipStream_t stream);
+
 }  // namespace sparoa

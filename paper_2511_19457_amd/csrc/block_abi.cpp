@@ -65,6 +65,61 @@ void set_plan(RouteArgs &a, int32_t *plan) {
   a.place = plan ? plan + plan_place(a.experts, a.tokens * a.top_k) : nullptr;
 }
 
+bool act_ok(int a, int last) { return a >= SPAROA_ACT_NONE && a <= last; }
+
+// Bytes of an operand the kernels address with 31 bits.
+bool below_2gib(int64_t rows, int64_t cols, int64_t size) {
+  return product_ok(rows, cols, size) && rows * cols * size < (int64_t)1 << 31;
+}
+
+int64_t round8(int64_t n) { return (n + 7) / 8 * 8; }
+size_t section(int64_t bytes) { return (size_t)((bytes + 255) / 256 * 256); }
+
+sparoa_status check_ffn(const sparoa_expert_ffn_desc *d) {
+  if (!d) return fail(SPAROA_ERR_INVALID_ARG, "null expert_ffn descriptor");
+  if (!dtype_ok(d->dtype)) return fail(SPAROA_ERR_INVALID_ARG, "unknown dtype");
+  sparoa_status st = check_plan(d->tokens, d->top_k, d->experts);
+  if (st != SPAROA_OK) return st;
+  if (d->hidden <= 0 || d->inner <= 0)
+    return fail(SPAROA_ERR_INVALID_ARG, "expert_ffn: sizes must be > 0");
+  const int64_t size = elem_size(d->dtype);
+  if (d->inner > INT32_MAX / 4 || !below_2gib(d->tokens, d->hidden, size) ||
+      !below_2gib(d->inner * (d->gated ? 2 : 1), d->hidden, size))
+    return fail(SPAROA_ERR_UNSUPPORTED, "expert_ffn: x or an expert's matrix of 2 GiB or more");
+  if (!product_ok(d->tokens * d->top_k, round8(d->inner) + round8(d->hidden), 4) ||
+      !product_ok(d->experts, 2 * d->inner * size, d->hidden))
+    return fail(SPAROA_ERR_INVALID_ARG, "expert_ffn: sizes too large");
+  return SPAROA_OK;
+}
+// Workspace: u, then the down products.
+size_t ffn_u_bytes(const sparoa_expert_ffn_desc &d) {
+  return section(d.tokens * d.top_k * round8(d.inner) * elem_size(d.dtype));
+}
+size_t ffn_bytes(const sparoa_expert_ffn_desc &d) {
+  return ffn_u_bytes(d) + section(d.tokens * d.top_k * round8(d.hidden) * 4);
+}
+
+sparoa_status check_adapted(const sparoa_fc_adapted_desc *d) {
+  if (!d) return fail(SPAROA_ERR_INVALID_ARG, "null fc_adapted descriptor");
+  if (!dtype_ok(d->dtype)) return fail(SPAROA_ERR_INVALID_ARG, "unknown dtype");
+  if (d->m <= 0 || d->k <= 0 || d->n <= 0 || d->adapters <= 0 || d->rank <= 0)
+    return fail(SPAROA_ERR_INVALID_ARG, "fc_adapted: sizes must be > 0");
+  const int64_t size = elem_size(d->dtype);
+  if (d->rank > 512) return fail(SPAROA_ERR_UNSUPPORTED, "fc_adapted: rank above 512");
+  if (d->adapters > INT32_MAX || !below_2gib(256, d->k, size) || !below_2gib(256, d->n, size) ||
+      !below_2gib(d->n, d->k, size) || !below_2gib(d->rank, d->k, size) ||
+      !below_2gib(d->n, d->rank, size))
+    return fail(SPAROA_ERR_UNSUPPORTED, "fc_adapted: rows of x or a matrix of 2 GiB or more");
+  if (!product_ok(d->m, d->k, size) || !product_ok(d->m, d->n, size) ||
+      !product_ok(d->m, round8(d->rank), 4) ||
+      !product_ok(d->adapters, d->rank * size, d->k > d->n ? d->k : d->n))
+    return fail(SPAROA_ERR_INVALID_ARG, "fc_adapted: sizes too large");
+  return SPAROA_OK;
+}
+size_t adapted_bytes(const sparoa_fc_adapted_desc &d) {
+  return section(d.m * round8(d.rank) * 4);   // h, fp32 or dtype
+}
+
 }  // namespace
 
 extern "C" {
@@ -143,6 +198,114 @@ sparoa_status sparoa_expert_plan(int64_t tokens, int64_t top_k, int64_t experts,
   a.counts = reinterpret_cast<uint32_t *>(workspace);
   set_plan(a, plan);
   return launch_expert_plan(a, stream);
+}
+
+// -------------------------------------------------------- experts' products
+
+sparoa_status sparoa_expert_ffn_workspace_size(const sparoa_expert_ffn_desc *d, size_t *bytes) {
+  clear_error();
+  if (!bytes) return fail(SPAROA_ERR_INVALID_ARG, "null result pointer");
+  sparoa_status st = check_ffn(d);
+  if (st != SPAROA_OK) return st;
+  *bytes = ffn_bytes(*d);
+  return SPAROA_OK;
+}
+
+sparoa_status sparoa_expert_ffn(const sparoa_expert_ffn_desc *d, sparoa_act act, const void *x,
+                                const void *w_up, const void *b_up, const void *w_down,
+                                const void *b_down, const float *weights, const int32_t *plan,
+                                const void *residual, void *y, void *workspace, size_t ws_bytes,
+                                hipStream_t stream) {
+  clear_error();
+  sparoa_status st = check_ffn(d);
+  if (st != SPAROA_OK) return st;
+  if (!act_ok(act, SPAROA_ACT_GELU)) return fail(SPAROA_ERR_INVALID_ARG, "unknown activation");
+  if (!x || !w_up || !w_down || !weights || !plan || !y)
+    return fail(SPAROA_ERR_INVALID_ARG, "expert_ffn: null x, weights, plan or y");
+  if ((d->has_bias != 0) != (b_up != nullptr) || (d->has_bias != 0) != (b_down != nullptr))
+    return fail(SPAROA_ERR_INVALID_ARG, "expert_ffn: has_bias does not match the biases");
+  st = check_ptrs16({x, w_up, b_up, w_down, b_down, weights, plan, residual, y, workspace});
+  if (st != SPAROA_OK) return st;
+  if (!workspace || ws_bytes < ffn_bytes(*d))
+    return fail(SPAROA_ERR_WORKSPACE, "expert_ffn: workspace too small");
+  const int64_t slots = d->tokens * d->top_k, size = elem_size(d->dtype);
+  const int64_t ldu = round8(d->inner), ldz = round8(d->hidden);
+  const int up_rows = (int)d->inner * (d->gated ? 2 : 1);
+  char *ws = reinterpret_cast<char *>(workspace);
+  void *u = ws, *z = ws + ffn_u_bytes(*d);
+  RowsArgs a{};
+  a.rows = slots;
+  a.plan = plan;
+  a.experts = (int)d->experts, a.top_k = (int)d->top_k;
+  a.x = x, a.w = w_up, a.bias = b_up, a.y = u;
+  a.order = plan + plan_order(d->experts);
+  a.x_bytes = d->tokens * d->hidden * size;
+  a.ldx = d->hidden, a.ldy = ldu;
+  a.n = (int)d->inner, a.k = (int)d->hidden;
+  a.w_rows = up_rows, a.w_stride = (int64_t)up_rows * d->hidden;
+  a.act = act;
+  st = launch_rows(d->gated ? kRowsUpGated : kRowsUp, a, d->dtype, stream);
+  if (st != SPAROA_OK) return st;
+  a.x = u, a.w = w_down, a.bias = b_down, a.y = z;
+  a.order = nullptr;
+  a.ldx = ldu, a.ldy = ldz;
+  a.n = (int)d->hidden, a.k = (int)d->inner;
+  a.w_rows = (int)d->hidden, a.w_stride = d->hidden * d->inner;
+  st = launch_rows(kRowsDown, a, d->dtype, stream);
+  if (st != SPAROA_OK) return st;
+  const CombineArgs c{reinterpret_cast<const float *>(z), residual, weights,
+                      plan + plan_place(d->experts, slots), y, d->tokens, d->hidden, ldz,
+                      (int)d->top_k};
+  return launch_combine(c, d->dtype, stream);
+}
+
+// -------------------------------------------------------------- adapted FC
+
+sparoa_status sparoa_fc_adapted_workspace_size(const sparoa_fc_adapted_desc *d, size_t *bytes) {
+  clear_error();
+  if (!bytes) return fail(SPAROA_ERR_INVALID_ARG, "null result pointer");
+  sparoa_status st = check_adapted(d);
+  if (st != SPAROA_OK) return st;
+  *bytes = adapted_bytes(*d);
+  return SPAROA_OK;
+}
+
+sparoa_status sparoa_fc_adapted(const sparoa_fc_adapted_desc *d, sparoa_act act, const void *x,
+                                const void *w_nk, const void *bias, const void *lora_a,
+                                const void *lora_b, const float *scale,
+                                const int32_t *adapter_ids, const void *residual, void *y,
+                                void *workspace, size_t ws_bytes, hipStream_t stream) {
+  clear_error();
+  sparoa_status st = check_adapted(d);
+  if (st != SPAROA_OK) return st;
+  if (!act_ok(act, SPAROA_ACT_RELU6)) return fail(SPAROA_ERR_INVALID_ARG, "unknown activation");
+  if (!x || !w_nk || !lora_a || !lora_b || !scale || !adapter_ids || !y)
+    return fail(SPAROA_ERR_INVALID_ARG, "fc_adapted: null x, w, adapters, ids or y");
+  if ((d->has_bias != 0) != (bias != nullptr))
+    return fail(SPAROA_ERR_INVALID_ARG, "fc_adapted: has_bias does not match bias");
+  st = check_ptrs16({x, w_nk, bias, lora_a, lora_b, scale, adapter_ids, residual, y, workspace});
+  if (st != SPAROA_OK) return st;
+  if (!workspace || ws_bytes < adapted_bytes(*d))
+    return fail(SPAROA_ERR_WORKSPACE, "fc_adapted: workspace too small");
+  RowsArgs a{};
+  a.rows = d->m;
+  a.ids = adapter_ids;
+  a.scale = scale;
+  a.adapters = (int)d->adapters, a.rank = (int)d->rank, a.ldh = (int)round8(d->rank);
+  a.h_f32 = 1;
+  a.x = x, a.w = lora_a, a.y = workspace;
+  a.ldx = d->k, a.ldy = a.ldh;
+  a.n = (int)d->rank, a.k = (int)d->k;
+  a.w_rows = (int)d->rank, a.w_stride = d->rank * d->k;
+  st = launch_rows(kRowsShrink, a, d->dtype, stream);
+  if (st != SPAROA_OK) return st;
+  a.w = w_nk, a.bias = bias, a.residual = residual, a.y = y;
+  a.h = workspace, a.b = lora_b;
+  a.ldy = d->n;
+  a.n = (int)d->n;
+  a.w_rows = (int)d->n, a.w_stride = 0;
+  a.act = act;
+  return launch_rows(kRowsFc, a, d->dtype, stream);
 }
 
 // ------------------------------------------------------------- block norm

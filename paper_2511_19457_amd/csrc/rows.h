@@ -1,0 +1,89 @@
+// What the row-product kernels share: MFMA over 16-byte operand pieces,
+// activations, epilogue pieces.
+#pragma once
+
+#include "block.h"
+#include "dtype.h"
+
+namespace sparoa {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// acc += W X^T of a 16 x 16 block over the 4 lanes' pieces of K: lane l holds
+// 16 bytes of W's row l & 15 and of X's row l & 15, the same elements of K on
+// both sides (a product over K asks for no order of them).  The result's lane
+// holds W rows 4 (l >> 4) + i of X row l & 15.
+template <int DT>
+__device__ __forceinline__ f32x4 mma16(u32x4 w, u32x4 x, f32x4 acc) {
+  if constexpr (DT == SPAROA_BF16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w),
+                                                   __builtin_bit_cast(bf16x8, x), acc, 0, 0, 0);
+  } else if constexpr (DT == SPAROA_F16) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, w),
+                                                  __builtin_bit_cast(f16x8, x), acc, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[i]), __uint_as_float(x[i]),
+                                                 acc, 0, 0, 0);
+    return acc;
+  }
+}
+
+__device__ __forceinline__ float block_act(float v, int act) {
+  if (act == SPAROA_ACT_SILU) return v / (1.f + expf(-v));
+  if (act == SPAROA_ACT_GELU) return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
+  return apply_act(v, act);
+}
+
+// V consecutive elements from an address aligned to them (V sizeof <= 16).
+template <int DT, int V>
+__device__ __forceinline__ void load_elems(const void *p, int64_t at, float (&v)[V]) {
+  using E = Elem<DT>;
+  using raw = typename E::raw;
+  raw r[V];
+  __builtin_memcpy(r, __builtin_assume_aligned(reinterpret_cast<const raw *>(p) + at,
+                                               V * E::size), V * E::size);
+#pragma unroll
+  for (int e = 0; e < V; ++e) v[e] = E::to_f32(r[e]);
+}
+template <int DT, int V>
+__device__ __forceinline__ void store_elems(void *p, int64_t at, const float (&v)[V]) {
+  using E = Elem<DT>;
+  using raw = typename E::raw;
+  raw r[V];
+#pragma unroll
+  for (int e = 0; e < V; ++e) r[e] = E::from_f32(v[e]);
+  __builtin_memcpy(__builtin_assume_aligned(reinterpret_cast<raw *>(p) + at, V * E::size), r,
+                   V * E::size);
+}
+
+// The distinct values in [0, limit) of ids[0 .. n), in order of appearance, to
+// LDS list; the whole wave, 64 BATCHES >= n.  Returns their number.
+template <int BATCHES>
+__device__ __forceinline__ int distinct_ids(const int32_t *ids, int n, int limit, int32_t *list) {
+  const int lane = threadIdx.x & 63;
+  int id[BATCHES];
+  uint64_t left[BATCHES];
+#pragma unroll
+  for (int b = 0; b < BATCHES; ++b) {
+    id[b] = 64 * b + lane < n ? ids[64 * b + lane] : -1;
+    left[b] = __ballot((uint32_t)id[b] < (uint32_t)limit);
+  }
+  int found = 0;
+#pragma unroll
+  for (int b = 0; b < BATCHES; ++b)
+    while (left[b]) {
+      const int a = __builtin_amdgcn_readlane(id[b], __builtin_ctzll(left[b]));
+      if (lane == 0) list[found] = a;
+      ++found;
+#pragma unroll
+      for (int c = b; c < BATCHES; ++c) left[c] &= ~__ballot(id[c] == a);
+    }
+  return found;
+}
+
+}  // namespace sparoa
