@@ -11,7 +11,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libsparoa.so")
 SOURCES = ["abi.cpp", "measure.hip", "gemm.hip", "fc_bw.hip", "direct.hip", "noalloc.hip",
            "pointwise.hip", "block_abi.cpp", "norm.hip",
-           "expert_route.hip", "rows_stream.hip"]
+           "expert_route.hip", "rows_stream.hip",
+           "rows_tile.hip"]
 OBJDIR = os.path.join(PKG, "_build")
 
 FLAGS = [

@@ -62,11 +62,17 @@ struct RowsArgs {
   const float *scale;          // (shrink: h = scale_a A_a x)
   int adapters, rank, ldh;
   int h_f32;                   // h is fp32 whatever the dtype
+  int col_groups;              // (set by the tile launcher)
 };
 enum RowsMode { kRowsUp, kRowsUpGated, kRowsDown, kRowsFc, kRowsShrink };
 sparoa_status launch_rows(RowsMode mode, const RowsArgs &a, sparoa_dtype dt, hipStream_t stream);
-// Whether the tile kernel (16-bit h) serves an adapted FC of these sizes.
-bool fc_adapted_tiles(int64_t m, int64_t k, int64_t n, int64_t rank, sparoa_dtype dt);
+// The kernels: weights streamed past few rows (any sizes and alignment;
+// rows_stream.hip), tiles through LDS (rows of x and w start on 16 bytes, and
+// with adapters those of b; h in dtype; rows_tile.hip).
+sparoa_status launch_rows_tile(RowsMode mode, const RowsArgs &a, sparoa_dtype dt,
+                               hipStream_t stream);
+// Whether the tile kernel serves a product of these sizes.
+bool rows_tiled(RowsMode mode, const RowsArgs &a, sparoa_dtype dt);
 
 // y[t] = residual[t] + sum_j weights[t][j] z[place[t][j]]
 struct CombineArgs {

@@ -292,18 +292,21 @@ sparoa_status sparoa_fc_adapted(const sparoa_fc_adapted_desc *d, sparoa_act act,
   a.ids = adapter_ids;
   a.scale = scale;
   a.adapters = (int)d->adapters, a.rank = (int)d->rank, a.ldh = (int)round8(d->rank);
-  a.h_f32 = 1;
-  a.x = x, a.w = lora_a, a.y = workspace;
-  a.ldx = d->k, a.ldy = a.ldh;
-  a.n = (int)d->rank, a.k = (int)d->k;
-  a.w_rows = (int)d->rank, a.w_stride = d->rank * d->k;
-  st = launch_rows(kRowsShrink, a, d->dtype, stream);
+  a.x = x;
+  a.ldx = d->k, a.ldy = d->n;
+  a.n = (int)d->n, a.k = (int)d->k;
+  // h in fp32 where the weights are streamed, else an operand of MFMA
+  a.h_f32 = !rows_tiled(kRowsFc, a, d->dtype);
+  RowsArgs s = a;
+  s.w = lora_a, s.y = workspace;
+  s.ldy = a.ldh;
+  s.n = s.w_rows = (int)d->rank;
+  s.w_stride = d->rank * d->k;
+  st = launch_rows(kRowsShrink, s, d->dtype, stream);
   if (st != SPAROA_OK) return st;
   a.w = w_nk, a.bias = bias, a.residual = residual, a.y = y;
   a.h = workspace, a.b = lora_b;
-  a.ldy = d->n;
-  a.n = (int)d->n;
-  a.w_rows = (int)d->n, a.w_stride = 0;
+  a.w_rows = (int)d->n;
   a.act = act;
   return launch_rows(kRowsFc, a, d->dtype, stream);
 }

@@ -329,7 +329,16 @@ void launch_combine_dt(const CombineArgs &a, hipStream_t stream) {
 
 }  // namespace
 
+bool rows_tiled(RowsMode mode, const RowsArgs &a, sparoa_dtype dt) {
+  const int v = 16 / (int)elem_size(dt);
+  if (mode == kRowsShrink || a.k % v || a.ldx % v) return false;
+  if (mode == kRowsFc)
+    return a.rank % v == 0 && a.rows > 256 && cdiv(a.rows, 128) * cdiv(a.n, 256) >= 128;
+  return a.rows / std::min<int64_t>(a.experts, a.rows) > 64;
+}
+
 sparoa_status launch_rows(RowsMode mode, const RowsArgs &a, sparoa_dtype dt, hipStream_t stream) {
+  if (rows_tiled(mode, a, dt)) return launch_rows_tile(mode, a, dt, stream);
   const int v = 16 / (int)elem_size(dt);
   const bool vec = a.k % v == 0 && a.ldx % v == 0;   // rows of x and w start on 16 bytes
   switch (dt) {
