@@ -22,28 +22,38 @@ namespace {
 constexpr int kNW = 8, kNT = 64 * kNW;   // waves, threads
 constexpr uint32_t kOut = 0x80000000u;   // past every descriptor's range
 
+// A word every lane wants alike, by the scalar unit: memory that no kernel of
+// this launch writes.
+__device__ __forceinline__ int uniform_word(const int32_t *p) {
+  return *reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(
+      reinterpret_cast<uintptr_t>(p));
+}
+
+// One operand matrix.  VEC: 16-byte pieces by buffer loads; else element by
+// element (rows that start anywhere).
 template <int DT, bool VEC>
 struct Operand {
   using raw = typename Elem<DT>::raw;
-  __amdgpu_buffer_rsrc_t rsrc;
-  const raw *base;
-  __device__ Operand(const void *p, int64_t bytes) {
-    base = reinterpret_cast<const raw *>(p);
-    if constexpr (VEC)
-      rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), (short)0, (int)bytes,
-                                               kBufDword3);
-  }
-  // 16 bytes of K from byte kb of the row at byte offset `row` (kOut: none).
-  __device__ __forceinline__ u32x4 piece(uint32_t row, int kb, int kbytes) const {
+  const void *base;
+  int bytes;
+  __device__ Operand(const void *p, int64_t n) : base(p), bytes((int)n) {}
+  // 16 bytes of K from byte kb + at of the row at byte offset `row` (kOut:
+  // none); kb alike in every lane, at < 128.  VEC: the whole 16 bytes lie
+  // before kbytes, or kb does not and they read zero.
+  __device__ __forceinline__ u32x4 piece(uint32_t row, int kb, int at, int kbytes) const {
     if constexpr (VEC) {
-      return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                                           rsrc, kb < kbytes ? row + kb : kOut, 0, 0));
-    } else {   // rows that start anywhere: element by element
+      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<void *>(base), (short)0, kb < kbytes ? bytes : 0, kBufDword3);
+      return __builtin_bit_cast(u32x4,
+                                __builtin_amdgcn_raw_buffer_load_b128(rsrc, row + at, kb, 0));
+    } else {
       constexpr int S = Elem<DT>::size;
       raw v[16 / S];
 #pragma unroll
       for (int e = 0; e < 16 / S; ++e)
-        v[e] = !(row & kOut) && kb + e * S < kbytes ? base[(row + kb) / S + e] : (raw)0;
+        v[e] = !(row & kOut) && kb + at + e * S < kbytes
+                   ? reinterpret_cast<const raw *>(base)[(row + kb + at) / S + e]
+                   : (raw)0;
       u32x4 r;
       __builtin_memcpy(&r, v, 16);
       return r;
@@ -51,20 +61,82 @@ struct Operand {
   }
 };
 
+// sum over the rank of h[row] b[adapter of row][ch].
+template <int DT>
+__device__ __forceinline__ float adapter_share(const RowsArgs &a, int64_t row, int ch) {
+  using E = Elem<DT>;
+  const int id = a.ids[row];
+  if ((uint32_t)id >= (uint32_t)a.adapters) return 0.f;
+  const float *h = reinterpret_cast<const float *>(a.h) + row * a.ldh;
+  const int64_t at = ((int64_t)id * a.n + ch) * a.rank;
+  float d = 0.f;
+  constexpr int V = 16 / E::size;
+  if (a.rank % V == 0) {   // (rows of b start on 16 bytes)
+#pragma unroll 2
+    for (int r = 0; r < a.rank; r += V) {
+      float bv[V];
+      load_elems<DT, V>(a.b, at + r, bv);
+#pragma unroll
+      for (int e = 0; e < V; e += 4) {
+        const f32x4 hv = *reinterpret_cast<const f32x4 *>(h + r + e);
+#pragma unroll
+        for (int z = 0; z < 4; ++z) d = fmaf(hv[z], bv[e + z], d);
+      }
+    }
+  } else {
+    for (int r = 0; r < a.rank; ++r)
+      d = fmaf(h[r], E::to_f32(reinterpret_cast<const typename E::raw *>(a.b)[at + r]), d);
+  }
+  return d;
+}
+
+// h[row][r] = scale_a a_a[r] x[row]: a wave per row and r (few rows, where
+// their adapters differ).
+template <int DT, bool VEC>
+__global__ __launch_bounds__(256) void shrink_rows_kernel(RowsArgs a) {
+  using E = Elem<DT>;
+  using raw = typename E::raw;
+  const int64_t row = blockIdx.y;
+  const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int id = a.ids[row];
+  if (r >= a.n || (uint32_t)id >= (uint32_t)a.adapters) return;   // (whole waves)
+  const raw *x = reinterpret_cast<const raw *>(a.x) + row * a.ldx;
+  const raw *w = reinterpret_cast<const raw *>(a.w) + id * a.w_stride + (int64_t)r * a.k;
+  constexpr int V = VEC ? 16 / E::size : 1;
+  float s = 0.f;
+#pragma unroll 4
+  for (int k = lane * V; k < a.k; k += 64 * V) {
+    float xv[V], wv[V];
+    load_elems<DT, V>(x, k, xv);
+    load_elems<DT, V>(w, k, wv);
+#pragma unroll
+    for (int e = 0; e < V; ++e) s = fmaf(xv[e], wv[e], s);
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+  if (lane == 0) reinterpret_cast<float *>(a.y)[row * a.ldy + r] = s * a.scale[id];
+}
+
+// (VEC, up to 32 rows: two work-groups a CU, one's start and end under the
+// other's stream)
 template <int DT, bool VEC, RowsMode MODE, int MT, int NB>
-__global__ __launch_bounds__(kNT) void rows_stream_kernel(RowsArgs a) {
+__global__ __launch_bounds__(kNT, VEC && MODE != kRowsFc && MT <= 2 && NB <= 2 ? 4 : 2) void rows_stream_kernel(RowsArgs a) {
   using E = Elem<DT>;
   constexpr bool GATED = MODE == kRowsUpGated, EXPERTS = MODE <= kRowsDown;
   constexpr int WB = GATED ? 2 * NB : NB;      // weight blocks of 16 rows
-  constexpr int PF = VEC ? (WB + MT <= 3 ? 4 : 2) : 1;   // steps in flight
+  constexpr bool FC = MODE == kRowsFc;
+  constexpr int PF = VEC ? std::max(2, (FC ? 12 : 8) / (WB + MT)) : 1;   // steps in flight
   __shared__ f32x4 part[kNW][WB * MT][64];
-  __shared__ int32_t list[16 * MT];
+  __shared__ float tail[FC ? 16 * MT : 1][FC ? 16 * NB + 1 : 1];   // the adapters' share
+  __shared__ int32_t list[MODE == kRowsShrink ? 16 * MT : 1];
   __shared__ int list_len;
 
   const int tid = threadIdx.x, lane = tid & 63, rl = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n0 = blockIdx.x * 16 * NB;
-  const int kbytes = a.k * E::size, steps = (kbytes + 127) / 128;
+  const int kbytes = a.k * E::size;
+  // whole steps; VEC: what is left of K is a step of its own, behind them
+  const int steps = VEC ? kbytes / 128 : (kbytes + 127) / 128;
 
   uint32_t woff[WB];
 #pragma unroll
@@ -76,13 +148,13 @@ __global__ __launch_bounds__(kNT) void rows_stream_kernel(RowsArgs a) {
 
   // experts: the blockIdx.y-th that has rows, its rows tile by tile; else
   // tiles of rows, every gridDim.y-th
-  const int64_t groups = EXPERTS ? a.plan[a.experts + 1] : (a.rows + 16 * MT - 1) / (16 * MT);
+  const int64_t groups = EXPERTS ? uniform_word(a.plan + a.experts + 1) : (a.rows + 16 * MT - 1) / (16 * MT);
   for (int64_t group = blockIdx.y; group < groups; group += gridDim.y) {
     int64_t s0, s1;
     int seg = 0, items = 1;
     if constexpr (EXPERTS) {
-      seg = a.plan[a.experts + 2 + group];
-      s0 = a.plan[seg], s1 = a.plan[seg + 1];
+      seg = uniform_word(a.plan + a.experts + 2 + group);
+      s0 = uniform_word(a.plan + seg), s1 = uniform_word(a.plan + seg + 1);
     } else {
       s0 = group * 16 * MT;
       s1 = s0 + 16 * MT < a.rows ? s0 + 16 * MT : a.rows;
@@ -107,15 +179,11 @@ __global__ __launch_bounds__(kNT) void rows_stream_kernel(RowsArgs a) {
         const Operand<DT, VEC> x(
             gather ? a.x : reinterpret_cast<const char *>(a.x) + r0 * a.ldx * E::size,
             gather ? a.x_bytes : std::min<int64_t>(s1 - r0, 16 * MT) * a.ldx * E::size);
-        uint32_t xoff[MT];
+        int slot[MT];   // (sent for first: loads land in order)
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-          const int64_t p = r0 + 16 * t + rl;
-          bool in = p < s1;
-          uint32_t row = 16 * t + rl;
-          if (gather && in) row = (uint32_t)a.order[p] / (uint32_t)a.top_k;
-          if (MODE == kRowsShrink && in) in = a.ids[p] == seg;
-          xoff[t] = in ? row * (uint32_t)(a.ldx * E::size) : kOut;
+          const int64_t p = r0 + 16 * t + rl < s1 ? r0 + 16 * t + rl : s1 - 1;
+          slot[t] = gather ? a.order[p] : MODE == kRowsShrink ? a.ids[p] : 0;
         }
 
         f32x4 acc[WB][MT];
@@ -124,34 +192,72 @@ __global__ __launch_bounds__(kNT) void rows_stream_kernel(RowsArgs a) {
 #pragma unroll
           for (int t = 0; t < MT; ++t) acc[b][t] = f32x4{0.f, 0.f, 0.f, 0.f};
         u32x4 wq[PF][WB][2], xq[PF][MT][2];
-        auto load = [&](int i, int step) __attribute__((always_inline)) {
-          const int kb = step * 128 + q * 32;
+        uint32_t xoff[MT];
+        auto load_w = [&](int i, int kb, int end) __attribute__((always_inline)) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int b = 0; b < WB; ++b) wq[i][b][h] = w.piece(woff[b], kb, q * 32 + 16 * h, end);
+        };
+        auto load_x = [&](int i, int kb, int end) __attribute__((always_inline)) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int t = 0; t < MT; ++t) xq[i][t][h] = x.piece(xoff[t], kb, q * 32 + 16 * h, end);
+        };
+        auto multiply = [&](int i) __attribute__((always_inline)) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int b = 0; b < WB; ++b)
+#pragma unroll
+              for (int t = 0; t < MT; ++t)
+                acc[b][t] = mma16<DT>(wq[i][b][h], xq[i][t][h], acc[b][t]);
+        };
+        const int kend = VEC ? steps * 128 : kbytes;
+        // (the weights are sent for before the rows' places are known)
+#pragma unroll
+        for (int i = 0; i < PF; ++i) load_w(i, (wave + i * kNW) * 128, kend);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+          uint32_t row = 16 * t + rl;
+          const bool in = r0 + row < s1 && (MODE != kRowsShrink || slot[t] == seg);
+          if (gather) row = (uint32_t)slot[t] / (uint32_t)a.top_k;
+          xoff[t] = in ? row * (uint32_t)(a.ldx * E::size) : kOut;
+        }
+#pragma unroll
+        for (int i = 0; i < PF; ++i) load_x(i, (wave + i * kNW) * 128, kend);
+        for (int s = wave; s < steps; s += PF * kNW) {
+#pragma unroll
+          for (int i = 0; i < PF; ++i) {
+            multiply(i);
+            load_w(i, (s + (i + PF) * kNW) * 128, kend);
+            load_x(i, (s + (i + PF) * kNW) * 128, kend);
+          }
+        }
+        if (VEC && kend < kbytes && wave == steps % kNW) {   // pieces past K read zero
+          const uint32_t past0 = kend + q * 32 < kbytes ? 0u : kOut;
+          const uint32_t past1 = kend + q * 32 + 16 < kbytes ? 0u : kOut;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
 #pragma unroll
             for (int b = 0; b < WB; ++b)
-              wq[i][b][h] = w.piece(woff[b], kb + 16 * h, kbytes);
+              wq[0][b][h] = w.piece(woff[b] | (h ? past1 : past0), kend, q * 32 + 16 * h, kbytes);
 #pragma unroll
             for (int t = 0; t < MT; ++t)
-              xq[i][t][h] = x.piece(xoff[t], kb + 16 * h, kbytes);
+              xq[0][t][h] = x.piece(xoff[t] | (h ? past1 : past0), kend, q * 32 + 16 * h, kbytes);
           }
-        };
-#pragma unroll
-        for (int i = 0; i < PF; ++i) load(i, wave + i * kNW);
-        for (int s = wave; s < steps; s += PF * kNW) {
-#pragma unroll
-          for (int i = 0; i < PF; ++i) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-              for (int b = 0; b < WB; ++b)
-#pragma unroll
-                for (int t = 0; t < MT; ++t)
-                  acc[b][t] = mma16<DT>(wq[i][b][h], xq[i][t][h], acc[b][t]);
-            load(i, s + (i + PF) * kNW);
-          }
+          multiply(0);
         }
         __syncthreads();   // the last tile's partial sums have been read
+        // the adapters' share of an output is one thread's sum over the rank
+        if constexpr (FC) {
+          if (a.ids)
+            for (int i = tid; i < 256 * MT * NB; i += kNT) {
+              const int r = i / (16 * NB), c = i % (16 * NB);
+              tail[r][c] = r0 + r < s1 && n0 + c < a.n ? adapter_share<DT>(a, r0 + r, n0 + c) : 0.f;
+            }
+        }
 #pragma unroll
         for (int b = 0; b < WB; ++b)
 #pragma unroll
@@ -188,8 +294,7 @@ __global__ __launch_bounds__(kNT) void rows_stream_kernel(RowsArgs a) {
             *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(a.y) + p * a.ldy + ch) = v;
             continue;
           }
-          float o[4];
-          const int adapter = MODE == kRowsFc && a.ids ? a.ids[p] : -1;
+          float o[4], mul[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             float g = v[e], up = u[e];
@@ -200,35 +305,15 @@ __global__ __launch_bounds__(kNT) void rows_stream_kernel(RowsArgs a) {
               g += E::to_f32(bias[c]);
               if (GATED) up += E::to_f32(bias[a.n + c]);
             }
-            if (MODE == kRowsFc && (uint32_t)adapter < (uint32_t)a.adapters) {
-              const float *h = reinterpret_cast<const float *>(a.h) + p * a.ldh;
-              const int64_t at = ((int64_t)adapter * a.n + c) * a.rank;
-              float d = 0.f;
-              if (a.rank % 8 == 0) {   // (rows of b start on 16 bytes)
-                for (int r = 0; r < a.rank; r += 8) {
-                  float bv[8];
-                  if constexpr (E::size == 2) {
-                    load_elems<DT, 8>(a.b, at + r, bv);
-                  } else {
-                    float lo[4], hi[4];
-                    load_elems<DT, 4>(a.b, at + r, lo);
-                    load_elems<DT, 4>(a.b, at + r + 4, hi);
-#pragma unroll
-                    for (int z = 0; z < 4; ++z) bv[z] = lo[z], bv[4 + z] = hi[z];
-                  }
-#pragma unroll
-                  for (int z = 0; z < 8; ++z) d = fmaf(h[r + z], bv[z], d);
-                }
-              } else {
-                for (int r = 0; r < a.rank; ++r)
-                  d = fmaf(h[r], E::to_f32(reinterpret_cast<const typename E::raw *>(a.b)[at + r]), d);
-              }
-              g += d;
-            }
-            if (MODE == kRowsFc && a.residual)
+            if (FC && a.ids) g += tail[16 * t + rl][16 * b + 4 * q + e];
+            if (FC && a.residual)
               g += E::to_f32(reinterpret_cast<const typename E::raw *>(a.residual)[p * a.ldy + c]);
-            o[e] = block_act(g, a.act);
-            if (GATED) o[e] *= up;
+            o[e] = g, mul[e] = up;
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            o[e] = FC ? apply_act(o[e], a.act) : block_act(o[e], a.act);
+            if (GATED) o[e] *= mul[e];
           }
           if (a.ldy % 4 == 0 && ch + 4 <= a.n) {
             store_elems<DT, 4>(a.y, p * a.ldy + ch, o);
@@ -255,11 +340,30 @@ void launch_mode(const RowsArgs &a, hipStream_t stream) {
   const int64_t per = MODE <= kRowsDown ? cdiv(a.rows, std::min<int64_t>(a.experts, a.rows))
                                         : a.rows;
   if constexpr (MODE == kRowsShrink) {
-    launch_one<DT, VEC, MODE, 1, 1>(a, stream);
+    // a wave per row and rank where all that these read is little (they share
+    // nothing but the L2), else tiles of 16 rows that read x once
+    if (a.h_f32 && a.rows <= 32768 &&
+        a.rows * a.n * a.k * Elem<DT>::size <= (int64_t)32 << 20) {
+      const dim3 grid((unsigned)cdiv(a.n, 4), (unsigned)a.rows);
+      shrink_rows_kernel<DT, VEC><<<grid, 256, 0, stream>>>(a);
+    } else if (a.n <= 16 || !VEC) {
+      launch_one<DT, VEC, MODE, 1, 1>(a, stream);
+    } else if (a.n <= 32) {
+      launch_one<DT, VEC, MODE, 1, 2>(a, stream);
+    } else {
+      launch_one<DT, VEC, MODE, 1, 4>(a, stream);
+    }
   } else if constexpr (!VEC) {
     launch_one<DT, VEC, MODE, 4, 1>(a, stream);
   } else {
     constexpr int NB = MODE == kRowsUpGated ? 1 : 2;
+    if (MODE == kRowsFc && cdiv(a.n, 32) * cdiv(a.rows, per <= 16 ? 16 : per <= 32 ? 32 : 64) < 160) {
+      // panels of 16 columns where those of 32 leave too many CUs without one
+      if (per <= 16) launch_one<DT, VEC, MODE, 1, 1>(a, stream);
+      else if (per <= 32) launch_one<DT, VEC, MODE, 2, 1>(a, stream);
+      else launch_one<DT, VEC, MODE, 4, 1>(a, stream);
+      return;
+    }
     if (per <= 16) launch_one<DT, VEC, MODE, 1, NB>(a, stream);
     else if (per <= 32) launch_one<DT, VEC, MODE, 2, NB>(a, stream);
     else launch_one<DT, VEC, MODE, 4, NB>(a, stream);
@@ -291,21 +395,33 @@ __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
     float s[V];
 #pragma unroll
     for (int e = 0; e < V; ++e) s[e] = 0.f;
-    for (int j = 0; j < a.top_k; ++j) {
-      const int p = a.place[t * a.top_k + j];
-      if (p < 0) continue;   // no expert: its weight is not looked at
-      const float w = a.weights[t * a.top_k + j];
-      const float *z = a.z + p * a.ldz + c;
-      if constexpr (V % 4 == 0) {
+    for (int j0 = 0; j0 < a.top_k; j0 += 8) {   // eight rows in flight
+      int p[8];
+      float w[8], z[8][V];
 #pragma unroll
-        for (int e = 0; e < V; e += 4) {
-          const f32x4 q = *reinterpret_cast<const f32x4 *>(z + e);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[e + i] = fmaf(w, q[i], s[e + i]);
-        }
-      } else {
-        s[0] = fmaf(w, z[0], s[0]);
+      for (int j = 0; j < 8; ++j) {
+        const int64_t slot = t * a.top_k + (j0 + j < a.top_k ? j0 + j : 0);
+        p[j] = j0 + j < a.top_k ? a.place[slot] : -1;
+        w[j] = a.weights[slot];
       }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float *from = a.z + (p[j] < 0 ? 0 : p[j]) * a.ldz + c;
+        if constexpr (V % 4 == 0) {
+#pragma unroll
+          for (int e = 0; e < V; e += 4) {
+            const f32x4 q = *reinterpret_cast<const f32x4 *>(from + e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[j][e + i] = q[i];
+          }
+        } else {
+          z[j][0] = from[0];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j)   // no expert: neither weight nor row is looked at
+#pragma unroll
+        for (int e = 0; e < V; ++e) s[e] = p[j] < 0 ? s[e] : fmaf(w[j], z[j][e], s[e]);
     }
     if (a.residual) {
       float r[V];

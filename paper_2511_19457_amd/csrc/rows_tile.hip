@@ -73,6 +73,13 @@ __device__ __forceinline__ int wave_prefix(int v) {
   return v;
 }
 
+int choose_tile(RowsMode mode, const RowsArgs &a) {
+#ifdef ROWS_SWEEP
+  if (const char *e = getenv("ROWS_TILE")) return atoi(e);
+#endif
+  return 0;
+}
+
 struct Tile {
   int seg, col;       // segment; column tile
   int64_t row0, end;  // rows [row0, min(row0 + BM, end)); end 0: no tile
@@ -285,9 +292,11 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
   // One step per chunk: on entry its operands are in registers or on their
   // way.  Steady steps (a next chunk, and a refill that is not K's last) have
   // no branch and constant stages.
-  auto step = [&](auto steady, Operands &cur, Operands &nxt, int slot, int i)
+  // A wave whose rows all lie past the segment only loads.
+  const bool busy_wave = wm * WTM * 16 < rows;
+  auto step = [&](auto steady, auto busy, Operands &cur, Operands &nxt, int slot, int i)
                   __attribute__((always_inline)) {
-    constexpr bool STEADY = decltype(steady)::value;
+    constexpr bool STEADY = decltype(steady)::value, BUSY = decltype(busy)::value;
     const bool more = STEADY || i + 1 < chunks, refill = STEADY || i + S < chunks;
     const uint32_t dst = ring + slot * STAGE;
     if (more) {
@@ -302,8 +311,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
     for (int m = 0; m < MF; ++m) {
       const int ks = m / (WTM * WTN), tm = m / WTN % WTM, b = m % WTN;
       __builtin_amdgcn_sched_barrier(0);
-      acc[tm][b] = mma16<DT>(cur.w[ks][b], cur.x[ks][tm], acc[tm][b]);
-      if (more) {
+      if constexpr (BUSY) acc[tm][b] = mma16<DT>(cur.w[ks][b], cur.x[ks][tm], acc[tm][b]);
+      if (BUSY && more) {
 #pragma unroll
         for (int q = m * R / RSPAN; q < (m + 1) * R / RSPAN && q < R; ++q) read_part(nxt, nslot, q);
       }
@@ -319,23 +328,28 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
     if (s < chunks) load_any(s, ring + s * STAGE);
   wait_ring<S - 1, L>(min(S - 1, chunks - 1));
   asm volatile("s_barrier" ::: "memory");
-  {
+  auto run = [&](auto busy) __attribute__((always_inline)) {
     Operands p, q;
+    if constexpr (decltype(busy)::value) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) read_part(p, 0, r);
+      for (int r = 0; r < R; ++r) read_part(p, 0, r);
+    }
     constexpr int U = S % 2 ? 2 * S : S;   // a turn of the ring and of (p, q)
     int i = 0;
     for (; i + U + S < n; i += U) {
 #pragma unroll
       for (int d = 0; d < U; ++d)
-        step(std::true_type{}, d % 2 ? q : p, d % 2 ? p : q, d % S, i + d);
+        step(std::true_type{}, busy, d % 2 ? q : p, d % 2 ? p : q, d % S, i + d);
     }
     for (; i < chunks; i += U) {
 #pragma unroll
       for (int d = 0; d < U; ++d)
-        if (i + d < chunks) step(std::false_type{}, d % 2 ? q : p, d % 2 ? p : q, d % S, i + d);
+        if (i + d < chunks)
+          step(std::false_type{}, busy, d % 2 ? q : p, d % 2 ? p : q, d % S, i + d);
     }
-  }
+  };
+  if (!busy_wave) return run(std::false_type{});
+  run(std::true_type{});
 
   // ---- epilogue, from registers: 8 consecutive channels of a row at a time
   const int mw = wm * WTM * 16 + rl;
@@ -424,13 +438,24 @@ void launch_one(RowsArgs a, hipStream_t stream) {
   rows_tile_kernel<DT, MODE, WGM, WGN, WTM, WTN, S><<<grid, 64 * WGM * WGN, 0, stream>>>(a);
 }
 
+template <int DT, RowsMode MODE>
+void launch_mode(const RowsArgs &a, hipStream_t stream) {
+  switch (choose_tile(MODE, a)) {
+    case 0: return launch_one<DT, MODE, 2, 4, 4, 4, 3>(a, stream);    // 128 x 256
+    case 1: return launch_one<DT, MODE, 2, 2, 4, 4, 2>(a, stream);    // 128 x 128
+    case 2: return launch_one<DT, MODE, 4, 1, 2, 4, 3>(a, stream);    // 128 x 64
+    case 3: return launch_one<DT, MODE, 2, 2, 2, 4, 3>(a, stream);    // 64 x 128
+    default: return launch_one<DT, MODE, 4, 1, 1, 4, 4>(a, stream);   // 64 x 64
+  }
+}
+
 template <int DT>
 void launch_dt(RowsMode mode, const RowsArgs &a, hipStream_t stream) {
   switch (mode) {
-    case kRowsUp: return launch_one<DT, kRowsUp, 2, 4, 4, 4, 3>(a, stream);
-    case kRowsUpGated: return launch_one<DT, kRowsUpGated, 2, 4, 4, 4, 3>(a, stream);
-    case kRowsDown: return launch_one<DT, kRowsDown, 2, 4, 4, 4, 3>(a, stream);
-    default: return launch_one<DT, kRowsFc, 2, 4, 4, 4, 3>(a, stream);
+    case kRowsUp: return launch_mode<DT, kRowsUp>(a, stream);
+    case kRowsUpGated: return launch_mode<DT, kRowsUpGated>(a, stream);
+    case kRowsDown: return launch_mode<DT, kRowsDown>(a, stream);
+    default: return launch_mode<DT, kRowsFc>(a, stream);
   }
 }
 
