@@ -10,9 +10,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libsparoa.so")
 SOURCES = ["abi.cpp", "measure.hip", "gemm.hip", "fc_bw.hip", "direct.hip", "noalloc.hip",
-           "pointwise.hip", "block_abi.cpp", "norm.hip",
-           "expert_route.hip", "rows_stream.hip",
-           "rows_tile.hip"]
+           "pointwise.hip", "block_abi.cpp", "norm.hip", "expert_route.hip", "rows.hip", "rows_stream.hip",
+           "rows_split.hip", "rows_tile.hip"]
 OBJDIR = os.path.join(PKG, "_build")
 
 FLAGS = [

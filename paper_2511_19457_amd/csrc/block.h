@@ -65,14 +65,20 @@ struct RowsArgs {
   int col_groups;              // (set by the tile launcher)
 };
 enum RowsMode { kRowsUp, kRowsUpGated, kRowsDown, kRowsFc, kRowsShrink };
+// Kernel and tile (rows x weight rows) of a product (rows.hip).
+enum RowsTile {
+  kRowsStream,       // rows of x or w that start off 16 bytes (rows_stream.hip)
+  kTile16x64, kTile32x32, kTile32x32x8,        // waves split K, 4 or 8 (rows_split.hip)
+  kTile64x64, kTile64x128, kTile128x256        // waves share the tile (rows_tile.hip)
+};
+RowsTile rows_tile_for(RowsMode mode, const RowsArgs &a, sparoa_dtype dt);
 sparoa_status launch_rows(RowsMode mode, const RowsArgs &a, sparoa_dtype dt, hipStream_t stream);
-// The kernels: weights streamed past few rows (any sizes and alignment;
-// rows_stream.hip), tiles through LDS (rows of x and w start on 16 bytes, and
-// with adapters those of b; h in dtype; rows_tile.hip).
-sparoa_status launch_rows_tile(RowsMode mode, const RowsArgs &a, sparoa_dtype dt,
+sparoa_status launch_rows_stream(RowsMode mode, const RowsArgs &a, sparoa_dtype dt,
+                                 hipStream_t stream);
+sparoa_status launch_rows_split(RowsMode mode, RowsTile tile, const RowsArgs &a, sparoa_dtype dt,
+                                hipStream_t stream);
+sparoa_status launch_rows_tile(RowsMode mode, RowsTile tile, const RowsArgs &a, sparoa_dtype dt,
                                hipStream_t stream);
-// Whether the tile kernel serves a product of these sizes.
-bool rows_tiled(RowsMode mode, const RowsArgs &a, sparoa_dtype dt);
 
 // y[t] = residual[t] + sum_j weights[t][j] z[place[t][j]]
 struct CombineArgs {

@@ -295,8 +295,8 @@ sparoa_status sparoa_fc_adapted(const sparoa_fc_adapted_desc *d, sparoa_act act,
   a.x = x;
   a.ldx = d->k, a.ldy = d->n;
   a.n = (int)d->n, a.k = (int)d->k;
-  // h in fp32 where the weights are streamed, else an operand of MFMA
-  a.h_f32 = !rows_tiled(kRowsFc, a, d->dtype);
+  // h is an operand of MFMA, but for the stream kernel, which adds it in fp32
+  a.h_f32 = rows_tile_for(kRowsFc, a, d->dtype) == kRowsStream;
   RowsArgs s = a;
   s.w = lora_a, s.y = workspace;
   s.ldy = a.ldh;

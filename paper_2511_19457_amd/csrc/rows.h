@@ -12,6 +12,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
+constexpr uint32_t kOut = 0x80000000u;   // an offset past every descriptor's range
+
 // acc += W X^T of a 16 x 16 block over the 4 lanes' pieces of K: lane l holds
 // 16 bytes of W's row l & 15 and of X's row l & 15, the same elements of K on
 // both sides (a product over K asks for no order of them).  The result's lane

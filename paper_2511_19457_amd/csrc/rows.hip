@@ -1,0 +1,158 @@
+// Row products: the kernel and tile of a product, the adapters' first product
+// of few rows, and the weighted sum of the experts' outputs.
+#include <algorithm>
+
+#include "rows.h"
+
+namespace sparoa {
+namespace {
+
+// h[row][r] = scale_a a_a[r] x[row]: a wave per row and r (few rows, where
+// their adapters differ).
+template <int DT, bool VEC>
+__global__ __launch_bounds__(256) void shrink_rows_kernel(RowsArgs a) {
+  using E = Elem<DT>;
+  using raw = typename E::raw;
+  const int64_t row = blockIdx.y;
+  const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int id = a.ids[row];
+  // (whole waves; columns past the rank, to ldy, are written as zeros)
+  if (r >= a.ldy || (uint32_t)id >= (uint32_t)a.adapters) return;
+  const raw *x = reinterpret_cast<const raw *>(a.x) + row * a.ldx;
+  const raw *w = reinterpret_cast<const raw *>(a.w) + id * a.w_stride + (int64_t)r * a.k;
+  constexpr int V = VEC ? 16 / E::size : 1;
+  float s = 0.f;
+#pragma unroll 4
+  for (int k = lane * V; k < (r < a.n ? a.k : 0); k += 64 * V) {
+    float xv[V], wv[V];
+    load_elems<DT, V>(x, k, xv);
+    load_elems<DT, V>(w, k, wv);
+#pragma unroll
+    for (int e = 0; e < V; ++e) s = fmaf(xv[e], wv[e], s);
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+  if (lane) return;
+  s *= a.scale[id];
+  if (a.h_f32) reinterpret_cast<float *>(a.y)[row * a.ldy + r] = s;
+  else reinterpret_cast<raw *>(a.y)[row * a.ldy + r] = E::from_f32(s);
+}
+
+template <int DT, int V>
+__global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
+  const int64_t per = a.hidden / V, total = a.tokens * per;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
+    const int64_t t = i / per, c = i % per * V;
+    float s[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) s[e] = 0.f;
+    for (int j0 = 0; j0 < a.top_k; j0 += 8) {   // eight rows in flight
+      int p[8];
+      float w[8], z[8][V];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int64_t slot = t * a.top_k + (j0 + j < a.top_k ? j0 + j : 0);
+        p[j] = j0 + j < a.top_k ? a.place[slot] : -1;
+        w[j] = a.weights[slot];
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float *from = a.z + (p[j] < 0 ? 0 : p[j]) * a.ldz + c;
+        if constexpr (V % 4 == 0) {
+#pragma unroll
+          for (int e = 0; e < V; e += 4) {
+            const f32x4 q = *reinterpret_cast<const f32x4 *>(from + e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[j][e + i] = q[i];
+          }
+        } else {
+          z[j][0] = from[0];
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j)   // no expert: neither weight nor row is looked at
+#pragma unroll
+        for (int e = 0; e < V; ++e) s[e] = p[j] < 0 ? s[e] : fmaf(w[j], z[j][e], s[e]);
+    }
+    if (a.residual) {
+      float r[V];
+      load_elems<DT, V>(a.residual, t * a.hidden + c, r);
+#pragma unroll
+      for (int e = 0; e < V; ++e) s[e] += r[e];
+    }
+    store_elems<DT, V>(a.y, t * a.hidden + c, s);
+  }
+}
+
+template <int DT>
+void launch_combine_dt(const CombineArgs &a, hipStream_t stream) {
+  constexpr int V = 16 / Elem<DT>::size;
+  const bool vec = a.hidden % V == 0;
+  const int64_t items = a.tokens * (vec ? a.hidden / V : a.hidden);
+  const unsigned grid = (unsigned)std::min<int64_t>(cdiv(items, 256), 1 << 20);
+  if (vec) combine_kernel<DT, V><<<grid, 256, 0, stream>>>(a);
+  else combine_kernel<DT, 1><<<grid, 256, 0, stream>>>(a);
+}
+
+
+template <int DT>
+void launch_shrink_rows(const RowsArgs &a, hipStream_t stream) {
+  constexpr int V = 16 / Elem<DT>::size;
+  const dim3 grid((unsigned)cdiv(a.ldy, 4), (unsigned)a.rows);
+  if (a.k % V == 0) shrink_rows_kernel<DT, true><<<grid, 256, 0, stream>>>(a);
+  else shrink_rows_kernel<DT, false><<<grid, 256, 0, stream>>>(a);
+}
+
+}  // namespace
+
+RowsTile rows_tile_for(RowsMode mode, const RowsArgs &a, sparoa_dtype dt) {
+  const int v = 16 / (int)elem_size(dt);
+  const bool f32 = dt == SPAROA_F32;
+  if (a.k % v || a.ldx % v) return kRowsStream;
+  const int64_t wide = (int64_t)a.n * (mode == kRowsUpGated ? 2 : 1);
+  if (mode == kRowsFc) {
+    const int64_t t32 = cdiv(a.rows, 32) * cdiv(wide, 32), t64 = cdiv(a.rows, 64) * cdiv(wide, 64);
+    if (a.rows <= 96 || t64 < (f32 ? 256 : 128)) return t32 <= 256 ? kTile32x32x8 : kTile32x32;
+    if (t64 <= 384) return kTile64x64;
+    return !f32 && cdiv(a.rows, 128) * cdiv(wide, 256) >= 384 ? kTile128x256 : kTile64x128;
+  }
+  const int64_t used = std::min<int64_t>(a.experts, a.rows), per = a.rows / used;
+  if (per <= 12) return kTile16x64;
+  if (per < 48) return kTile64x64;
+  if (f32) return per >= 256 ? kTile64x128 : kTile64x64;
+  return per >= 96 && used * cdiv(per, 128) * cdiv(wide, 256) >= 128 ? kTile128x256 : kTile64x128;
+}
+
+sparoa_status launch_rows(RowsMode mode, const RowsArgs &a, sparoa_dtype dt, hipStream_t stream) {
+  if (mode == kRowsShrink) {
+    // a wave per row and rank where all that these read is little (they share
+    // nothing but the L2), else tiles of 16 rows that read x once
+    if (a.rows <= 32768 && a.rows * a.n * a.k * elem_size(dt) <= (int64_t)32 << 20) {
+      switch (dt) {
+        case SPAROA_F32: launch_shrink_rows<SPAROA_F32>(a, stream); break;
+        case SPAROA_F16: launch_shrink_rows<SPAROA_F16>(a, stream); break;
+        default: launch_shrink_rows<SPAROA_BF16>(a, stream); break;
+      }
+      SPAROA_LAUNCH_CHECK("fc_adapted: first product of few rows");
+      return SPAROA_OK;
+    }
+    return a.h_f32 ? launch_rows_stream(mode, a, dt, stream)
+                   : launch_rows_split(mode, kTile16x64, a, dt, stream);
+  }
+  const RowsTile tile = rows_tile_for(mode, a, dt);
+  if (tile == kRowsStream) return launch_rows_stream(mode, a, dt, stream);
+  return tile >= kTile64x64 ? launch_rows_tile(mode, tile, a, dt, stream)
+                            : launch_rows_split(mode, tile, a, dt, stream);
+}
+
+sparoa_status launch_combine(const CombineArgs &a, sparoa_dtype dt, hipStream_t stream) {
+  switch (dt) {
+    case SPAROA_F32: launch_combine_dt<SPAROA_F32>(a, stream); break;
+    case SPAROA_F16: launch_combine_dt<SPAROA_F16>(a, stream); break;
+    default: launch_combine_dt<SPAROA_BF16>(a, stream); break;
+  }
+  SPAROA_LAUNCH_CHECK("expert_ffn: combine");
+  return SPAROA_OK;
+}
+
+}  // namespace sparoa

@@ -1,0 +1,146 @@
+// Rings of K chunks in LDS, and the walk over tiles, of the row-product
+// kernels.
+#pragma once
+
+#include "rows.h"
+
+namespace sparoa {
+
+constexpr int kRow = 128;                // bytes of a chunk row
+
+// s_waitcnt immediates: at most n vector-memory operations outstanding; LDS
+// operations done.
+constexpr int vm_outstanding(int n) { return (n & 15) | (7 << 4) | (15 << 8) | ((n >> 4) << 14); }
+constexpr int kLdsDone = 15 | (7 << 4) | (3 << 14);
+
+// Waits until all but this wave's newest `chunks` <= C chunks' loads (L per
+// chunk) have landed.
+template <int C, int L>
+__device__ __forceinline__ void wait_ring(int chunks) {
+  static_assert(C * L < 64, "vmcnt range");
+  if constexpr (C > 0) {
+    if (chunks < C) return wait_ring<C - 1, L>(chunks);
+  }
+  __builtin_amdgcn_s_waitcnt(vm_outstanding(C * L));
+}
+
+// A 16-byte-per-lane buffer load whose data goes to LDS (lane l's to lds + 16
+// l, lds uniform), zeros where the offset is past the range.  In assembly: by
+// the builtin the compiler cannot tell the ring's stages apart and waits for
+// every load in flight before each LDS read; the waits are at the barriers
+// instead (wait_ring).  It writes no register.  The wait states: a scalar
+// register that a vector instruction wrote (a descriptor from
+// v_readfirstlane, a reloaded one) may be read by a memory instruction five
+// states later, and the compiler does not look into the statement.
+__device__ __forceinline__ void ring_load(u32x4 rsrc, uint32_t lds, uint32_t voffset,
+                                          uint32_t soffset) {
+  asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+               :
+               : "{m0}"(lds), "v"(voffset), "s"(rsrc), "s"(soffset)
+               : "memory");
+}
+__device__ __forceinline__ u32x4 descriptor(const void *p, int64_t bytes) {
+  const uint64_t b = reinterpret_cast<uint64_t>(p);
+  return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b),
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32) & 0xFFFF),
+               (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)bytes),
+               (uint32_t)kBufDword3};
+}
+
+// Bytes [at, at + 16) of row ch of an adapter's second matrix b [n][rank], zeros
+// past the rank and past n, to LDS at lds + 16 lane (`to` the same as a
+// pointer).  Rows that start on 16 bytes go there by themselves; others pass
+// through registers, element by element: their own waits then cover every
+// load before them, and nothing is loaded behind the adapters' chunks.
+template <int DT>
+__device__ __forceinline__ void rank_piece(const RowsArgs &a, int adapter, int ch, int at,
+                                           uint32_t lds, char *to) {
+  using raw = typename Elem<DT>::raw;
+  constexpr int S = Elem<DT>::size;
+  const int bytes = a.rank * S;
+  const int64_t from = (int64_t)adapter * a.n * a.rank;
+  if (bytes % 16 == 0) {
+    const u32x4 br = descriptor(reinterpret_cast<const raw *>(a.b) + from, (int64_t)a.n * bytes);
+    ring_load(br, lds, ch < a.n && at < bytes ? (uint32_t)ch * (uint32_t)bytes + at : kOut, 0);
+  } else {
+    const raw *row = reinterpret_cast<const raw *>(a.b) + from + (int64_t)ch * a.rank;
+    raw v[16 / S];
+#pragma unroll
+    for (int e = 0; e < 16 / S; ++e)
+      v[e] = ch < a.n && at + e * S < bytes ? row[at / S + e] : (raw)0;
+    __builtin_memcpy(__builtin_assume_aligned(to + 16 * (threadIdx.x & 63), 16), v, 16);
+  }
+}
+
+// Inclusive prefix sum over the wave.
+__device__ __forceinline__ int wave_prefix(int v) {
+#define SPAROA_DPP_ADD(ctrl, rows) \
+  v += __builtin_amdgcn_update_dpp(0, v, ctrl, rows, 0xF, false)
+  SPAROA_DPP_ADD(0x111, 0xF);
+  SPAROA_DPP_ADD(0x112, 0xF);
+  SPAROA_DPP_ADD(0x114, 0xF);
+  SPAROA_DPP_ADD(0x118, 0xF);
+  SPAROA_DPP_ADD(0x142, 0xA);
+  SPAROA_DPP_ADD(0x143, 0xC);
+#undef SPAROA_DPP_ADD
+  return v;
+}
+
+struct Tile {
+  int seg, col;       // segment; column tile
+  int64_t row0, end;  // rows [row0, min(row0 + BM, end)); end 0: no tile
+};
+
+// The tile of work-group b: XCD b % 8 has the b % 8-th run of the tiles that
+// there are (their number follows from the plan), column tiles innermost.
+template <RowsMode MODE, int BM>
+__device__ __forceinline__ Tile find_tile(const RowsArgs &a, int cols) {
+  const int lane = threadIdx.x & 63, b = blockIdx.x;
+  Tile t{0, 0, 0, 0};
+  int total;
+  if constexpr (MODE <= kRowsDown) {
+    total = 0;
+    for (int e0 = 0; e0 < a.experts; e0 += 64) {
+      const int e = min(e0 + lane, a.experts - 1);
+      const int n = e0 + lane < a.experts ? a.plan[e + 1] - a.plan[e] : 0;
+      total += __builtin_amdgcn_readlane(wave_prefix((n + BM - 1) / BM), 63);
+    }
+  } else {
+    total = (int)((a.rows + BM - 1) / BM);
+  }
+  const int64_t tiles = (int64_t)total * cols, per = (tiles + 7) / 8;
+  const int64_t id = (b & 7) * per + (b >> 3);
+  if ((b >> 3) >= per || id >= tiles) return t;
+  if constexpr (MODE <= kRowsDown) {
+    int rt = (int)(id / cols);
+    t.col = (int)(id - (int64_t)rt * cols);
+    for (int e0 = 0; e0 < a.experts; e0 += 64) {
+      const int e = min(e0 + lane, a.experts - 1);
+      const int at = a.plan[e], end = a.plan[e + 1];
+      const int n = e0 + lane < a.experts ? (end - at + BM - 1) / BM : 0;
+      const int upto = wave_prefix(n);
+      const uint64_t past = __ballot(upto > rt);
+      if (past) {
+        const int l = __builtin_ctzll(past);
+        t.seg = e0 + l;
+        const int first = __builtin_amdgcn_readlane(upto - n, l);
+        t.row0 = __builtin_amdgcn_readlane(at, l) + (int64_t)(rt - first) * BM;
+        t.end = __builtin_amdgcn_readlane(end, l);
+        return t;
+      }
+      rt -= __builtin_amdgcn_readlane(upto, 63);
+    }
+  } else {
+    // column groups outermost: an XCD keeps to a part of the weights
+    const int per_group = (cols + a.col_groups - 1) / a.col_groups;
+    const int group = (int)(id / ((int64_t)total * per_group));
+    const int64_t in = id - (int64_t)group * total * per_group;
+    const int wide = min(per_group, cols - group * per_group);
+    t.row0 = in / wide * BM;
+    t.col = group * per_group + (int)(in % wide);
+    t.end = a.rows;
+  }
+  return t;
+}
+
+}  // namespace sparoa

@@ -1,17 +1,17 @@
-// Products of few rows: the weights are streamed.
+// Row products whose rows start off 16 bytes (k no multiple of a 16-byte
+// vector): any size and alignment.
 //
 // A work-group has a panel of 16 NB output columns of one segment (an
 // expert, or the one matrix of an FC) and 16 MT rows; its waves split K.  A
 // wave's step is 128 bytes of K: lane l loads 32 bytes of weight row l & 15 of
-// each 16-row block and of x row l & 15, straight into the MFMA's operands --
-// each weight byte is read once and used for every row of the tile, so
-// nothing is staged.  PF steps are in flight a wave.  The waves' partial
-// tiles meet in LDS, added in wave order.
-// Loads go through buffer descriptors: rows past the segment, columns past n
-// and pieces past K have offsets past their range and read zero without a
-// memory access.
-// Bound by the weights' stream (16-bit decode: 2 bytes a weight, at most
-// 16 MT products of it).
+// each 16-row block and of x row l & 15, straight into the MFMA's operands.  A
+// 16-byte piece of 16-bit elements may start between two words: five words
+// are loaded and shifted into place.  The waves' partial tiles meet in LDS,
+// added in wave order.  The adapters' share of an output is a thread's sum over
+// the rank in fp32.
+// Loads go through buffer descriptors: rows past the segment and columns past
+// n have offsets past their range and read zero without a memory access;
+// elements past K are masked.
 #include <algorithm>
 
 #include "rows.h"
@@ -20,7 +20,6 @@ namespace sparoa {
 namespace {
 
 constexpr int kNW = 8, kNT = 64 * kNW;   // waves, threads
-constexpr uint32_t kOut = 0x80000000u;   // past every descriptor's range
 
 // A word every lane wants alike, by the scalar unit: memory that no kernel of
 // this launch writes.
@@ -29,35 +28,50 @@ __device__ __forceinline__ int uniform_word(const int32_t *p) {
       reinterpret_cast<uintptr_t>(p));
 }
 
-// One operand matrix.  VEC: 16-byte pieces by buffer loads; else element by
-// element (rows that start anywhere).
-template <int DT, bool VEC>
+// One operand matrix: 16-byte pieces of rows at any element.
+template <int DT>
 struct Operand {
-  using raw = typename Elem<DT>::raw;
-  const void *base;
-  int bytes;
-  __device__ Operand(const void *p, int64_t n) : base(p), bytes((int)n) {}
-  // 16 bytes of K from byte kb + at of the row at byte offset `row` (kOut:
-  // none); kb alike in every lane, at < 128.  VEC: the whole 16 bytes lie
-  // before kbytes, or kb does not and they read zero.
-  __device__ __forceinline__ u32x4 piece(uint32_t row, int kb, int at, int kbytes) const {
-    if constexpr (VEC) {
-      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(
-          const_cast<void *>(base), (short)0, kb < kbytes ? bytes : 0, kBufDword3);
-      return __builtin_bit_cast(u32x4,
-                                __builtin_amdgcn_raw_buffer_load_b128(rsrc, row + at, kb, 0));
-    } else {
-      constexpr int S = Elem<DT>::size;
-      raw v[16 / S];
+  static constexpr int S = Elem<DT>::size;
+  __amdgpu_buffer_rsrc_t rsrc;
+  uint32_t lead;   // bytes from the descriptor's word-aligned base to the matrix
+  struct Piece {
+    u32x4 q;
+    uint32_t tail;   // (16-bit) the word behind q
+  };
+  __device__ Operand(const void *p, int64_t n) {
+    const uint64_t at = reinterpret_cast<uint64_t>(p);
+    lead = S == 2 ? (uint32_t)at & 2u : 0u;
+    // (to the end of the last element's word: a word past the range reads zero)
+    rsrc = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>(at - lead), (short)0,
+                                             (int)((n + lead + 3) & ~3ll), kBufDword3);
+  }
+  // The words that hold bytes [kb, kb + 16) of the row at byte offset `row`
+  // (kOut: none).
+  __device__ __forceinline__ Piece request(uint32_t row, int kb, int kbytes) const {
+    const uint32_t at = kb < kbytes ? (row + lead + kb) & ~3u : kOut;
+    Piece p;
+    p.q = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at, 0, 0));
+    p.tail = S == 2 ? __builtin_amdgcn_raw_buffer_load_b32(rsrc, at + 16, 0, 0) : 0u;
+    return p;
+  }
+  // The piece itself, zeros past K.
+  __device__ __forceinline__ u32x4 value(const Piece &p, uint32_t row, int kb, int kbytes) const {
+    u32x4 v = p.q;
+    if constexpr (S == 2) {
+      const uint32_t by = (row + lead + kb) & 2u;
 #pragma unroll
-      for (int e = 0; e < 16 / S; ++e)
-        v[e] = !(row & kOut) && kb + at + e * S < kbytes
-                   ? reinterpret_cast<const raw *>(base)[(row + kb + at) / S + e]
-                   : (raw)0;
-      u32x4 r;
-      __builtin_memcpy(&r, v, 16);
-      return r;
+      for (int i = 0; i < 4; ++i)
+        v[i] = __builtin_amdgcn_alignbyte(i < 3 ? p.q[i + 1] : p.tail, p.q[i], by);
     }
+    const int left = (kbytes - kb) / S;   // elements of the piece before K's end
+    if (left < 16 / S) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (S == 4) v[i] = i < left ? v[i] : 0u;
+        else v[i] &= 2 * i + 1 < left ? ~0u : 2 * i < left ? 0xFFFFu : 0u;
+      }
+    }
+    return v;
   }
 };
 
@@ -90,42 +104,13 @@ __device__ __forceinline__ float adapter_share(const RowsArgs &a, int64_t row, i
   return d;
 }
 
-// h[row][r] = scale_a a_a[r] x[row]: a wave per row and r (few rows, where
-// their adapters differ).
-template <int DT, bool VEC>
-__global__ __launch_bounds__(256) void shrink_rows_kernel(RowsArgs a) {
-  using E = Elem<DT>;
-  using raw = typename E::raw;
-  const int64_t row = blockIdx.y;
-  const int r = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int id = a.ids[row];
-  if (r >= a.n || (uint32_t)id >= (uint32_t)a.adapters) return;   // (whole waves)
-  const raw *x = reinterpret_cast<const raw *>(a.x) + row * a.ldx;
-  const raw *w = reinterpret_cast<const raw *>(a.w) + id * a.w_stride + (int64_t)r * a.k;
-  constexpr int V = VEC ? 16 / E::size : 1;
-  float s = 0.f;
-#pragma unroll 4
-  for (int k = lane * V; k < a.k; k += 64 * V) {
-    float xv[V], wv[V];
-    load_elems<DT, V>(x, k, xv);
-    load_elems<DT, V>(w, k, wv);
-#pragma unroll
-    for (int e = 0; e < V; ++e) s = fmaf(xv[e], wv[e], s);
-  }
-#pragma unroll
-  for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-  if (lane == 0) reinterpret_cast<float *>(a.y)[row * a.ldy + r] = s * a.scale[id];
-}
-
-// (VEC, up to 32 rows: two work-groups a CU, one's start and end under the
-// other's stream)
-template <int DT, bool VEC, RowsMode MODE, int MT, int NB>
-__global__ __launch_bounds__(kNT, VEC && MODE != kRowsFc && MT <= 2 && NB <= 2 ? 4 : 2) void rows_stream_kernel(RowsArgs a) {
+template <int DT, RowsMode MODE, int MT, int NB>
+__global__ __launch_bounds__(kNT, 2) void rows_stream_kernel(RowsArgs a) {
   using E = Elem<DT>;
   constexpr bool GATED = MODE == kRowsUpGated, EXPERTS = MODE <= kRowsDown;
   constexpr int WB = GATED ? 2 * NB : NB;      // weight blocks of 16 rows
   constexpr bool FC = MODE == kRowsFc;
-  constexpr int PF = VEC ? std::max(2, (FC ? 12 : 8) / (WB + MT)) : 1;   // steps in flight
+  constexpr int PF = 2;   // steps in flight
   __shared__ f32x4 part[kNW][WB * MT][64];
   __shared__ float tail[FC ? 16 * MT : 1][FC ? 16 * NB + 1 : 1];   // the adapters' share
   __shared__ int32_t list[MODE == kRowsShrink ? 16 * MT : 1];
@@ -135,8 +120,7 @@ __global__ __launch_bounds__(kNT, VEC && MODE != kRowsFc && MT <= 2 && NB <= 2 ?
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n0 = blockIdx.x * 16 * NB;
   const int kbytes = a.k * E::size;
-  // whole steps; VEC: what is left of K is a step of its own, behind them
-  const int steps = VEC ? kbytes / 128 : (kbytes + 127) / 128;
+  const int steps = (kbytes + 127) / 128;
 
   uint32_t woff[WB];
 #pragma unroll
@@ -173,10 +157,10 @@ __global__ __launch_bounds__(kNT, VEC && MODE != kRowsFc && MT <= 2 && NB <= 2 ?
     for (int item = 0; item < items; ++item)
       for (int64_t r0 = s0; r0 < s1; r0 += 16 * MT) {
         if constexpr (MODE == kRowsShrink) seg = list[item];
-        const Operand<DT, VEC> w(reinterpret_cast<const char *>(a.w) + (int64_t)seg * a.w_stride * E::size,
+        const Operand<DT> w(reinterpret_cast<const char *>(a.w) + (int64_t)seg * a.w_stride * E::size,
                                  (int64_t)a.w_rows * kbytes);
         const bool gather = EXPERTS && a.order;
-        const Operand<DT, VEC> x(
+        const Operand<DT> x(
             gather ? a.x : reinterpret_cast<const char *>(a.x) + r0 * a.ldx * E::size,
             gather ? a.x_bytes : std::min<int64_t>(s1 - r0, 16 * MT) * a.ldx * E::size);
         int slot[MT];   // (sent for first: loads land in order)
@@ -191,33 +175,40 @@ __global__ __launch_bounds__(kNT, VEC && MODE != kRowsFc && MT <= 2 && NB <= 2 ?
         for (int b = 0; b < WB; ++b)
 #pragma unroll
           for (int t = 0; t < MT; ++t) acc[b][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-        u32x4 wq[PF][WB][2], xq[PF][MT][2];
+        typename Operand<DT>::Piece wq[PF][WB][2], xq[PF][MT][2];
         uint32_t xoff[MT];
-        auto load_w = [&](int i, int kb, int end) __attribute__((always_inline)) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int b = 0; b < WB; ++b) wq[i][b][h] = w.piece(woff[b], kb, q * 32 + 16 * h, end);
-        };
-        auto load_x = [&](int i, int kb, int end) __attribute__((always_inline)) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int t = 0; t < MT; ++t) xq[i][t][h] = x.piece(xoff[t], kb, q * 32 + 16 * h, end);
-        };
-        auto multiply = [&](int i) __attribute__((always_inline)) {
+        auto load_w = [&](int i, int kb) __attribute__((always_inline)) {
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int b = 0; b < WB; ++b)
-#pragma unroll
-              for (int t = 0; t < MT; ++t)
-                acc[b][t] = mma16<DT>(wq[i][b][h], xq[i][t][h], acc[b][t]);
+              wq[i][b][h] = w.request(woff[b], kb + q * 32 + 16 * h, kbytes);
         };
-        const int kend = VEC ? steps * 128 : kbytes;
+        auto load_x = [&](int i, int kb) __attribute__((always_inline)) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+              xq[i][t][h] = x.request(xoff[t], kb + q * 32 + 16 * h, kbytes);
+        };
+        auto multiply = [&](int i, int kb) __attribute__((always_inline)) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            u32x4 wv[WB];
+#pragma unroll
+            for (int b = 0; b < WB; ++b)
+              wv[b] = w.value(wq[i][b][h], woff[b], kb + q * 32 + 16 * h, kbytes);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+              const u32x4 xv = x.value(xq[i][t][h], xoff[t], kb + q * 32 + 16 * h, kbytes);
+#pragma unroll
+              for (int b = 0; b < WB; ++b) acc[b][t] = mma16<DT>(wv[b], xv, acc[b][t]);
+            }
+          }
+        };
         // (the weights are sent for before the rows' places are known)
 #pragma unroll
-        for (int i = 0; i < PF; ++i) load_w(i, (wave + i * kNW) * 128, kend);
+        for (int i = 0; i < PF; ++i) load_w(i, (wave + i * kNW) * 128);
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
           uint32_t row = 16 * t + rl;
@@ -226,28 +217,14 @@ __global__ __launch_bounds__(kNT, VEC && MODE != kRowsFc && MT <= 2 && NB <= 2 ?
           xoff[t] = in ? row * (uint32_t)(a.ldx * E::size) : kOut;
         }
 #pragma unroll
-        for (int i = 0; i < PF; ++i) load_x(i, (wave + i * kNW) * 128, kend);
+        for (int i = 0; i < PF; ++i) load_x(i, (wave + i * kNW) * 128);
         for (int s = wave; s < steps; s += PF * kNW) {
 #pragma unroll
           for (int i = 0; i < PF; ++i) {
-            multiply(i);
-            load_w(i, (s + (i + PF) * kNW) * 128, kend);
-            load_x(i, (s + (i + PF) * kNW) * 128, kend);
+            multiply(i, (s + i * kNW) * 128);
+            load_w(i, (s + (i + PF) * kNW) * 128);
+            load_x(i, (s + (i + PF) * kNW) * 128);
           }
-        }
-        if (VEC && kend < kbytes && wave == steps % kNW) {   // pieces past K read zero
-          const uint32_t past0 = kend + q * 32 < kbytes ? 0u : kOut;
-          const uint32_t past1 = kend + q * 32 + 16 < kbytes ? 0u : kOut;
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-#pragma unroll
-            for (int b = 0; b < WB; ++b)
-              wq[0][b][h] = w.piece(woff[b] | (h ? past1 : past0), kend, q * 32 + 16 * h, kbytes);
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-              xq[0][t][h] = x.piece(xoff[t] | (h ? past1 : past0), kend, q * 32 + 16 * h, kbytes);
-          }
-          multiply(0);
         }
         __syncthreads();   // the last tile's partial sums have been read
         // the adapters' share of an output is one thread's sum over the rank
@@ -326,153 +303,46 @@ __global__ __launch_bounds__(kNT, VEC && MODE != kRowsFc && MT <= 2 && NB <= 2 ?
   }
 }
 
-template <int DT, bool VEC, RowsMode MODE, int MT, int NB>
+template <int DT, RowsMode MODE, int MT, int NB>
 void launch_one(const RowsArgs &a, hipStream_t stream) {
   const int64_t groups = MODE <= kRowsDown ? std::min<int64_t>(a.experts, a.rows)
                                            : cdiv(a.rows, 16 * MT);
-  const dim3 grid((unsigned)cdiv(a.n, 16 * NB), (unsigned)std::min<int64_t>(groups, 32768));
-  rows_stream_kernel<DT, VEC, MODE, MT, NB><<<grid, kNT, 0, stream>>>(a);
+  const dim3 grid((unsigned)cdiv(MODE == kRowsShrink ? a.ldy : a.n, 16 * NB),
+                  (unsigned)std::min<int64_t>(groups, 32768));
+  rows_stream_kernel<DT, MODE, MT, NB><<<grid, kNT, 0, stream>>>(a);
 }
 
-// Rows a tile: as few 16-row blocks as hold an average segment.
-template <int DT, bool VEC, RowsMode MODE>
+// Rows a tile: one block of 16 where that holds an average segment.
+template <int DT, RowsMode MODE>
 void launch_mode(const RowsArgs &a, hipStream_t stream) {
+  constexpr int NB = MODE == kRowsUpGated ? 1 : 2;
   const int64_t per = MODE <= kRowsDown ? cdiv(a.rows, std::min<int64_t>(a.experts, a.rows))
                                         : a.rows;
-  if constexpr (MODE == kRowsShrink) {
-    // a wave per row and rank where all that these read is little (they share
-    // nothing but the L2), else tiles of 16 rows that read x once
-    if (a.h_f32 && a.rows <= 32768 &&
-        a.rows * a.n * a.k * Elem<DT>::size <= (int64_t)32 << 20) {
-      const dim3 grid((unsigned)cdiv(a.n, 4), (unsigned)a.rows);
-      shrink_rows_kernel<DT, VEC><<<grid, 256, 0, stream>>>(a);
-    } else if (a.n <= 16 || !VEC) {
-      launch_one<DT, VEC, MODE, 1, 1>(a, stream);
-    } else if (a.n <= 32) {
-      launch_one<DT, VEC, MODE, 1, 2>(a, stream);
-    } else {
-      launch_one<DT, VEC, MODE, 1, 4>(a, stream);
-    }
-  } else if constexpr (!VEC) {
-    launch_one<DT, VEC, MODE, 4, 1>(a, stream);
-  } else {
-    constexpr int NB = MODE == kRowsUpGated ? 1 : 2;
-    if (MODE == kRowsFc && cdiv(a.n, 32) * cdiv(a.rows, per <= 16 ? 16 : per <= 32 ? 32 : 64) < 160) {
-      // panels of 16 columns where those of 32 leave too many CUs without one
-      if (per <= 16) launch_one<DT, VEC, MODE, 1, 1>(a, stream);
-      else if (per <= 32) launch_one<DT, VEC, MODE, 2, 1>(a, stream);
-      else launch_one<DT, VEC, MODE, 4, 1>(a, stream);
-      return;
-    }
-    if (per <= 16) launch_one<DT, VEC, MODE, 1, NB>(a, stream);
-    else if (per <= 32) launch_one<DT, VEC, MODE, 2, NB>(a, stream);
-    else launch_one<DT, VEC, MODE, 4, NB>(a, stream);
-  }
+  if (MODE == kRowsShrink || per <= 16) launch_one<DT, MODE, 1, NB>(a, stream);
+  else if constexpr (MODE != kRowsShrink) launch_one<DT, MODE, 4, NB>(a, stream);
 }
 
 template <int DT>
-void launch_dt(RowsMode mode, const RowsArgs &a, bool vec, hipStream_t stream) {
-#define SPAROA_ROWS(M)                                     \
-  case M:                                                  \
-    if (vec) launch_mode<DT, true, M>(a, stream);          \
-    else launch_mode<DT, false, M>(a, stream);             \
-    break
+void launch_dt(RowsMode mode, const RowsArgs &a, hipStream_t stream) {
   switch (mode) {
-    SPAROA_ROWS(kRowsUp);
-    SPAROA_ROWS(kRowsUpGated);
-    SPAROA_ROWS(kRowsDown);
-    SPAROA_ROWS(kRowsFc);
-    SPAROA_ROWS(kRowsShrink);
+    case kRowsUp: return launch_mode<DT, kRowsUp>(a, stream);
+    case kRowsUpGated: return launch_mode<DT, kRowsUpGated>(a, stream);
+    case kRowsDown: return launch_mode<DT, kRowsDown>(a, stream);
+    case kRowsFc: return launch_mode<DT, kRowsFc>(a, stream);
+    case kRowsShrink: return launch_mode<DT, kRowsShrink>(a, stream);
   }
-#undef SPAROA_ROWS
-}
-
-template <int DT, int V>
-__global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
-  const int64_t per = a.hidden / V, total = a.tokens * per;
-  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
-    const int64_t t = i / per, c = i % per * V;
-    float s[V];
-#pragma unroll
-    for (int e = 0; e < V; ++e) s[e] = 0.f;
-    for (int j0 = 0; j0 < a.top_k; j0 += 8) {   // eight rows in flight
-      int p[8];
-      float w[8], z[8][V];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int64_t slot = t * a.top_k + (j0 + j < a.top_k ? j0 + j : 0);
-        p[j] = j0 + j < a.top_k ? a.place[slot] : -1;
-        w[j] = a.weights[slot];
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float *from = a.z + (p[j] < 0 ? 0 : p[j]) * a.ldz + c;
-        if constexpr (V % 4 == 0) {
-#pragma unroll
-          for (int e = 0; e < V; e += 4) {
-            const f32x4 q = *reinterpret_cast<const f32x4 *>(from + e);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) z[j][e + i] = q[i];
-          }
-        } else {
-          z[j][0] = from[0];
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j)   // no expert: neither weight nor row is looked at
-#pragma unroll
-        for (int e = 0; e < V; ++e) s[e] = p[j] < 0 ? s[e] : fmaf(w[j], z[j][e], s[e]);
-    }
-    if (a.residual) {
-      float r[V];
-      load_elems<DT, V>(a.residual, t * a.hidden + c, r);
-#pragma unroll
-      for (int e = 0; e < V; ++e) s[e] += r[e];
-    }
-    store_elems<DT, V>(a.y, t * a.hidden + c, s);
-  }
-}
-
-template <int DT>
-void launch_combine_dt(const CombineArgs &a, hipStream_t stream) {
-  constexpr int V = 16 / Elem<DT>::size;
-  const bool vec = a.hidden % V == 0;
-  const int64_t items = a.tokens * (vec ? a.hidden / V : a.hidden);
-  const unsigned grid = (unsigned)std::min<int64_t>(cdiv(items, 256), 1 << 20);
-  if (vec) combine_kernel<DT, V><<<grid, 256, 0, stream>>>(a);
-  else combine_kernel<DT, 1><<<grid, 256, 0, stream>>>(a);
 }
 
 }  // namespace
 
-bool rows_tiled(RowsMode mode, const RowsArgs &a, sparoa_dtype dt) {
-  const int v = 16 / (int)elem_size(dt);
-  if (mode == kRowsShrink || a.k % v || a.ldx % v) return false;
-  if (mode == kRowsFc)
-    return a.rank % v == 0 && a.rows > 256 && cdiv(a.rows, 128) * cdiv(a.n, 256) >= 128;
-  return a.rows / std::min<int64_t>(a.experts, a.rows) > 64;
-}
-
-sparoa_status launch_rows(RowsMode mode, const RowsArgs &a, sparoa_dtype dt, hipStream_t stream) {
-  if (rows_tiled(mode, a, dt)) return launch_rows_tile(mode, a, dt, stream);
-  const int v = 16 / (int)elem_size(dt);
-  const bool vec = a.k % v == 0 && a.ldx % v == 0;   // rows of x and w start on 16 bytes
+sparoa_status launch_rows_stream(RowsMode mode, const RowsArgs &a, sparoa_dtype dt,
+                                 hipStream_t stream) {
   switch (dt) {
-    case SPAROA_F32: launch_dt<SPAROA_F32>(mode, a, vec, stream); break;
-    case SPAROA_F16: launch_dt<SPAROA_F16>(mode, a, vec, stream); break;
-    default: launch_dt<SPAROA_BF16>(mode, a, vec, stream); break;
+    case SPAROA_F32: launch_dt<SPAROA_F32>(mode, a, stream); break;
+    case SPAROA_F16: launch_dt<SPAROA_F16>(mode, a, stream); break;
+    default: launch_dt<SPAROA_BF16>(mode, a, stream); break;
   }
   SPAROA_LAUNCH_CHECK("row products");
-  return SPAROA_OK;
-}
-
-sparoa_status launch_combine(const CombineArgs &a, sparoa_dtype dt, hipStream_t stream) {
-  switch (dt) {
-    case SPAROA_F32: launch_combine_dt<SPAROA_F32>(a, stream); break;
-    case SPAROA_F16: launch_combine_dt<SPAROA_F16>(a, stream); break;
-    default: launch_combine_dt<SPAROA_BF16>(a, stream); break;
-  }
-  SPAROA_LAUNCH_CHECK("expert_ffn: combine");
   return SPAROA_OK;
 }
 

@@ -15,127 +15,10 @@
 // tiles, column tiles innermost, so the tiles of one expert share an L2.
 #include <algorithm>
 
-#include "rows.h"
+#include "rows_ring.h"
 
 namespace sparoa {
 namespace {
-
-constexpr uint32_t kOut = 0x80000000u;   // past every descriptor's range
-constexpr int kRow = 128;                // bytes of a chunk row
-
-// s_waitcnt immediates: at most n vector-memory operations outstanding; LDS
-// operations done.
-constexpr int vm_outstanding(int n) { return (n & 15) | (7 << 4) | (15 << 8) | ((n >> 4) << 14); }
-constexpr int kLdsDone = 15 | (7 << 4) | (3 << 14);
-
-// Waits until all but this wave's newest `chunks` <= C chunks' loads (L per
-// chunk) have landed.
-template <int C, int L>
-__device__ __forceinline__ void wait_ring(int chunks) {
-  static_assert(C * L < 64, "vmcnt range");
-  if constexpr (C > 0) {
-    if (chunks < C) return wait_ring<C - 1, L>(chunks);
-  }
-  __builtin_amdgcn_s_waitcnt(vm_outstanding(C * L));
-}
-
-// A 16-byte-per-lane buffer load whose data goes to LDS (lane l's to lds + 16
-// l, lds uniform), zeros where the offset is past the range.  In assembly: by
-// the builtin the compiler cannot tell the ring's stages apart and waits for
-// every load in flight before each LDS read; the waits are at the barriers
-// instead (wait_ring).  It writes no register.
-__device__ __forceinline__ void ring_load(u32x4 rsrc, uint32_t lds, uint32_t voffset,
-                                          uint32_t soffset) {
-  asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-               :
-               : "{m0}"(lds), "v"(voffset), "s"(rsrc), "s"(soffset)
-               : "memory");
-}
-__device__ __forceinline__ u32x4 descriptor(const void *p, int64_t bytes) {
-  const uint64_t b = reinterpret_cast<uint64_t>(p);
-  return u32x4{(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b),
-               (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32) & 0xFFFF),
-               (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)bytes),
-               (uint32_t)kBufDword3};
-}
-
-// Inclusive prefix sum over the wave.
-__device__ __forceinline__ int wave_prefix(int v) {
-#define SPAROA_DPP_ADD(ctrl, rows) \
-  v += __builtin_amdgcn_update_dpp(0, v, ctrl, rows, 0xF, false)
-  SPAROA_DPP_ADD(0x111, 0xF);
-  SPAROA_DPP_ADD(0x112, 0xF);
-  SPAROA_DPP_ADD(0x114, 0xF);
-  SPAROA_DPP_ADD(0x118, 0xF);
-  SPAROA_DPP_ADD(0x142, 0xA);
-  SPAROA_DPP_ADD(0x143, 0xC);
-#undef SPAROA_DPP_ADD
-  return v;
-}
-
-int choose_tile(RowsMode mode, const RowsArgs &a) {
-#ifdef ROWS_SWEEP
-  if (const char *e = getenv("ROWS_TILE")) return atoi(e);
-#endif
-  return 0;
-}
-
-struct Tile {
-  int seg, col;       // segment; column tile
-  int64_t row0, end;  // rows [row0, min(row0 + BM, end)); end 0: no tile
-};
-
-// The tile of work-group b: XCD b % 8 has the b % 8-th run of the tiles that
-// there are (their number follows from the plan), column tiles innermost.
-template <RowsMode MODE, int BM>
-__device__ __forceinline__ Tile find_tile(const RowsArgs &a, int cols) {
-  const int lane = threadIdx.x & 63, b = blockIdx.x;
-  Tile t{0, 0, 0, 0};
-  int total;
-  if constexpr (MODE <= kRowsDown) {
-    total = 0;
-    for (int e0 = 0; e0 < a.experts; e0 += 64) {
-      const int e = min(e0 + lane, a.experts - 1);
-      const int n = e0 + lane < a.experts ? a.plan[e + 1] - a.plan[e] : 0;
-      total += __builtin_amdgcn_readlane(wave_prefix((n + BM - 1) / BM), 63);
-    }
-  } else {
-    total = (int)((a.rows + BM - 1) / BM);
-  }
-  const int64_t tiles = (int64_t)total * cols, per = (tiles + 7) / 8;
-  const int64_t id = (b & 7) * per + (b >> 3);
-  if ((b >> 3) >= per || id >= tiles) return t;
-  if constexpr (MODE <= kRowsDown) {
-    int rt = (int)(id / cols);
-    t.col = (int)(id - (int64_t)rt * cols);
-    for (int e0 = 0; e0 < a.experts; e0 += 64) {
-      const int e = min(e0 + lane, a.experts - 1);
-      const int at = a.plan[e], end = a.plan[e + 1];
-      const int n = e0 + lane < a.experts ? (end - at + BM - 1) / BM : 0;
-      const int upto = wave_prefix(n);
-      const uint64_t past = __ballot(upto > rt);
-      if (past) {
-        const int l = __builtin_ctzll(past);
-        t.seg = e0 + l;
-        const int first = __builtin_amdgcn_readlane(upto - n, l);
-        t.row0 = __builtin_amdgcn_readlane(at, l) + (int64_t)(rt - first) * BM;
-        t.end = __builtin_amdgcn_readlane(end, l);
-        return t;
-      }
-      rt -= __builtin_amdgcn_readlane(upto, 63);
-    }
-  } else {
-    // column groups outermost: an XCD keeps to a part of the weights
-    const int per_group = (cols + a.col_groups - 1) / a.col_groups;
-    const int group = (int)(id / ((int64_t)total * per_group));
-    const int64_t in = id - (int64_t)group * total * per_group;
-    const int wide = min(per_group, cols - group * per_group);
-    t.row0 = in / wide * BM;
-    t.col = group * per_group + (int)(in % wide);
-    t.end = a.rows;
-  }
-  return t;
-}
 
 template <int DT, RowsMode MODE, int WGM, int WGN, int WTM, int WTN, int S>
 __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a) {
@@ -240,25 +123,21 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
     if constexpr (FC) {
       const int c = i - n, d = c / rank_chunks, r = (c - d * rank_chunks) * kRow;
       const int id = __builtin_amdgcn_readfirstlane(list[d]);
-      const int hbytes = a.ldh * E::size, bbytes = a.rank * E::size;
+      const int hbytes = a.ldh * E::size;   // (columns past the rank hold zeros)
       const u32x4 hr = descriptor(reinterpret_cast<const char *>(a.h) + row0 * hbytes,
                                   (int64_t)rows * hbytes);
-      const u32x4 br = descriptor(reinterpret_cast<const char *>(a.b) +
-                                      (int64_t)id * a.n * bbytes, (int64_t)a.n * bbytes);
 #pragma unroll
       for (int u = 0; u < AV; ++u) {
         const int row = 8 * (u * NW + wave) + lrow;
-        const bool in = a_id[u] == id && r + cgA * 16 < bbytes;
+        const bool in = a_id[u] == id && r + cgA * 16 < hbytes;
         ring_load(hr, dst + u * (NW * 1024),
                   in ? (uint32_t)(row * hbytes + r + cgA * 16) : kOut, 0);
       }
 #pragma unroll
-      for (int u = 0; u < BV; ++u) {
-        const int ch = n0 + 8 * (u * NW + wave) + lrow;
-        const bool in = ch < a.n && r + cgB * 16 < bbytes;
-        ring_load(br, dst + BM * kRow + u * (NW * 1024),
-                  in ? (uint32_t)ch * (uint32_t)bbytes + r + cgB * 16 : kOut, 0);
-      }
+      for (int u = 0; u < BV; ++u)
+        rank_piece<DT>(a, id, n0 + 8 * (u * NW + wave) + lrow, r + cgB * 16,
+                       dst + BM * kRow + u * (NW * 1024),
+                       smem + (dst - ring) + wave * 1024 + BM * kRow + u * (NW * 1024));
     }
   };
 
@@ -327,6 +206,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
   for (int s = 0; s < S; ++s)
     if (s < chunks) load_any(s, ring + s * STAGE);
   wait_ring<S - 1, L>(min(S - 1, chunks - 1));
+  __builtin_amdgcn_s_waitcnt(kLdsDone);   // (pieces that passed through registers)
   asm volatile("s_barrier" ::: "memory");
   auto run = [&](auto busy) __attribute__((always_inline)) {
     Operands p, q;
@@ -439,34 +319,34 @@ void launch_one(RowsArgs a, hipStream_t stream) {
 }
 
 template <int DT, RowsMode MODE>
-void launch_mode(const RowsArgs &a, hipStream_t stream) {
-  switch (choose_tile(MODE, a)) {
-    case 0: return launch_one<DT, MODE, 2, 4, 4, 4, 3>(a, stream);    // 128 x 256
-    case 1: return launch_one<DT, MODE, 2, 2, 4, 4, 2>(a, stream);    // 128 x 128
-    case 2: return launch_one<DT, MODE, 4, 1, 2, 4, 3>(a, stream);    // 128 x 64
-    case 3: return launch_one<DT, MODE, 2, 2, 2, 4, 3>(a, stream);    // 64 x 128
-    default: return launch_one<DT, MODE, 4, 1, 1, 4, 4>(a, stream);   // 64 x 64
+void launch_mode(RowsTile tile, const RowsArgs &a, hipStream_t stream) {
+  if (tile == kTile128x256) {
+    if constexpr (DT != SPAROA_F32) launch_one<DT, MODE, 2, 4, 4, 4, 3>(a, stream);   // 144 KB
+  } else if (tile == kTile64x128) {
+    launch_one<DT, MODE, 2, 2, 2, 4, 3>(a, stream);                                   // 72 KB
+  } else {
+    launch_one<DT, MODE, 4, 1, 1, 4, 4>(a, stream);                                   // 64 KB
   }
 }
 
 template <int DT>
-void launch_dt(RowsMode mode, const RowsArgs &a, hipStream_t stream) {
+void launch_dt(RowsMode mode, RowsTile tile, const RowsArgs &a, hipStream_t stream) {
   switch (mode) {
-    case kRowsUp: return launch_mode<DT, kRowsUp>(a, stream);
-    case kRowsUpGated: return launch_mode<DT, kRowsUpGated>(a, stream);
-    case kRowsDown: return launch_mode<DT, kRowsDown>(a, stream);
-    default: return launch_mode<DT, kRowsFc>(a, stream);
+    case kRowsUp: return launch_mode<DT, kRowsUp>(tile, a, stream);
+    case kRowsUpGated: return launch_mode<DT, kRowsUpGated>(tile, a, stream);
+    case kRowsDown: return launch_mode<DT, kRowsDown>(tile, a, stream);
+    default: return launch_mode<DT, kRowsFc>(tile, a, stream);
   }
 }
 
 }  // namespace
 
-sparoa_status launch_rows_tile(RowsMode mode, const RowsArgs &a, sparoa_dtype dt,
+sparoa_status launch_rows_tile(RowsMode mode, RowsTile tile, const RowsArgs &a, sparoa_dtype dt,
                                hipStream_t stream) {
   switch (dt) {
-    case SPAROA_F32: launch_dt<SPAROA_F32>(mode, a, stream); break;
-    case SPAROA_F16: launch_dt<SPAROA_F16>(mode, a, stream); break;
-    default: launch_dt<SPAROA_BF16>(mode, a, stream); break;
+    case SPAROA_F32: launch_dt<SPAROA_F32>(mode, tile, a, stream); break;
+    case SPAROA_F16: launch_dt<SPAROA_F16>(mode, tile, a, stream); break;
+    default: launch_dt<SPAROA_BF16>(mode, tile, a, stream); break;
   }
   SPAROA_LAUNCH_CHECK("row product tiles");
   return SPAROA_OK;

@@ -121,7 +121,8 @@ def run(t, e, k, hidden, inner, dt, gated, act, kind="even", bias=False, residua
 SHAPES = [(1, 8, 2, 64, 64), (1, 1, 1, 8, 8), (3, 5, 2, 72, 40), (16, 4, 1, 128, 96),
           (17, 3, 3, 200, 33), (33, 2, 2, 33, 200), (50, 64, 8, 136, 8), (65, 2, 1, 1, 1),
           (70, 6, 2, 768, 264), (130, 3, 2, 260, 136), (300, 2, 2, 192, 320), (517, 4, 2, 320, 256),
-          (700, 3, 1, 64, 1000), (257, 5, 3, 1000, 72)]
+          (700, 3, 1, 64, 1000), (257, 5, 3, 1000, 72),
+          (2100, 16, 1, 64, 1100), (2100, 16, 1, 1096, 72)]
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f16", "f32"])

@@ -88,7 +88,8 @@ def run(m, k, n, adapters, rank, dt, kind="runs", act=0, bias=False, residual=Fa
 SHAPES = [(1, 64, 64, 1, 8), (1, 8, 1, 3, 1), (5, 200, 130, 4, 16), (16, 1000, 72, 16, 4),
           (33, 33, 47, 5, 3), (64, 256, 512, 40, 32), (65, 520, 264, 3, 64), (130, 96, 1000, 2, 24),
           (333, 768, 100, 9, 8), (300, 1001, 64, 2, 100), (700, 256, 384, 12, 136),
-          (1030, 128, 520, 70, 16), (2050, 320, 1024, 5, 40)]
+          (1030, 128, 520, 70, 16), (2050, 320, 1024, 5, 40), (2050, 200, 2104, 70, 12),
+          (6200, 64, 2056, 9, 20)]
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f16", "f32"])
