@@ -16,6 +16,7 @@ struct NormArgs {
 sparoa_status launch_block_norm(const NormArgs &a, sparoa_dtype dt, hipStream_t stream);
 
 // Routing and plan (expert_route.hip).  top_k <= 32, experts <= 512, groups <= 64.
+constexpr int kMaxExperts = 512;
 constexpr int kPlanBlocks = 256;       // blocks of tokens that leave their counts
 constexpr int kPlaceGroups = 64;       // work-groups that place slots by them
 constexpr int kOneGroupSlots = 4096;   // given choices that one work-group plans

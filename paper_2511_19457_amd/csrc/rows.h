@@ -66,18 +66,33 @@ __device__ __forceinline__ void store_elems(void *p, int64_t at, const float (&v
                    V * E::size);
 }
 
-// The distinct values in [0, limit) of ids[0 .. n), in order of appearance, to
-// LDS list; the whole wave, 64 BATCHES >= n.  Returns their number.
+// A word every lane wants alike, by the scalar unit: memory that no kernel of
+// this launch writes.
+__device__ __forceinline__ int uniform_word(const int32_t *p) {
+  return *reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(
+      reinterpret_cast<uintptr_t>(p));
+}
+
+// Eight elements as one 16-byte vector (16-bit types).
+template <int DT>
+__device__ __forceinline__ u32x4 pack8(const float (&v)[8]) {
+  u32x4 w = {};
+  if constexpr (DT != SPAROA_F32) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = Elem<DT>::pack2(v[2 * e], v[2 * e + 1]);
+  }
+  return w;
+}
+
+// The distinct values in [0, limit) among id[b] of every lane, in order, to LDS
+// list; the whole wave.  Returns their number.
 template <int BATCHES>
-__device__ __forceinline__ int distinct_ids(const int32_t *ids, int n, int limit, int32_t *list) {
+__device__ __forceinline__ int distinct_values(const int (&id)[BATCHES], int limit,
+                                               int32_t *list) {
   const int lane = threadIdx.x & 63;
-  int id[BATCHES];
   uint64_t left[BATCHES];
 #pragma unroll
-  for (int b = 0; b < BATCHES; ++b) {
-    id[b] = 64 * b + lane < n ? ids[64 * b + lane] : -1;
-    left[b] = __ballot((uint32_t)id[b] < (uint32_t)limit);
-  }
+  for (int b = 0; b < BATCHES; ++b) left[b] = __ballot((uint32_t)id[b] < (uint32_t)limit);
   int found = 0;
 #pragma unroll
   for (int b = 0; b < BATCHES; ++b)
@@ -89,6 +104,18 @@ __device__ __forceinline__ int distinct_ids(const int32_t *ids, int n, int limit
       for (int c = b; c < BATCHES; ++c) left[c] &= ~__ballot(id[c] == a);
     }
   return found;
+}
+
+// The same of ids[0 .. n), n <= 64 BATCHES.
+template <int BATCHES>
+__device__ __forceinline__ int distinct_ids(const int32_t *ids, int n, int limit, int32_t *list) {
+  int id[BATCHES];
+#pragma unroll
+  for (int b = 0; b < BATCHES; ++b) {
+    const int i = 64 * b + (threadIdx.x & 63);
+    id[b] = i < n ? ids[i] : -1;
+  }
+  return distinct_values<BATCHES>(id, limit, list);
 }
 
 }  // namespace sparoa

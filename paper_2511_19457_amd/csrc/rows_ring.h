@@ -91,15 +91,15 @@ struct Tile {
   int64_t row0, end;  // rows [row0, min(row0 + BM, end)); end 0: no tile
 };
 
-// The tile of work-group b: XCD b % 8 has the b % 8-th run of the tiles that
-// there are (their number follows from the plan), column tiles innermost.
+// The tile of work-group b where every work-group has one: XCD b % 8 has the
+// b % 8-th run of the tiles that there are (their number follows from the
+// plan), column tiles innermost.  Each wave finds it by itself.
 template <RowsMode MODE, int BM>
 __device__ __forceinline__ Tile find_tile(const RowsArgs &a, int cols) {
   const int lane = threadIdx.x & 63, b = blockIdx.x;
   Tile t{0, 0, 0, 0};
-  int total;
+  int total = 0;
   if constexpr (MODE <= kRowsDown) {
-    total = 0;
     for (int e0 = 0; e0 < a.experts; e0 += 64) {
       const int e = min(e0 + lane, a.experts - 1);
       const int n = e0 + lane < a.experts ? a.plan[e + 1] - a.plan[e] : 0;
@@ -111,9 +111,9 @@ __device__ __forceinline__ Tile find_tile(const RowsArgs &a, int cols) {
   const int64_t tiles = (int64_t)total * cols, per = (tiles + 7) / 8;
   const int64_t id = (b & 7) * per + (b >> 3);
   if ((b >> 3) >= per || id >= tiles) return t;
+  int rt = (int)(id / cols);
+  t.col = (int)(id - (int64_t)rt * cols);
   if constexpr (MODE <= kRowsDown) {
-    int rt = (int)(id / cols);
-    t.col = (int)(id - (int64_t)rt * cols);
     for (int e0 = 0; e0 < a.experts; e0 += 64) {
       const int e = min(e0 + lane, a.experts - 1);
       const int at = a.plan[e], end = a.plan[e + 1];
@@ -131,16 +131,73 @@ __device__ __forceinline__ Tile find_tile(const RowsArgs &a, int cols) {
       rt -= __builtin_amdgcn_readlane(upto, 63);
     }
   } else {
-    // column groups outermost: an XCD keeps to a part of the weights
-    const int per_group = (cols + a.col_groups - 1) / a.col_groups;
-    const int group = (int)(id / ((int64_t)total * per_group));
-    const int64_t in = id - (int64_t)group * total * per_group;
-    const int wide = min(per_group, cols - group * per_group);
-    t.row0 = in / wide * BM;
-    t.col = group * per_group + (int)(in % wide);
+    t.row0 = (int64_t)rt * BM;
     t.end = a.rows;
   }
   return t;
 }
+
+// The walk of work-groups that take several tiles: the same runs, of which an
+// XCD's work-groups take every gridDim.x / 8-th tile.
+template <RowsMode MODE, int BM>
+struct TileWalk {
+  static constexpr bool kExperts = MODE <= kRowsDown;
+  const RowsArgs &a;
+  const int32_t *cum;   // LDS: row tiles of the experts up to each
+  int cols, total;
+  int64_t at, end;      // this work-group's next tile, and its XCD's end
+
+  // One wave fills the table; a barrier, then start().
+  static __device__ __forceinline__ void fill(const RowsArgs &a, int32_t *cum) {
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+    for (int e0 = 0; e0 < a.experts; e0 += 64) {
+      const int e = e0 + lane;
+      const int n = e < a.experts ? a.plan[e + 1] - a.plan[e] : 0;
+      const int upto = before + wave_prefix((n + BM - 1) / BM);
+      if (e < a.experts) cum[e] = upto;
+      before = __builtin_amdgcn_readlane(upto, 63);
+    }
+  }
+  __device__ __forceinline__ void start(int column_tiles) {
+    cols = column_tiles;
+    total = kExperts ? __builtin_amdgcn_readfirstlane(cum[a.experts - 1])
+                     : (int)((a.rows + BM - 1) / BM);
+    const int64_t tiles = (int64_t)total * cols, per = (tiles + 7) / 8;
+    const int xcd = blockIdx.x & 7;
+    at = xcd * per + (blockIdx.x >> 3);
+    end = std::min<int64_t>((xcd + 1) * per, tiles);
+  }
+  __device__ __forceinline__ Tile next() {
+    Tile t{0, 0, 0, 0};
+    if (at >= end) return t;
+    const int64_t id = at;
+    at += gridDim.x >> 3;
+    if constexpr (kExperts) {
+      const int rt = (int)(id / cols), lane = threadIdx.x & 63;
+      t.col = (int)(id - (int64_t)rt * cols);
+      for (int e0 = 0; e0 < a.experts; e0 += 64) {
+        const int upto = cum[min(e0 + lane, a.experts - 1)];
+        const uint64_t past = __ballot(upto > rt);
+        if (!past) continue;
+        t.seg = e0 + __builtin_ctzll(past);
+        const int first = t.seg ? __builtin_amdgcn_readfirstlane(cum[t.seg - 1]) : 0;
+        t.row0 = uniform_word(a.plan + t.seg) + (int64_t)(rt - first) * BM;
+        t.end = uniform_word(a.plan + t.seg + 1);
+        break;
+      }
+    } else {
+      // column groups outermost: an XCD keeps to a part of the weights
+      const int per_group = (cols + a.col_groups - 1) / a.col_groups;
+      const int group = (int)(id / ((int64_t)total * per_group));
+      const int64_t in = id - (int64_t)group * total * per_group;
+      const int wide = min(per_group, cols - group * per_group);
+      t.row0 = in / wide * BM;
+      t.col = group * per_group + (int)(in % wide);
+      t.end = a.rows;
+    }
+    return t;
+  }
+};
 
 }  // namespace sparoa

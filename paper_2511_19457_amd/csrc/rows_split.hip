@@ -250,7 +250,6 @@ void launch_one(RowsArgs a, hipStream_t stream) {
   const int64_t row_tiles = MODE <= kRowsDown
                                 ? a.rows / BM + std::min<int64_t>(a.experts, a.rows)
                                 : cdiv(a.rows, BM);
-  a.col_groups = 1;
   const unsigned grid = (unsigned)(8 * cdiv(row_tiles * cols, 8));
   rows_split_kernel<DT, MODE, TM, TN, NW, S><<<grid, 64 * NW, 0, stream>>>(a);
 }

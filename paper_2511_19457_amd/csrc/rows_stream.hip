@@ -21,13 +21,6 @@ namespace {
 
 constexpr int kNW = 8, kNT = 64 * kNW;   // waves, threads
 
-// A word every lane wants alike, by the scalar unit: memory that no kernel of
-// this launch writes.
-__device__ __forceinline__ int uniform_word(const int32_t *p) {
-  return *reinterpret_cast<const __attribute__((address_space(4))) int32_t *>(
-      reinterpret_cast<uintptr_t>(p));
-}
-
 // One operand matrix: 16-byte pieces of rows at any element.
 template <int DT>
 struct Operand {

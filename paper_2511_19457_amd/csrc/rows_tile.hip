@@ -20,6 +20,13 @@
 namespace sparoa {
 namespace {
 
+// The lane's number, anew: what is derived from it is not kept in registers
+// through the K loop.
+__device__ __forceinline__ int fresh_lane(int lane) {
+  asm volatile("" : "+v"(lane));
+  return lane;
+}
+
 template <int DT, RowsMode MODE, int WGM, int WGN, int WTM, int WTN, int S>
 __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a) {
   using E = Elem<DT>;
@@ -32,19 +39,23 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
   static_assert(WTN % 4 == 0 && NW % 2 == 0, "a lane's channels; weight row swizzle");
   constexpr int L = AV + BV;       // loads per wave and chunk
   constexpr int NG = WTN / 4;      // groups of 64 weight rows of a wave
-  constexpr int STAGE = (BM + BN) * kRow;
-  __shared__ __attribute__((aligned(1024))) char smem[S * STAGE];
+  // the stages of x, then those of the weights (offsets that fit an LDS read)
+  constexpr int XS = BM * kRow, WS = BN * kRow, W0 = S * XS;
+  __shared__ __attribute__((aligned(1024))) char smem[S * (XS + WS) + (FC ? NW * 1024 : 0)];
   __shared__ int32_t list[FC ? BM : 1];
   __shared__ int list_len;
+  __shared__ int32_t cum[MODE <= kRowsDown ? kMaxExperts : 1];
 
-  const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = wave / WGN, wn = wave % WGN;
-  const Tile tl = find_tile<MODE, BM>(a, (a.n + OC - 1) / OC);
+  TileWalk<MODE, BM> walk{a, cum};
+  if constexpr (walk.kExperts) {
+    if (wave == 0) walk.fill(a, cum);
+    __syncthreads();
+  }
+  walk.start((a.n + OC - 1) / OC);
+  Tile tl = walk.next();
   if (tl.end == 0) return;
-  const int n0 = tl.col * OC;
-  const int64_t row0 = tl.row0;
-  const int rows = (int)std::min<int64_t>(tl.end - row0, BM);
   const int kbytes = a.k * E::size;
   const int n = (kbytes + kRow - 1) / kRow;
 
@@ -54,283 +65,361 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
   // row & 7; weight rows, read in the order that leaves a lane 8 consecutive
   // channels (MFMA row 4 q + t of block b is tile row 32 (b / 2) + 8 q + 4 (b %
   // 2) + t), f = (row >> 3 & 1) * 4 + (row & 3).
-  const int lrow = lane >> 3;
-  const int cgA = (lane & 7) ^ lrow;
-  const int cgB = (lane & 7) ^ (((wave & 1) << 2) | (lrow & 3));
-  const bool gather = MODE <= kRowsUpGated;
-  const u32x4 xr = gather ? descriptor(a.x, a.x_bytes)
-                          : descriptor(reinterpret_cast<const char *>(a.x) +
-                                           row0 * a.ldx * E::size,
-                                       rows * a.ldx * E::size);
-  const u32x4 wr = descriptor(reinterpret_cast<const char *>(a.w) +
-                                  tl.seg * a.w_stride * E::size,
-                              (int64_t)a.w_rows * kbytes);
-  uint32_t a_off[AV], b_off[BV];
-  int a_id[AV];   // (FC) the row's adapter
-#pragma unroll
-  for (int u = 0; u < AV; ++u) {
-    const int r = 8 * (u * NW + wave) + lrow;
-    uint32_t row = r;
-    if (gather && r < rows) row = (uint32_t)a.order[row0 + r] / (uint32_t)a.top_k;
-    a_off[u] = r < rows ? row * (uint32_t)(a.ldx * E::size) + cgA * 16 : kOut;
-    a_id[u] = FC && a.ids && r < rows ? a.ids[row0 + r] : -1;
-  }
-#pragma unroll
-  for (int u = 0; u < BV; ++u) {
-    const int tr = 8 * (u * NW + wave) + lrow;
-    const int ch = n0 + (GATED ? (tr >> 6) * 32 + (tr & 31) : tr);
-    const int row = GATED && (tr & 32) ? a.n + ch : ch;
-    b_off[u] = ch < a.n ? (uint32_t)row * (uint32_t)kbytes + cgB * 16 : kOut;
-  }
+  auto vector_a = [&](int l) { return (l & 7) ^ (l >> 3); };
+  auto vector_b = [&](int l) { return (l & 7) ^ (((wave & 1) << 2) | (l >> 3 & 3)); };
+  constexpr bool gather = MODE <= kRowsUpGated;
   // bits that put a lane's piece of the last chunk out of range, past K
   const int tail = kbytes - (n - 1) * kRow;
-  const uint32_t pastA = cgA * 16 < tail ? 0u : kOut, pastB = cgB * 16 < tail ? 0u : kOut;
 
-  // ---- chunks behind K's: the adapters among the rows
-  int extra = 0, rank_chunks = 1;
-  if constexpr (FC) {
-    if (a.ids) {
-      if (wave == 0) {
-        const int f = distinct_ids<(BM + 63) / 64>(a.ids + row0, rows, a.adapters, list);
-        if (lane == 0) list_len = f;
+  // What a tile's rows are known by: their slots (gathered) or adapters.
+  int place[AV], member[FC ? (BM + 63) / 64 : 1];
+  auto fetch = [&](const Tile &t) __attribute__((always_inline)) {
+    const int rows = (int)std::min<int64_t>(t.end - t.row0, BM);
+    const int lane = fresh_lane(threadIdx.x & 63), lrow = lane >> 3;
+    if constexpr (gather || FC) {
+      if (!gather && !a.ids) return;
+#pragma unroll
+      for (int u = 0; u < AV; ++u) {
+        const int64_t r = t.row0 + min(8 * (u * NW + wave) + lrow, rows - 1);
+        place[u] = gather ? a.order[r] : a.ids[r];
       }
-      __syncthreads();
-      rank_chunks = (a.rank * E::size + kRow - 1) / kRow;
-      extra = __builtin_amdgcn_readfirstlane(list_len) * rank_chunks;
+      if constexpr (FC) {
+#pragma unroll
+        for (int b = 0; b < (BM + 63) / 64; ++b) {
+          const int m = a.ids[t.row0 + min(64 * b + lane, rows - 1)];
+          member[b] = 64 * b + lane < rows ? m : -1;
+        }
+      }
     }
-  }
-  const int chunks = n + extra;
+  };
+  // The loads' descriptors and offsets of a tile, and the adapters among its
+  // rows (chunks behind K's) in the list, which a barrier follows.
+  u32x4 xr, wr;
+  uint32_t a_off[AV], b_off[BV];
+  int row_id[FC ? AV : 1];   // adapters of this lane's rows
+  int rows = 0, n0 = 0;
+  int64_t row0 = 0;
+  auto make = [&](const Tile &t) __attribute__((always_inline)) {
+    const int lane = fresh_lane(threadIdx.x & 63), lrow = lane >> 3;
+    const int cgA = vector_a(lane), cgB = vector_b(lane);
+    n0 = t.col * OC, row0 = t.row0;
+    rows = (int)std::min<int64_t>(t.end - row0, BM);
+    xr = gather ? descriptor(a.x, a.x_bytes)
+                : descriptor(reinterpret_cast<const char *>(a.x) + row0 * a.ldx * E::size,
+                             rows * a.ldx * E::size);
+    wr = descriptor(reinterpret_cast<const char *>(a.w) + t.seg * a.w_stride * E::size,
+                    (int64_t)a.w_rows * kbytes);
+#pragma unroll
+    for (int u = 0; u < AV; ++u) {
+      const int r = 8 * (u * NW + wave) + lrow;
+      const uint32_t row = gather ? (uint32_t)place[u] / (uint32_t)a.top_k : (uint32_t)r;
+      a_off[u] = r < rows ? row * (uint32_t)(a.ldx * E::size) + cgA * 16 : kOut;
+      if constexpr (FC) row_id[u] = a.ids && r < rows ? place[u] : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < BV; ++u) {
+      const int tr = 8 * (u * NW + wave) + lrow;
+      const int ch = n0 + (GATED ? (tr >> 6) * 32 + (tr & 31) : tr);
+      const int row = GATED && (tr & 32) ? a.n + ch : ch;
+      b_off[u] = ch < a.n ? (uint32_t)row * (uint32_t)kbytes + cgB * 16 : kOut;
+    }
+    if constexpr (FC) {
+      if (a.ids && wave == 0) {
+        const int f = distinct_values<(BM + 63) / 64>(member, a.adapters, list);
+        if ((threadIdx.x & 63) == 0) list_len = f;
+      }
+    }
+  };
+  int chunks = n, rank_chunks = 1;
 
   const uint32_t ring =
       (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem + wave * 1024;
-  // load u of K's chunk i (any but the last) into the stage at dst
-  auto load_plain = [&](int i, uint32_t dst, int u) __attribute__((always_inline)) {
-    if (u < AV) ring_load(xr, dst + u * (NW * 1024), a_off[u], i * kRow);
-    else ring_load(wr, dst + BM * kRow + (u - AV) * (NW * 1024), b_off[u - AV], i * kRow);
+  // What keeps a chunk's loads out of range: nothing, pieces past K in K's last
+  // chunk, all of a chunk behind the last (loads that only keep the count).
+  uint32_t past_a, past_b;
+  {
+    const int l = threadIdx.x & 63;
+    past_a = vector_a(l) * 16 < tail ? 0u : kOut;
+    past_b = vector_b(l) * 16 < tail ? 0u : kOut;
+  }
+  auto outside = [&](int i, uint32_t past) __attribute__((always_inline)) {
+    return i < n - 1 ? 0u : i == n - 1 ? past : kOut;
   };
-  // the loads of any chunk
-  auto load_any = [&](int i, uint32_t dst) __attribute__((always_inline)) {
-    if (i < n) {
-      const uint32_t last = i == n - 1 ? kOut : 0u;
+  // load u of K's chunk i into stage `slot` (behind K: zeros; in an adapter's
+  // chunk the loads only keep the count, to a place apart)
+  auto load_part = [&](int i, int slot, int u, uint32_t oa, uint32_t ob)
+                       __attribute__((always_inline)) {
+    const bool apart = FC && i >= n && i < chunks;
+    const uint32_t to = apart ? ring + S * (XS + WS)
+                        : u < AV ? ring + slot * XS + u * (NW * 1024)
+                                 : ring + W0 + slot * WS + (u - AV) * (NW * 1024);
+    if (u < AV) ring_load(xr, to, a_off[u] | oa, i * kRow);
+    else ring_load(wr, to, b_off[u - AV] | ob, i * kRow);
+  };
+  // the loads of adapters' chunk i
+  auto load_adapter = [&](int i, int slot) __attribute__((always_inline)) {
+    const int lane = fresh_lane(threadIdx.x & 63), lrow = lane >> 3;
+    const int cgA = vector_a(lane), cgB = vector_b(lane);
+    const uint32_t xd = ring + slot * XS, wd = ring + W0 + slot * WS;
+    const int c = i - n, d = c / rank_chunks, r = (c - d * rank_chunks) * kRow;
+    const int id = __builtin_amdgcn_readfirstlane(list[d]);
+    const int hbytes = a.ldh * E::size;   // (columns past the rank hold zeros)
+    const u32x4 hr = descriptor(reinterpret_cast<const char *>(a.h) + row0 * hbytes,
+                                (int64_t)rows * hbytes);
 #pragma unroll
-      for (int u = 0; u < AV; ++u)
-        ring_load(xr, dst + u * (NW * 1024), a_off[u] | (pastA & last), i * kRow);
-#pragma unroll
-      for (int u = 0; u < BV; ++u)
-        ring_load(wr, dst + BM * kRow + u * (NW * 1024), b_off[u] | (pastB & last), i * kRow);
-      return;
+    for (int u = 0; u < AV; ++u) {
+      const int row = 8 * (u * NW + wave) + lrow;
+      const bool in = row_id[FC ? u : 0] == id && r + cgA * 16 < hbytes;
+      ring_load(hr, xd + u * (NW * 1024), in ? (uint32_t)(row * hbytes + r + cgA * 16) : kOut, 0);
     }
-    if constexpr (FC) {
-      const int c = i - n, d = c / rank_chunks, r = (c - d * rank_chunks) * kRow;
-      const int id = __builtin_amdgcn_readfirstlane(list[d]);
-      const int hbytes = a.ldh * E::size;   // (columns past the rank hold zeros)
-      const u32x4 hr = descriptor(reinterpret_cast<const char *>(a.h) + row0 * hbytes,
-                                  (int64_t)rows * hbytes);
 #pragma unroll
-      for (int u = 0; u < AV; ++u) {
-        const int row = 8 * (u * NW + wave) + lrow;
-        const bool in = a_id[u] == id && r + cgA * 16 < hbytes;
-        ring_load(hr, dst + u * (NW * 1024),
-                  in ? (uint32_t)(row * hbytes + r + cgA * 16) : kOut, 0);
-      }
-#pragma unroll
-      for (int u = 0; u < BV; ++u)
-        rank_piece<DT>(a, id, n0 + 8 * (u * NW + wave) + lrow, r + cgB * 16,
-                       dst + BM * kRow + u * (NW * 1024),
-                       smem + (dst - ring) + wave * 1024 + BM * kRow + u * (NW * 1024));
-    }
+    for (int u = 0; u < BV; ++u)
+      rank_piece<DT>(a, id, n0 + 8 * (u * NW + wave) + lrow, r + cgB * 16,
+                     wd + u * (NW * 1024), smem + W0 + slot * WS + (wave + u * NW) * 1024);
   };
 
   f32x4 acc[WTM][WTN];
+  const int fB = [&](int rl) { return (((rl >> 2) & 1) << 2) | (rl & 3); }(threadIdx.x & 15);
+  int offA[2], offB[2];   // this lane's operand offsets of a chunk's two halves
+  {
+    const int g = (threadIdx.x & 63) >> 4, rl = threadIdx.x & 15;
 #pragma unroll
-  for (int i = 0; i < WTM; ++i)
-#pragma unroll
-    for (int j = 0; j < WTN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-  const int g = lane >> 4, rl = lane & 15;
-  const int fB = (((rl >> 2) & 1) << 2) | (rl & 3);
-  int offA[2], offB[2];   // this lane's operand offsets of the chunk's two halves
-#pragma unroll
-  for (int ks = 0; ks < 2; ++ks) {
-    offA[ks] = (wm * WTM * 16 + rl) * kRow + 16 * ((4 * ks + g) ^ (rl & 7));
-    offB[ks] = (BM + wn * WTN * 16 + 8 * (rl >> 2) + (rl & 3)) * kRow + 16 * ((4 * ks + g) ^ fB);
+    for (int ks = 0; ks < 2; ++ks) {
+      offA[ks] = (wm * WTM * 16 + rl) * kRow + 16 * ((4 * ks + g) ^ (rl & 7));
+      offB[ks] = W0 + (wn * WTN * 16 + 8 * (rl >> 2) + (rl & 3)) * kRow + 16 * ((4 * ks + g) ^ fB);
+    }
   }
-  struct Operands {
-    u32x4 x[2][WTM], w[2][WTN];
-  };
-  constexpr int R = 2 * (WTM + WTN), MF = 2 * WTM * WTN, RSPAN = MF * 3 / 4;
-  auto read_part = [&](Operands &o, int slot, int q) __attribute__((always_inline)) {
-    const int ks = q / (WTM + WTN), v = q % (WTM + WTN);
-    const char *st = smem + slot * STAGE;
-    if (v < WTN)
-      o.w[ks][v] = *reinterpret_cast<const u32x4 *>(st + offB[ks] +
-                                                    (32 * (v >> 1) + 4 * (v & 1)) * kRow);
-    else
-      o.x[ks][v - WTN] = *reinterpret_cast<const u32x4 *>(st + offA[ks] + (v - WTN) * 16 * kRow);
-  };
-  // One step per chunk: on entry its operands are in registers or on their
-  // way.  Steady steps (a next chunk, and a refill that is not K's last) have
-  // no branch and constant stages.
-  // A wave whose rows all lie past the segment only loads.
-  const bool busy_wave = wm * WTM * 16 < rows;
-  auto step = [&](auto steady, auto busy, Operands &cur, Operands &nxt, int slot, int i)
-                  __attribute__((always_inline)) {
-    constexpr bool STEADY = decltype(steady)::value, BUSY = decltype(busy)::value;
-    const bool more = STEADY || i + 1 < chunks, refill = STEADY || i + S < chunks;
-    const uint32_t dst = ring + slot * STAGE;
-    if (more) {
-      if constexpr (STEADY) wait_ring<S - 2, L>(S - 2);
-      else wait_ring<S - 2, L>(min(S - 2, chunks - 2 - i));
-      __builtin_amdgcn_s_waitcnt(kLdsDone);   // this wave has read its stage
-      asm volatile("s_barrier" ::: "memory");
-    }
-    const int nslot = slot == S - 1 ? 0 : slot + 1;
-    if (!STEADY && refill) load_any(i + S, dst);
-#pragma unroll
-    for (int m = 0; m < MF; ++m) {
-      const int ks = m / (WTM * WTN), tm = m / WTN % WTM, b = m % WTN;
-      __builtin_amdgcn_sched_barrier(0);
-      if constexpr (BUSY) acc[tm][b] = mma16<DT>(cur.w[ks][b], cur.x[ks][tm], acc[tm][b]);
-      if (BUSY && more) {
-#pragma unroll
-        for (int q = m * R / RSPAN; q < (m + 1) * R / RSPAN && q < R; ++q) read_part(nxt, nslot, q);
-      }
-      if constexpr (STEADY) {
-#pragma unroll
-        for (int u = m * L / MF; u < (m + 1) * L / MF; ++u) load_plain(i + S, dst, u);
+  // Everything a tile needs before its K loop: list, then the first chunks.
+  auto begin = [&](const Tile &t) __attribute__((always_inline)) {
+    make(t);
+    __builtin_amdgcn_s_waitcnt(kLdsDone);
+    asm volatile("s_barrier" ::: "memory");   // (and every wave has read its last stage)
+    if constexpr (FC) {
+      if (a.ids) {
+        rank_chunks = (a.rank * E::size + kRow - 1) / kRow;
+        chunks = n + __builtin_amdgcn_readfirstlane(list_len) * rank_chunks;
       }
     }
-    __builtin_amdgcn_sched_barrier(0);
-  };
 #pragma unroll
-  for (int s = 0; s < S; ++s)
-    if (s < chunks) load_any(s, ring + s * STAGE);
-  wait_ring<S - 1, L>(min(S - 1, chunks - 1));
-  __builtin_amdgcn_s_waitcnt(kLdsDone);   // (pieces that passed through registers)
-  asm volatile("s_barrier" ::: "memory");
+    for (int s = 0; s < S; ++s) {
+      if (FC && s >= n && s < chunks) load_adapter(s, s);
+      const uint32_t oa = outside(s, past_a), ob = outside(s, past_b);
+#pragma unroll
+      for (int u = 0; u < L; ++u) load_part(s, s, u, oa, ob);
+    }
+  };
+  // The K loop.  A chunk's operands are read from LDS, and the loads that refill
+  // the stage freed by the barrier are sent, between the MFMAs of the chunk
+  // before, so they have a chunk's time to land.  No branch but the turn of two
+  // chunks: loads behind the last chunk fall out of range, and so an odd last
+  // chunk is followed by one of zeros.  A wave whose rows all lie past the
+  // segment only loads.
   auto run = [&](auto busy) __attribute__((always_inline)) {
-    Operands p, q;
-    if constexpr (decltype(busy)::value) {
+    constexpr bool BUSY = decltype(busy)::value;
+    constexpr int MF = 2 * WTM * WTN, R = 2 * (WTM + WTN), RSPAN = MF * 3 / 4;
+    struct Operands {
+      u32x4 x[2][WTM], w[2][WTN];
+    } p, q;
+    auto read = [&](Operands &o, int slot, int v) __attribute__((always_inline)) {
+      const int ks = v / (WTM + WTN), b = v % (WTM + WTN);
+      if (b < WTN)
+        o.w[ks][b] = *reinterpret_cast<const u32x4 *>(smem + offB[ks] + slot * WS +
+                                                      (32 * (b >> 1) + 4 * (b & 1)) * kRow);
+      else
+        o.x[ks][b - WTN] = *reinterpret_cast<const u32x4 *>(smem + offA[ks] + slot * XS +
+                                                            (b - WTN) * 16 * kRow);
+    };
+    int slot = 0;
+    auto step = [&](int i, const Operands &cur, Operands &nxt) __attribute__((always_inline)) {
+      if (i >= S - 1) wait_ring<S - 2, L>(S - 2);   // (the first S have landed)
+      __builtin_amdgcn_s_waitcnt(kLdsDone);         // this wave has read its stage
+      asm volatile("s_barrier" ::: "memory");
+      if (FC && i + S >= n && i + S < chunks) load_adapter(i + S, slot);
+      const int next = slot == S - 1 ? 0 : slot + 1;
+      const uint32_t oa = outside(i + S, past_a), ob = outside(i + S, past_b);
 #pragma unroll
-      for (int r = 0; r < R; ++r) read_part(p, 0, r);
-    }
-    constexpr int U = S % 2 ? 2 * S : S;   // a turn of the ring and of (p, q)
-    int i = 0;
-    for (; i + U + S < n; i += U) {
+      for (int m = 0; m < MF; ++m) {
+        const int ks = m / (WTM * WTN), tm = m / WTN % WTM, b = m % WTN;
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (BUSY) {
+          acc[tm][b] = mma16<DT>(cur.w[ks][b], cur.x[ks][tm], acc[tm][b]);
 #pragma unroll
-      for (int d = 0; d < U; ++d)
-        step(std::true_type{}, busy, d % 2 ? q : p, d % 2 ? p : q, d % S, i + d);
-    }
-    for (; i < chunks; i += U) {
+          for (int v = m * R / RSPAN; v < (m + 1) * R / RSPAN && v < R; ++v) read(nxt, next, v);
+        }
 #pragma unroll
-      for (int d = 0; d < U; ++d)
-        if (i + d < chunks)
-          step(std::false_type{}, busy, d % 2 ? q : p, d % 2 ? p : q, d % S, i + d);
-    }
-  };
-  if (!busy_wave) return run(std::false_type{});
-  run(std::true_type{});
-
-  // ---- epilogue, from registers: 8 consecutive channels of a row at a time
-  const int mw = wm * WTM * 16 + rl;
-  const bool whole = a.n % 8 == 0 && a.ldy % 8 == 0;
-  const raw *bias = reinterpret_cast<const raw *>(a.bias) + (a.bias ? (int64_t)tl.seg * a.w_rows : 0);
-  auto get8 = [&](const raw *p, int c, float (&v)[8]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = E::to_f32(p[min(c + e, a.n - 1)]);
-  };
-#pragma unroll
-  for (int q = 0; q < NG; ++q)
-#pragma unroll
-    for (int h = 0; h < (GATED ? 1 : 2); ++h) {
-      const int col = n0 + 8 * g + (GATED ? wn * WTN * 8 + 32 * q : wn * WTN * 16 + 64 * q + 32 * h);
-      if (col >= a.n) continue;
-      float bv[8], bu[8];
-      if (a.bias) {
-        get8(bias, col, bv);
-        if constexpr (GATED) get8(bias + a.n, col, bu);
+        for (int u = m * L / MF; u < (m + 1) * L / MF; ++u) load_part(i + S, slot, u, oa, ob);
       }
+      __builtin_amdgcn_sched_barrier(0);
+      slot = next;
+    };
+    if constexpr (BUSY) {
 #pragma unroll
-      for (int tm = 0; tm < WTM; ++tm) {
-        const int r = mw + 16 * tm;
-        if (r >= rows) continue;
-        const int64_t at = (row0 + r) * a.ldy + col;
-        float o[8];
+      for (int v = 0; v < R; ++v) read(p, 0, v);
+    }
+    for (int i = 0; i < chunks; i += 2) {
+      step(i, p, q);
+      step(i + 1, q, p);
+    }
+  };
+  // The epilogue, from registers: 8 consecutive channels of a row at a time.
+  // WHOLE vectors are stored unconditionally, those of no row or column at an
+  // offset past the range, so the next tile's first wait knows their number.
+  constexpr int OS = MODE == kRowsDown ? 4 : E::size;   // (z is fp32)
+  constexpr int kStores = WTM * NG * (GATED ? 1 : 2) * (OS / 2);
+  const bool whole = MODE == kRowsDown || (a.n % 8 == 0 && a.ldy % 8 == 0);
+  auto finish = [&](auto vectors, int seg, int n0, int64_t row0, int rows)
+                    __attribute__((always_inline)) {
+    constexpr bool WHOLE = decltype(vectors)::value;
+    const int lane = fresh_lane(threadIdx.x & 63), g = lane >> 4;
+    const int mw = wm * WTM * 16 + (lane & 15);
+    const int64_t y0 = row0 * a.ldy;
+    const __amdgpu_buffer_rsrc_t yr = __builtin_amdgcn_make_buffer_rsrc(
+        reinterpret_cast<char *>(a.y) + y0 * OS, (short)0, (int)(rows * a.ldy * OS), kBufDword3);
+    const raw *res = FC && a.residual ? reinterpret_cast<const raw *>(a.residual) + y0 : nullptr;
+    const __amdgpu_buffer_rsrc_t rr = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<raw *>(res), (short)0, res ? (int)(rows * a.ldy * E::size) : 0, kBufDword3);
+    const raw *bias = a.bias ? reinterpret_cast<const raw *>(a.bias) + (int64_t)seg * a.w_rows
+                             : nullptr;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          o[e] = acc[tm][4 * q + 2 * h + (e >> 2)][e & 3];
-          if (a.bias) o[e] += bv[e];
-          if constexpr (GATED) {
-            float up = acc[tm][4 * q + 2 + (e >> 2)][e & 3];
-            if (a.bias) up += bu[e];
-            o[e] = block_act(o[e], a.act) * up;
+    for (int q = 0; q < NG; ++q)
+#pragma unroll
+      for (int h = 0; h < (GATED ? 1 : 2); ++h) {
+        const int col = n0 + 8 * g + (GATED ? wn * WTN * 8 + 32 * q
+                                            : wn * WTN * 16 + 64 * q + 32 * h);
+        float bv[8], bu[8];
+        if (bias) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int c = min(col + e, a.n - 1);
+            bv[e] = E::to_f32(bias[c]);
+            if constexpr (GATED) bu[e] = E::to_f32(bias[a.n + c]);
           }
         }
-        if constexpr (MODE == kRowsDown) {
-          float *z = reinterpret_cast<float *>(a.y) + at;   // (rows padded to 8 channels)
-          *reinterpret_cast<f32x4 *>(z) = f32x4{o[0], o[1], o[2], o[3]};
-          *reinterpret_cast<f32x4 *>(z + 4) = f32x4{o[4], o[5], o[6], o[7]};
-          continue;
-        }
-        raw *y = reinterpret_cast<raw *>(a.y) + at;
-        if (FC && a.residual) {
-          const raw *res = reinterpret_cast<const raw *>(a.residual) + at;
-          float rv[8];
-          if (whole) {
-            raw t[8];
-            __builtin_memcpy(t, __builtin_assume_aligned(res, 16), sizeof t);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) rv[e] = E::to_f32(t[e]);
+        for (int tm = 0; tm < WTM; ++tm) {
+          const int r = mw + 16 * tm;
+          const bool in = r < rows && col < a.n;
+          const uint32_t at = r * (uint32_t)a.ldy + col;   // (below 2^31 bytes)
+          float o[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            o[e] = acc[tm][4 * q + 2 * h + (e >> 2)][e & 3];
+            if (bias) o[e] += bv[e];
+            if constexpr (GATED) {
+              float up = acc[tm][4 * q + 2 + (e >> 2)][e & 3];
+              if (bias) up += bu[e];
+              o[e] = block_act(o[e], a.act) * up;
+            }
+          }
+          if (FC && res) {
+            constexpr int RV = E::size / 2;   // 16-byte vectors of 8 elements
+            u32x4 t[RV] = {};
+            if constexpr (WHOLE) {
+#pragma unroll
+              for (int v = 0; v < RV; ++v)
+                t[v] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                     rr, in ? at * E::size + 16 * v : kOut, 0, 0));
+            }
+            raw e8[8];
+            __builtin_memcpy(e8, t, sizeof e8);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              if constexpr (!WHOLE) e8[e] = in && col + e < a.n ? res[at + e] : (raw)0;
+              o[e] += E::to_f32(e8[e]);
+            }
+          }
+          if constexpr (MODE == kRowsUp || FC) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = FC ? apply_act(o[e], a.act) : block_act(o[e], a.act);
+          }
+          if constexpr (OS == 4 && WHOLE) {
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+              const f32x4 f = {o[4 * v], o[4 * v + 1], o[4 * v + 2], o[4 * v + 3]};
+              __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f), yr,
+                                                     in ? at * 4 + 16 * v : kOut, 0, 0);
+            }
+          } else if constexpr (WHOLE) {
+            __builtin_amdgcn_raw_buffer_store_b128(pack8<DT>(o), yr, in ? at * 2 : kOut, 0, 0);
           } else {
+            raw *y = reinterpret_cast<raw *>(a.y) + y0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) rv[e] = col + e < a.n ? E::to_f32(res[e]) : 0.f;
+            for (int e = 0; e < 8; ++e)
+              if (in && col + e < a.n) y[at + e] = E::from_f32(o[e]);
           }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] += rv[e];
-        }
-        if constexpr (!GATED) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) o[e] = FC ? apply_act(o[e], a.act) : block_act(o[e], a.act);
-        }
-        if (whole) {
-          raw t[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) t[e] = E::from_f32(o[e]);
-          __builtin_memcpy(__builtin_assume_aligned(y, 16), t, sizeof t);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (col + e < a.n) y[e] = E::from_f32(o[e]);
         }
       }
+  };
+
+  // ---- tile by tile.  The next tile's first chunks are sent for before the
+  // epilogue, and the rows of the tile behind it before the stores, which are
+  // then the newest operations: K starts when the chunks have landed, under
+  // the stores.
+  fetch(tl);
+  begin(tl);
+  Tile nt = walk.next();
+  if (nt.end) fetch(nt);
+  bool stored = false;
+  for (;;) {
+    const bool busy = wm * WTM * 16 < rows;
+    static_assert(kStores < 64, "vmcnt range");
+    if (stored) __builtin_amdgcn_s_waitcnt(vm_outstanding(kStores));
+    else __builtin_amdgcn_s_waitcnt(vm_outstanding(0));
+    __builtin_amdgcn_s_waitcnt(kLdsDone);   // (pieces that passed through registers)
+    asm volatile("s_barrier" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < WTM; ++i)
+#pragma unroll
+      for (int j = 0; j < WTN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (busy) run(std::true_type{});
+    else run(std::false_type{});
+    const int seg = tl.seg, n0_ = n0, rows_ = rows;
+    const int64_t row0_ = row0;
+    const bool more = nt.end != 0;
+    if (more) {
+      tl = nt;
+      begin(tl);
+      nt = walk.next();
+      if (nt.end) fetch(nt);
     }
+    if (busy) {
+      if (whole) finish(std::true_type{}, seg, n0_, row0_, rows_);
+      else if constexpr (MODE != kRowsDown) finish(std::false_type{}, seg, n0_, row0_, rows_);
+    }
+    stored = busy && whole;
+    if (!more) return;
+  }
 }
 
 template <int DT, RowsMode MODE, int WGM, int WGN, int WTM, int WTN, int S>
-void launch_one(RowsArgs a, hipStream_t stream) {
+sparoa_status launch_one(RowsArgs a, hipStream_t stream) {
   constexpr int BM = 16 * WGM * WTM, BN = 16 * WGN * WTN;
   const int64_t cols = cdiv(a.n, MODE == kRowsUpGated ? BN / 2 : BN);
   const int64_t row_tiles = MODE <= kRowsDown
                                 ? a.rows / BM + std::min<int64_t>(a.experts, a.rows)
                                 : cdiv(a.rows, BM);
   a.col_groups = cols >= 8 ? 2 : 1;
-  const unsigned grid = (unsigned)(8 * cdiv(row_tiles * cols, 8));
+  const void *fn = reinterpret_cast<const void *>(
+      &rows_tile_kernel<DT, MODE, WGM, WGN, WTM, WTN, S>);
+  int resident = 0;
+  const sparoa_status st = resident_blocks(fn, 64 * WGM * WGN, 0, &resident);
+  if (st != SPAROA_OK) return st;
+  const unsigned grid =
+      (unsigned)(8 * cdiv(std::min<int64_t>(row_tiles * cols, resident), 8));
   rows_tile_kernel<DT, MODE, WGM, WGN, WTM, WTN, S><<<grid, 64 * WGM * WGN, 0, stream>>>(a);
+  return SPAROA_OK;
 }
 
 template <int DT, RowsMode MODE>
-void launch_mode(RowsTile tile, const RowsArgs &a, hipStream_t stream) {
-  if (tile == kTile128x256) {
-    if constexpr (DT != SPAROA_F32) launch_one<DT, MODE, 2, 4, 4, 4, 3>(a, stream);   // 144 KB
-  } else if (tile == kTile64x128) {
-    launch_one<DT, MODE, 2, 2, 2, 4, 3>(a, stream);                                   // 72 KB
-  } else {
-    launch_one<DT, MODE, 4, 1, 1, 4, 4>(a, stream);                                   // 64 KB
-  }
+sparoa_status launch_mode(RowsTile tile, const RowsArgs &a, hipStream_t stream) {
+  if constexpr (DT != SPAROA_F32)
+    if (tile == kTile128x256) return launch_one<DT, MODE, 2, 4, 4, 4, 3>(a, stream);   // 144 KB
+  if (tile == kTile64x128) return launch_one<DT, MODE, 2, 2, 2, 4, 3>(a, stream);      // 72 KB
+  return launch_one<DT, MODE, 4, 1, 1, 4, 4>(a, stream);                               // 64 KB
 }
 
 template <int DT>
-void launch_dt(RowsMode mode, RowsTile tile, const RowsArgs &a, hipStream_t stream) {
+sparoa_status launch_dt(RowsMode mode, RowsTile tile, const RowsArgs &a, hipStream_t stream) {
   switch (mode) {
     case kRowsUp: return launch_mode<DT, kRowsUp>(tile, a, stream);
     case kRowsUpGated: return launch_mode<DT, kRowsUpGated>(tile, a, stream);
@@ -343,11 +432,10 @@ void launch_dt(RowsMode mode, RowsTile tile, const RowsArgs &a, hipStream_t stre
 
 sparoa_status launch_rows_tile(RowsMode mode, RowsTile tile, const RowsArgs &a, sparoa_dtype dt,
                                hipStream_t stream) {
-  switch (dt) {
-    case SPAROA_F32: launch_dt<SPAROA_F32>(mode, tile, a, stream); break;
-    case SPAROA_F16: launch_dt<SPAROA_F16>(mode, tile, a, stream); break;
-    default: launch_dt<SPAROA_BF16>(mode, tile, a, stream); break;
-  }
+  const sparoa_status st = dt == SPAROA_F32   ? launch_dt<SPAROA_F32>(mode, tile, a, stream)
+                           : dt == SPAROA_F16 ? launch_dt<SPAROA_F16>(mode, tile, a, stream)
+                                              : launch_dt<SPAROA_BF16>(mode, tile, a, stream);
+  if (st != SPAROA_OK) return st;
   SPAROA_LAUNCH_CHECK("row product tiles");
   return SPAROA_OK;
 }
