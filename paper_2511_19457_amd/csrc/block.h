@@ -18,7 +18,7 @@ sparoa_status launch_block_norm(const NormArgs &a, sparoa_dtype dt, hipStream_t 
 // Routing and plan (expert_route.hip).  top_k <= 32, experts <= 512, groups <= 64.
 constexpr int kMaxExperts = 512;
 constexpr int kPlanBlocks = 256;       // blocks of tokens that leave their counts
-constexpr int kPlaceGroups = 64;       // work-groups that place slots by them
+constexpr int kPlaceGroups = 128;      // work-groups that place slots by them
 constexpr int kOneGroupSlots = 4096;   // given choices that one work-group plans
 struct RouteArgs {
   const void *logits;
@@ -27,13 +27,15 @@ struct RouteArgs {
   int32_t *idx;
   float *weights;
   int32_t *plan, *order, *place;   // the plan's parts; plan null: none is made
-  uint32_t *counts;                // workspace: [blocks][experts + 1]
+  uint32_t *counts;                // workspace: [blocks][count_stride]
   int64_t tokens;
   int experts, top_k, groups, top_groups, group_best, score, renormalise;
   int by_score;                    // keys are scores, not logits
   float scale;
   int64_t tokens_per_block;        // (set by the launchers)
   int blocks, blocks_per_group, bits;
+  int count_stride;                // words of a block's counts
+  int group_lanes;                 // lanes of a group that has lanes of its own, or 0
 };
 sparoa_status launch_expert_route(RouteArgs a, sparoa_dtype dt, hipStream_t stream);
 sparoa_status launch_expert_plan(RouteArgs a, hipStream_t stream);

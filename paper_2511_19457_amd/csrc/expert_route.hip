@@ -22,7 +22,7 @@
 namespace sparoa {
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kMaxWaves = 16;   // waves of a work-group (4 for up to 4 tokens)
 constexpr float kLow = -__builtin_inff();
 
 // Maximum over the wave, in every lane (no NaN among the values).
@@ -40,10 +40,33 @@ __device__ __forceinline__ float wave_max(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
 }
 
+// Sum over the wave, in every lane.
 __device__ __forceinline__ float wave_add(float v) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
-  return v;
+#define SPAROA_DPP_ADD(ctrl, rows)                                                         \
+  v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), \
+                                                             ctrl, rows, 0xF, false))
+  SPAROA_DPP_ADD(0x111, 0xF);
+  SPAROA_DPP_ADD(0x112, 0xF);
+  SPAROA_DPP_ADD(0x114, 0xF);
+  SPAROA_DPP_ADD(0x118, 0xF);
+  SPAROA_DPP_ADD(0x142, 0xA);
+  SPAROA_DPP_ADD(0x143, 0xC);
+#undef SPAROA_DPP_ADD
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+
+// The value of the lane that ctrl pairs with this one.
+template <int CTRL>
+__device__ __forceinline__ float paired(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF,
+                                                            0xF, true));
+}
+// The two best of the pair's four.
+template <int CTRL>
+__device__ __forceinline__ void merge_best(float &b1, float &b2) {
+  const float o1 = paired<CTRL>(b1), o2 = paired<CTRL>(b2);
+  b2 = __builtin_fmaxf(__builtin_fminf(b1, o1), __builtin_fmaxf(b2, o2));
+  b1 = __builtin_fmaxf(b1, o1);
 }
 
 // Orders LDS accesses of the lanes of one wave for the compiler (the hardware
@@ -66,22 +89,22 @@ __device__ __forceinline__ uint64_t same_lanes(int e, int bits) {
 
 // The work-group places slots [s0, s1).  first[e]: the place of the first of
 // them that goes to expert e (e = experts: no expert, places behind all
-// others, which hold -1).  cnt: kWaves x (experts + 1) words of LDS.
-template <class ExpertOf>
+// others, which hold -1).  cnt: W x (experts + 1) words of LDS, W the waves.
+template <int W, class ExpertOf>
 __device__ __forceinline__ void place_slots(int64_t s0, int64_t s1, int experts, int bits,
                                             const uint32_t *first, uint32_t *cnt,
                                             int32_t *order, int32_t *place, ExpertOf expert_of) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, nb = experts + 1;
   // wave w has the w-th run of whole 64s
-  const int64_t per = ((s1 - s0 + 63) / 64 + kWaves - 1) / kWaves * 64;
+  const int64_t per = ((s1 - s0 + 63) / 64 + W - 1) / W * 64;
   const int64_t b = s0 + wave * per, e_ = b + per < s1 ? b + per : s1;
-  for (int i = tid; i < kWaves * nb; i += kThreads) cnt[i] = 0;
+  for (int i = tid; i < W * nb; i += 64 * W) cnt[i] = 0;
   __syncthreads();
   for (int64_t s = b + lane; s < e_; s += 64) atomicAdd(&cnt[wave * nb + expert_of(s)], 1u);
   __syncthreads();
-  for (int e = tid; e < nb; e += kThreads) {
+  for (int e = tid; e < nb; e += 64 * W) {
     uint32_t at = first[e];
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       const uint32_t c = cnt[w * nb + e];
       cnt[w * nb + e] = at;
       at += c;
@@ -160,8 +183,12 @@ struct Router {
   int lpg;               // lanes per group (a power of two)
 
   __device__ Router(const RouteArgs &args) : a(args), lane(threadIdx.x & 63) {
-    lpg = 64;
-    while (lpg * a.groups > 64) lpg >>= 1;
+    // whole lanes to a group where its experts are a power of two of lanes
+    lpg = a.group_lanes;
+    if (!lpg) {
+      lpg = 64;
+      while (lpg * a.groups > 64) lpg >>= 1;
+    }
     const int per = a.experts / a.groups;
 #pragma unroll
     for (int i = 0; i < EPL; ++i) {
@@ -171,17 +198,23 @@ struct Router {
     }
   }
 
-  // Routes token t (the whole wave); chosen: LDS words for the keys of one
-  // wave, used where there are groups.  Afterwards lane j < top_k holds choice
-  // j (-1: none) and its weight.
-  __device__ void token(int64_t t, float *scratch, int &choice, float &weight) {
+  // This lane's logits of token t; an expert that takes no part holds -inf.
+  __device__ __forceinline__ void request(int64_t t, raw (&l)[EPL], bool &live) const {
     const raw *row = reinterpret_cast<const raw *>(a.logits) + t * a.experts;
-    const bool live = !a.token_mask || a.token_mask[t] != 0;
+    live = !a.token_mask || a.token_mask[t] != 0;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) l[i] = row[min(lane * EPL + i, a.experts - 1)];
+  }
+
+  // Routes token t (the whole wave); scratch: LDS words for the keys of one
+  // wave (groups that share lanes).  Afterwards lane j < top_k holds choice j
+  // (-1: none) and its weight.
+  __device__ __forceinline__ void token(int64_t t, const raw (&lr)[EPL], bool live,
+                                        float *scratch, int &choice, float &weight) {
     float l[EPL], key[EPL];
 #pragma unroll
     for (int i = 0; i < EPL; ++i) {
-      const int e = lane * EPL + i;
-      l[i] = live && e < a.experts ? E::to_f32(row[e]) : kLow;
+      l[i] = live && lane * EPL + i < a.experts ? E::to_f32(lr[i]) : kLow;
       l[i] = l[i] > kLow ? l[i] : kLow;   // a NaN takes no part either
     }
     const bool softmax = a.score == SPAROA_SCORE_SOFTMAX;
@@ -208,7 +241,7 @@ struct Router {
       }
       key[i] = k;
     }
-    if (a.groups > 1) {
+    if (a.groups > 1 && !a.group_lanes) {   // scores from LDS, then the keys one by one
 #pragma unroll
       for (int i = 0; i < EPL; ++i)
         if (lane * EPL + i < a.experts) scratch[lane * EPL + i] = key[i];
@@ -226,40 +259,58 @@ struct Router {
         b2 = __builtin_fmaxf(__builtin_fminf(b1, o1), __builtin_fmaxf(b2, o2));
         b1 = __builtin_fmaxf(b1, o1);
       }
-      const float score = a.group_best == 2 && b2 > kLow ? b1 + b2 : b1;
-      int rank = 0;
-      for (int o = 0; o < a.groups; ++o) {
-        const float s = __builtin_bit_cast(
-            float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, score), o * lpg));
-        rank += s > score || (s == score && o < g) ? 1 : 0;
-      }
-      const uint64_t keep = __ballot(g < a.groups && rank < a.top_groups && score > kLow);
+      const uint64_t keep = kept_groups(b1, b2);
 #pragma unroll
       for (int i = 0; i < EPL; ++i) key[i] = keep >> group_lane[i] & 1 ? key[i] : kLow;
       wave_fence();
     }
+    // this lane's keys in descending order (equal ones stay in the experts'),
+    // their places in bits 3 i of `order`
+    int at[EPL];
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) at[i] = i;
+#pragma unroll
+    for (int r = 0; r < EPL; ++r)
+#pragma unroll
+      for (int i = r & 1; i + 1 < EPL; i += 2) {
+        const bool swap = key[i + 1] > key[i];
+        const float k = swap ? key[i + 1] : key[i], o = swap ? key[i] : key[i + 1];
+        const int p = swap ? at[i + 1] : at[i], q = swap ? at[i] : at[i + 1];
+        key[i] = k, key[i + 1] = o, at[i] = p, at[i + 1] = q;
+      }
+    int order = 0;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) order |= at[i] << (3 * i);
+    if (a.group_lanes) {   // a lane's two best are its first two; its keys stay or go together
+      float b1 = key[0], b2 = kLow;
+      if constexpr (EPL > 1) b2 = key[1];
+      if (lpg > 1) merge_best<0xB1>(b1, b2);    // quad_perm 1 0 3 2
+      if (lpg > 2) merge_best<0x4E>(b1, b2);    // quad_perm 2 3 0 1
+      if (lpg > 4) merge_best<0x141>(b1, b2);   // row_half_mirror
+      if (lpg > 8) merge_best<0x140>(b1, b2);   // row_mirror
+      const uint64_t keep = kept_groups(b1, b2);
+      const bool stays = keep >> (lane & ~(lpg - 1)) & 1;
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) key[i] = stays ? key[i] : kLow;
+    }
     choice = -1;
-    float chosen = kLow;   // lane j: the logit of choice j
     for (int j = 0; j < a.top_k; ++j) {
-      float best = key[0], bl = l[0];
-      int bi = 0;
-#pragma unroll
-      for (int i = 1; i < EPL; ++i)
-        if (key[i] > best) best = key[i], bl = l[i], bi = i;
-      const float m = wave_max(best);
+      const float m = wave_max(key[0]);
       if (!(m > kLow)) break;
-      const int w = __ffsll((unsigned long long)__ballot(best == m)) - 1;
-      const int e = w * EPL + __builtin_amdgcn_readlane(bi, w);
-      const float el = __builtin_bit_cast(
-          float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, bl), w));
-      if (lane == j) choice = e, chosen = el;
+      const int w = __ffsll((unsigned long long)__ballot(key[0] == m)) - 1;
+      const int e = w * EPL + (__builtin_amdgcn_readlane(order, w) & 7);
+      choice = lane == j ? e : choice;
+      const bool won = lane == w;   // the next of its keys comes up
 #pragma unroll
-      for (int i = 0; i < EPL; ++i)
-        if (lane * EPL + i == e) key[i] = kLow;
+      for (int i = 0; i + 1 < EPL; ++i) key[i] = won ? key[i + 1] : key[i];
+      key[EPL - 1] = won ? kLow : key[EPL - 1];
+      order = won ? order >> 3 : order;
     }
     // weights: of the choices alone where they are renormalised (the softmax's
     // own sum cancels, and choices far below the row's largest logit keep
     // their ratios)
+    const raw *row = reinterpret_cast<const raw *>(a.logits) + t * a.experts;
+    const float chosen = choice >= 0 ? E::to_f32(row[choice]) : kLow;
     float s = 0.f;
     if (softmax) {
       if (a.renormalise) top = wave_max(chosen);
@@ -274,6 +325,20 @@ struct Router {
     }
     weight = choice >= 0 ? s * a.scale : 0.f;
   }
+
+  // Bit g lpg: group g is among the best; b1, b2: the two best keys of the
+  // group of this lane's lpg lanes.
+  __device__ __forceinline__ uint64_t kept_groups(float b1, float b2) const {
+    const int g = lane / lpg;
+    const float score = a.group_best == 2 && b2 > kLow ? b1 + b2 : b1;
+    int rank = 0;
+    for (int o = 0; o < a.groups; ++o) {
+      const float s = __builtin_bit_cast(
+          float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, score), o * lpg));
+      rank += s > score || (s == score && o < g) ? 1 : 0;
+    }
+    return __ballot(g < a.groups && rank < a.top_groups && score > kLow);
+  }
 };
 
 __device__ __forceinline__ int slot_expert(const int32_t *idx, int64_t s, int experts) {
@@ -281,24 +346,29 @@ __device__ __forceinline__ int slot_expert(const int32_t *idx, int64_t s, int ex
   return (uint32_t)e < (uint32_t)experts ? e : experts;
 }
 
-// Routes a block of tokens_per_block tokens a work-group.  ONE: the only
-// work-group, which also makes the plan (choices kept in LDS).
-template <int DT, int EPL, bool ONE>
-__global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
+// Routes a block of tokens_per_block tokens a work-group of W waves, a wave's
+// next token sent for before it chooses for one.  ONE: the only work-group,
+// which also makes the plan (choices kept in LDS).
+template <int DT, int EPL, bool ONE, int W>
+__global__ __launch_bounds__(64 * W) void route_kernel(RouteArgs a) {
   extern __shared__ uint32_t lds[];
   const int nb = a.experts + 1, wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   // [counts nb][first nb][keys of each wave, or the waves' counts][ONE: choices]
   uint32_t *total = lds, *first = lds + nb, *scratch = first + nb;
-  int32_t *mine = reinterpret_cast<int32_t *>(scratch + kWaves * nb);
-  for (int i = threadIdx.x; i < nb; i += kThreads) total[i] = 0;
-  __syncthreads();
-  Router<DT, EPL> r(a);
+  int32_t *mine = reinterpret_cast<int32_t *>(scratch + W * nb);
   const int64_t t0 = (int64_t)blockIdx.x * a.tokens_per_block;
   const int64_t t1 = t0 + a.tokens_per_block < a.tokens ? t0 + a.tokens_per_block : a.tokens;
-  for (int64_t t = t0 + wave; t < t1; t += kWaves) {
+  Router<DT, EPL> r(a);
+  typename Elem<DT>::raw l[EPL], nl[EPL];
+  bool live = false, next_live = false;
+  if (t0 + wave < t1) r.request(t0 + wave, l, live);
+  for (int i = threadIdx.x; i < nb; i += 64 * W) total[i] = 0;
+  __syncthreads();
+  for (int64_t t = t0 + wave; t < t1; t += W) {
+    if (t + W < t1) r.request(t + W, nl, next_live);
     int choice;
     float weight;
-    r.token(t, reinterpret_cast<float *>(scratch + wave * nb), choice, weight);
+    r.token(t, l, live, reinterpret_cast<float *>(scratch + wave * nb), choice, weight);
     if (lane < a.top_k) {
       a.idx[t * a.top_k + lane] = choice;
       a.weights[t * a.top_k + lane] = weight;
@@ -308,6 +378,9 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
         if (ONE) mine[t * a.top_k + lane] = e;
       }
     }
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) l[i] = nl[i];
+    live = next_live;
   }
   if (!a.plan) return;
   __syncthreads();
@@ -315,100 +388,113 @@ __global__ __launch_bounds__(kThreads) void route_kernel(RouteArgs a) {
     scan_counts(total, first, nb);
     __syncthreads();
     write_head(total, first, a.experts, a.plan);
-    place_slots(0, a.tokens * a.top_k, a.experts, a.bits, first, scratch, a.order, a.place,
-                [&](int64_t s) { return mine[s]; });
+    place_slots<W>(0, a.tokens * a.top_k, a.experts, a.bits, first, scratch, a.order, a.place,
+                   [&](int64_t s) { return mine[s]; });
   } else {
-    for (int i = threadIdx.x; i < nb; i += kThreads)
-      a.counts[(int64_t)blockIdx.x * nb + i] = total[i];
+    for (int i = threadIdx.x; i < nb; i += 64 * W)
+      a.counts[(int64_t)blockIdx.x * a.count_stride + i] = total[i];
   }
 }
 
 // Counts of given choices, a block of slots a work-group.  ONE: the only
 // work-group, which also makes the plan.
-template <bool ONE>
-__global__ __launch_bounds__(kThreads) void count_kernel(RouteArgs a) {
+template <bool ONE, int W>
+__global__ __launch_bounds__(64 * W) void count_kernel(RouteArgs a) {
   extern __shared__ uint32_t lds[];
   const int nb = a.experts + 1;
   uint32_t *total = lds, *first = lds + nb, *scratch = first + nb;
-  for (int i = threadIdx.x; i < nb; i += kThreads) total[i] = 0;
+  for (int i = threadIdx.x; i < nb; i += 64 * W) total[i] = 0;
   __syncthreads();
   const int64_t slots = a.tokens * a.top_k, per = a.tokens_per_block * a.top_k;
   const int64_t s0 = blockIdx.x * per, s1 = s0 + per < slots ? s0 + per : slots;
-  for (int64_t s = s0 + threadIdx.x; s < s1; s += kThreads)
+  for (int64_t s = s0 + threadIdx.x; s < s1; s += 64 * W)
     atomicAdd(&total[slot_expert(a.idx, s, a.experts)], 1u);
   __syncthreads();
   if (ONE) {
     scan_counts(total, first, nb);
     __syncthreads();
     write_head(total, first, a.experts, a.plan);
-    place_slots(0, slots, a.experts, a.bits, first, scratch, a.order, a.place,
+    place_slots<W>(0, slots, a.experts, a.bits, first, scratch, a.order, a.place,
                 [&](int64_t s) { return slot_expert(a.idx, s, a.experts); });
   } else {
-    for (int i = threadIdx.x; i < nb; i += kThreads)
-      a.counts[(int64_t)blockIdx.x * nb + i] = total[i];
+    for (int i = threadIdx.x; i < nb; i += 64 * W)
+      a.counts[(int64_t)blockIdx.x * a.count_stride + i] = total[i];
   }
 }
 
 // Places the slots of blocks_per_group blocks a work-group.
-__global__ __launch_bounds__(kThreads) void place_kernel(RouteArgs a) {
+__global__ __launch_bounds__(64 * kMaxWaves) void place_kernel(RouteArgs a) {
+  constexpr int W = kMaxWaves, NT = 64 * W;
   extern __shared__ uint32_t lds[];
-  const int nb = a.experts + 1;
+  const int nb = a.experts + 1, vecs = a.count_stride / 4;
   uint32_t *total = lds, *first = lds + nb, *scratch = first + nb;
   uint32_t *before = scratch;   // until place_slots takes the scratch
-  for (int i = threadIdx.x; i < nb; i += kThreads) total[i] = before[i] = 0;
+  for (int i = threadIdx.x; i < nb; i += NT) total[i] = before[i] = 0;
   __syncthreads();
-  // 1024 threads as rows x experts: each adds up every rows-th block's counts
-  const int width = 1 << a.bits, rows = kThreads / width;
-  const int e = threadIdx.x & (width - 1), b0 = blockIdx.x * a.blocks_per_group;
-  if (e < nb) {
-    uint32_t all = 0, mine = 0;
+  // the threads as rows of blocks' counts, four experts each: every rows-th
+  // block's, 8 in flight
+  const int rows = NT / vecs, v = threadIdx.x % vecs, b0 = blockIdx.x * a.blocks_per_group;
+  if ((int)threadIdx.x < rows * vecs) {
+    uint32_t all[4] = {}, mine[4] = {};
 #pragma unroll 8
-    for (int b = threadIdx.x >> a.bits; b < a.blocks; b += rows) {
-      const uint32_t c = a.counts[(int64_t)b * nb + e];
-      all += c;
-      mine += b < b0 ? c : 0;
+    for (int b = threadIdx.x / vecs; b < a.blocks; b += rows) {
+      const uint4 c =
+          *reinterpret_cast<const uint4 *>(a.counts + (int64_t)b * a.count_stride + 4 * v);
+      all[0] += c.x, all[1] += c.y, all[2] += c.z, all[3] += c.w;
+      if (b < b0) mine[0] += c.x, mine[1] += c.y, mine[2] += c.z, mine[3] += c.w;
     }
-    atomicAdd(&total[e], all);
-    atomicAdd(&before[e], mine);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (4 * v + i < nb) {   // (a row's padding holds anything)
+        atomicAdd(&total[4 * v + i], all[i]);
+        atomicAdd(&before[4 * v + i], mine[i]);
+      }
   }
   __syncthreads();
   scan_counts(total, first, nb);
   __syncthreads();
   if (blockIdx.x == 0) write_head(total, first, a.experts, a.plan);
   __syncthreads();
-  for (int i = threadIdx.x; i < nb; i += kThreads) first[i] += before[i];
+  for (int i = threadIdx.x; i < nb; i += NT) first[i] += before[i];
   __syncthreads();
   const int64_t slots = a.tokens * a.top_k;
   const int64_t per = a.tokens_per_block * a.top_k * a.blocks_per_group;
   const int64_t s0 = blockIdx.x * per, s1 = s0 + per < slots ? s0 + per : slots;
-  place_slots(s0, s1, a.experts, a.bits, first, scratch, a.order, a.place,
-              [&](int64_t s) { return slot_expert(a.idx, s, a.experts); });
+  place_slots<W>(s0, s1, a.experts, a.bits, first, scratch, a.order, a.place,
+                 [&](int64_t s) { return slot_expert(a.idx, s, a.experts); });
+}
+
+unsigned lds_bytes(const RouteArgs &a, int waves, int64_t kept) {
+  return (unsigned)(4 * ((2 + waves) * (a.experts + 1) + kept));
 }
 
 template <int DT, int EPL>
-void launch_route(const RouteArgs &a, bool one, unsigned lds, hipStream_t stream) {
-  if (one)
-    route_kernel<DT, EPL, true><<<1, kThreads, lds, stream>>>(a);
+void launch_route(RouteArgs a, bool one, hipStream_t stream) {
+  const int per = a.experts / a.groups, lanes = per / EPL;
+  a.group_lanes = a.groups > 1 && per % EPL == 0 && lanes <= 16 && (lanes & (lanes - 1)) == 0 ? lanes : 0;
+  if (one && a.tokens <= 4)
+    route_kernel<DT, EPL, true, 4><<<1, 256, lds_bytes(a, 4, a.tokens * a.top_k), stream>>>(a);
+  else if (one)
+    route_kernel<DT, EPL, true, kMaxWaves>
+        <<<1, 64 * kMaxWaves, lds_bytes(a, kMaxWaves, a.tokens * a.top_k), stream>>>(a);
   else
-    route_kernel<DT, EPL, false><<<(unsigned)a.blocks, kThreads, lds, stream>>>(a);
+    route_kernel<DT, EPL, false, kMaxWaves>
+        <<<(unsigned)a.blocks, 64 * kMaxWaves, lds_bytes(a, kMaxWaves, 0), stream>>>(a);
 }
 template <int DT>
-void launch_route(const RouteArgs &a, bool one, unsigned lds, hipStream_t stream) {
-  if (a.experts <= 64) launch_route<DT, 1>(a, one, lds, stream);
-  else if (a.experts <= 128) launch_route<DT, 2>(a, one, lds, stream);
-  else if (a.experts <= 256) launch_route<DT, 4>(a, one, lds, stream);
-  else launch_route<DT, 8>(a, one, lds, stream);
-}
-
-unsigned lds_bytes(const RouteArgs &a, int64_t kept) {
-  return (unsigned)(4 * ((2 + kWaves) * (a.experts + 1) + kept));
+void launch_route(const RouteArgs &a, bool one, hipStream_t stream) {
+  if (a.experts <= 64) launch_route<DT, 1>(a, one, stream);
+  else if (a.experts <= 128) launch_route<DT, 2>(a, one, stream);
+  else if (a.experts <= 256) launch_route<DT, 4>(a, one, stream);
+  else launch_route<DT, 8>(a, one, stream);
 }
 
 // Blocks of tokens, a token or more to every wave, at most kPlanBlocks.
 void split_tokens(RouteArgs &a) {
-  a.tokens_per_block = kWaves * cdiv(a.tokens, (int64_t)kWaves * kPlanBlocks);
+  a.tokens_per_block = kMaxWaves * cdiv(a.tokens, (int64_t)kMaxWaves * kPlanBlocks);
   a.blocks = (int)cdiv(a.tokens, a.tokens_per_block);
   a.blocks_per_group = (int)cdiv(a.blocks, kPlaceGroups);
+  a.count_stride = (a.experts + 1 + 3) / 4 * 4;
   a.bits = 1;
   while ((1 << a.bits) < a.experts + 1) ++a.bits;
 }
@@ -418,37 +504,42 @@ void split_tokens(RouteArgs &a) {
 sparoa_status launch_expert_route(RouteArgs a, sparoa_dtype dt, hipStream_t stream) {
   split_tokens(a);
   // one work-group up to four tokens a wave
-  const bool one = a.tokens <= 4 * kWaves;
+  const bool one = a.tokens <= 4 * kMaxWaves;
   if (one) {
     a.blocks = 1;
     a.tokens_per_block = a.tokens;
   }
-  const unsigned lds = lds_bytes(a, one ? a.tokens * a.top_k : 0);
   switch (dt) {
-    case SPAROA_F32: launch_route<SPAROA_F32>(a, one, lds, stream); break;
-    case SPAROA_F16: launch_route<SPAROA_F16>(a, one, lds, stream); break;
-    default: launch_route<SPAROA_BF16>(a, one, lds, stream); break;
+    case SPAROA_F32: launch_route<SPAROA_F32>(a, one, stream); break;
+    case SPAROA_F16: launch_route<SPAROA_F16>(a, one, stream); break;
+    default: launch_route<SPAROA_BF16>(a, one, stream); break;
   }
   SPAROA_LAUNCH_CHECK("expert_route");
   if (one || !a.plan) return SPAROA_OK;
-  place_kernel<<<(unsigned)cdiv(a.blocks, a.blocks_per_group), kThreads, lds_bytes(a, 0),
-                 stream>>>(a);
+  place_kernel<<<(unsigned)cdiv(a.blocks, a.blocks_per_group), 64 * kMaxWaves,
+                 lds_bytes(a, kMaxWaves, 0), stream>>>(a);
   SPAROA_LAUNCH_CHECK("expert_route: plan");
   return SPAROA_OK;
 }
 
 sparoa_status launch_expert_plan(RouteArgs a, hipStream_t stream) {
   split_tokens(a);
-  if (a.tokens * a.top_k <= kOneGroupSlots) {
+  const int64_t slots = a.tokens * a.top_k;
+  if (slots <= kOneGroupSlots) {
     a.tokens_per_block = a.tokens;
-    count_kernel<true><<<1, kThreads, lds_bytes(a, 0), stream>>>(a);
+    if (slots <= 256)
+      count_kernel<true, 4><<<1, 256, lds_bytes(a, 4, 0), stream>>>(a);
+    else
+      count_kernel<true, kMaxWaves>
+          <<<1, 64 * kMaxWaves, lds_bytes(a, kMaxWaves, 0), stream>>>(a);
     SPAROA_LAUNCH_CHECK("expert_plan");
     return SPAROA_OK;
   }
-  count_kernel<false><<<(unsigned)a.blocks, kThreads, lds_bytes(a, 0), stream>>>(a);
+  count_kernel<false, kMaxWaves>
+      <<<(unsigned)a.blocks, 64 * kMaxWaves, lds_bytes(a, kMaxWaves, 0), stream>>>(a);
   SPAROA_LAUNCH_CHECK("expert_plan: counts");
-  place_kernel<<<(unsigned)cdiv(a.blocks, a.blocks_per_group), kThreads, lds_bytes(a, 0),
-                 stream>>>(a);
+  place_kernel<<<(unsigned)cdiv(a.blocks, a.blocks_per_group), 64 * kMaxWaves,
+                 lds_bytes(a, kMaxWaves, 0), stream>>>(a);
   SPAROA_LAUNCH_CHECK("expert_plan");
   return SPAROA_OK;
 }
@@ -458,7 +549,7 @@ size_t expert_plan_workspace(int64_t tokens, int64_t experts) {
   a.tokens = tokens;
   a.experts = (int)experts;
   split_tokens(a);
-  return (size_t)a.blocks * (size_t)(experts + 1) * 4;
+  return (size_t)a.blocks * (size_t)a.count_stride * 4;
 }
 
 }  // namespace sparoa

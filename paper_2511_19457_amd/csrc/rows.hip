@@ -114,7 +114,9 @@ RowsTile rows_tile_for(RowsMode mode, const RowsArgs &a, sparoa_dtype dt) {
     const int64_t t32 = cdiv(a.rows, 32) * cdiv(wide, 32), t64 = cdiv(a.rows, 64) * cdiv(wide, 64);
     if (a.rows <= 96 || t64 < (f32 ? 256 : 128)) return t32 <= 256 ? kTile32x32x8 : kTile32x32;
     if (t64 <= 384) return kTile64x64;
-    return !f32 && cdiv(a.rows, 128) * cdiv(wide, 256) >= 384 ? kTile128x256 : kTile64x128;
+    // whole rounds of one tile a CU, or nearly
+    const int64_t t256 = cdiv(a.rows, 128) * cdiv(wide, 256);
+    return !f32 && 4 * t256 >= 3 * 256 * cdiv(t256, 256) ? kTile128x256 : kTile64x128;
   }
   const int64_t used = std::min<int64_t>(a.experts, a.rows), per = a.rows / used;
   if (per <= 12) return kTile16x64;
