@@ -64,6 +64,7 @@ struct RowsArgs {
   const void *h, *b;           // h [rows][ldh], b [adapters][n][rank]
   const float *scale;          // (shrink: h = scale_a A_a x)
   int adapters, rank, ldh;
+  int pack;                    // adapters side by side in a chunk of 128 bytes
   int h_f32;                   // h is fp32 whatever the dtype
   int col_groups;              // (set by the tile launcher)
 };

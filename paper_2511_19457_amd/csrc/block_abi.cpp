@@ -298,6 +298,12 @@ sparoa_status sparoa_fc_adapted(const sparoa_fc_adapted_desc *d, sparoa_act act,
   a.n = (int)d->n, a.k = (int)d->k;
   // h is an operand of MFMA, but for the stream kernel, which adds it in fp32
   a.h_f32 = rows_tile_for(kRowsFc, a, d->dtype) == kRowsStream;
+  // adapters of up to 64 bytes of rank lie 2, 4 or 8 to a chunk (all of b
+  // below 2 GiB)
+  const int64_t size = elem_size(d->dtype), rank_bytes = d->rank * size;
+  a.pack = 1;
+  if (product_ok(d->adapters, d->n, rank_bytes) && d->adapters * d->n * rank_bytes < INT32_MAX)
+    while (a.pack < 8 && rank_bytes * 2 * a.pack <= 128) a.pack *= 2;
   RowsArgs s = a;
   s.w = lora_a, s.y = workspace;
   s.ldy = a.ldh;

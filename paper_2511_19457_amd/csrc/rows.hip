@@ -20,15 +20,21 @@ __global__ __launch_bounds__(256) void shrink_rows_kernel(RowsArgs a) {
   if (r >= a.ldy || (uint32_t)id >= (uint32_t)a.adapters) return;
   const raw *x = reinterpret_cast<const raw *>(a.x) + row * a.ldx;
   const raw *w = reinterpret_cast<const raw *>(a.w) + id * a.w_stride + (int64_t)r * a.k;
-  constexpr int V = VEC ? 16 / E::size : 1;
+  constexpr int V = VEC ? 16 / E::size : 1, U = VEC ? 8 : 4;   // pieces in flight
   float s = 0.f;
-#pragma unroll 4
-  for (int k = lane * V; k < (r < a.n ? a.k : 0); k += 64 * V) {
-    float xv[V], wv[V];
-    load_elems<DT, V>(x, k, xv);
-    load_elems<DT, V>(w, k, wv);
+  for (int k0 = lane * V; k0 < (r < a.n ? a.k : 0); k0 += 64 * V * U) {
+    float xv[U][V], wv[U][V];
 #pragma unroll
-    for (int e = 0; e < V; ++e) s = fmaf(xv[e], wv[e], s);
+    for (int u = 0; u < U; ++u) {   // (past K: the row's first piece, not added)
+      const int k = k0 + 64 * V * u < a.k ? k0 + 64 * V * u : 0;
+      load_elems<DT, V>(x, k, xv[u]);
+      load_elems<DT, V>(w, k, wv[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (k0 + 64 * V * u < a.k)
+#pragma unroll
+        for (int e = 0; e < V; ++e) s = fmaf(xv[u][e], wv[u][e], s);
   }
 #pragma unroll
   for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);

@@ -47,27 +47,55 @@ __device__ __forceinline__ u32x4 descriptor(const void *p, int64_t bytes) {
                (uint32_t)kBufDword3};
 }
 
+// The chunks of the low-rank adapters among a tile's rows, behind K's: a chunk
+// holds a.pack adapters side by side (a power of two; their ranks padded to
+// 8 / pack vectors), or one adapter takes `per` chunks.
+struct AdapterChunks {
+  int number, found, per;
+  __device__ AdapterChunks() : number(0), found(0), per(1) {}
+  template <int DT>
+  __device__ __forceinline__ void set(const RowsArgs &a, int distinct) {
+    found = distinct;
+    per = a.pack > 1 ? 1 : (a.rank * Elem<DT>::size + kRow - 1) / kRow;
+    number = (found + a.pack - 1) / a.pack * per;
+  }
+  // Vector v of chunk c: which of the tile's adapters, and the byte of its rank.
+  __device__ __forceinline__ void place(const RowsArgs &a, int c, int v, int &which,
+                                        int &at) const {
+    const int wide = 8 / a.pack;
+    which = c / per * a.pack + v / wide;
+    at = c % per * kRow + v % wide * 16;
+  }
+};
+
 // Bytes [at, at + 16) of row ch of an adapter's second matrix b [n][rank], zeros
 // past the rank and past n, to LDS at lds + 16 lane (`to` the same as a
-// pointer).  Rows that start on 16 bytes go there by themselves; others pass
-// through registers, element by element: their own waits then cover every
-// load before them, and nothing is loaded behind the adapters' chunks.
+// pointer); adapter -1: zeros.  Rows that start on 16 bytes go there by
+// themselves (pack > 1: all of b below 2 GiB); others pass through registers,
+// element by element: their own waits then cover every load before them, and
+// nothing but adapters' chunks comes behind.
 template <int DT>
 __device__ __forceinline__ void rank_piece(const RowsArgs &a, int adapter, int ch, int at,
                                            uint32_t lds, char *to) {
   using raw = typename Elem<DT>::raw;
   constexpr int S = Elem<DT>::size;
   const int bytes = a.rank * S;
-  const int64_t from = (int64_t)adapter * a.n * a.rank;
+  const bool in = adapter >= 0 && ch < a.n && at < bytes;
   if (bytes % 16 == 0) {
-    const u32x4 br = descriptor(reinterpret_cast<const raw *>(a.b) + from, (int64_t)a.n * bytes);
-    ring_load(br, lds, ch < a.n && at < bytes ? (uint32_t)ch * (uint32_t)bytes + at : kOut, 0);
+    if (a.pack > 1) {
+      const u32x4 br = descriptor(a.b, (int64_t)a.adapters * a.n * bytes);
+      ring_load(br, lds, in ? (uint32_t)(adapter * a.n + ch) * (uint32_t)bytes + at : kOut, 0);
+    } else {   // (the adapter is alike in every lane)
+      const int id = __builtin_amdgcn_readfirstlane(adapter < 0 ? 0 : adapter);
+      const u32x4 br = descriptor(reinterpret_cast<const char *>(a.b) + (int64_t)id * a.n * bytes,
+                                  (int64_t)a.n * bytes);
+      ring_load(br, lds, in ? (uint32_t)ch * (uint32_t)bytes + at : kOut, 0);
+    }
   } else {
-    const raw *row = reinterpret_cast<const raw *>(a.b) + from + (int64_t)ch * a.rank;
+    const raw *row = reinterpret_cast<const raw *>(a.b) + ((int64_t)adapter * a.n + ch) * a.rank;
     raw v[16 / S];
 #pragma unroll
-    for (int e = 0; e < 16 / S; ++e)
-      v[e] = ch < a.n && at + e * S < bytes ? row[at / S + e] : (raw)0;
+    for (int e = 0; e < 16 / S; ++e) v[e] = in && at + e * S < bytes ? row[at / S + e] : (raw)0;
     __builtin_memcpy(__builtin_assume_aligned(to + 16 * (threadIdx.x & 63), 16), v, 16);
   }
 }

@@ -44,6 +44,9 @@ __global__ __launch_bounds__(64 * NW, 2) void rows_split_kernel(RowsArgs a) {
   // ---- this lane's share of the loads: slot lane & 7 of row lane >> 3 of 8,
   // which holds the row's vector (lane & 7) ^ (row & 7)
   const int cg = (lane & 7) ^ lrow;
+  static_assert(BM <= 64, "a lane per row");
+  int member[1] = {-1};   // (adapters) row `lane`'s
+  if ((FC || SHRINK) && a.ids && lane < rows) member[0] = a.ids[row0 + lane];
   const bool gather = MODE <= kRowsUpGated;
   int slot[AV], id[AV];   // (sent for first: loads land in order)
 #pragma unroll
@@ -62,25 +65,24 @@ __global__ __launch_bounds__(64 * NW, 2) void rows_split_kernel(RowsArgs a) {
   }
   const uint32_t past = cg * 16 < kbytes - (n - 1) * kRow ? 0u : kOut;   // past K, last chunk
 
-  int extra = 0, rank_chunks = 1, items = 1;
-  if constexpr (FC || SHRINK) {
-    if (a.ids) {
+  // The adapters among the rows: (FC) chunks behind K's, (shrink) a tile each.
+  int items = 1;
+  AdapterChunks adapters;
+  auto find_adapters = [&]() __attribute__((always_inline)) {
+    if ((FC || SHRINK) && a.ids) {
       if (wave == 0) {
-        const int f = distinct_ids<(BM + 63) / 64>(a.ids + row0, rows, a.adapters, list);
+        const int f = distinct_values<1>(member, a.adapters, list);
         if (lane == 0) list_len = f;
       }
       __syncthreads();
       const int f = __builtin_amdgcn_readfirstlane(list_len);
-      if constexpr (FC) {
-        rank_chunks = (a.rank * E::size + kRow - 1) / kRow;
-        extra = f * rank_chunks;
-      } else {
-        items = f;
-      }
+      if constexpr (FC) adapters.set<DT>(a, f);
+      else items = f;
     }
-  }
-  const int chunks = n + extra;
-  const int mine = chunks > wave ? (chunks - wave + NW - 1) / NW : 0;   // this wave's chunks
+  };
+  // (FC: the first chunks, all of K, are sent for before that)
+  const bool early = FC && n >= S * NW;
+  if (!early) find_adapters();
 
   const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem +
                         wave * (S * STAGE);
@@ -102,11 +104,12 @@ __global__ __launch_bounds__(64 * NW, 2) void rows_split_kernel(RowsArgs a) {
         for (int u = 0; u < BV; ++u)
           ring_load(wr, dst + BM * kRow + u * 1024, b_off[u] | out, c * kRow);
       } else {
-        const int e = c - n, d = e / rank_chunks, r = (e - d * rank_chunks) * kRow;
-        const int adapter = __builtin_amdgcn_readfirstlane(list[d]);
+        int which, from;
+        adapters.place(a, c - n, cg, which, from);
+        const int adapter = which < adapters.found ? list[which] : -1;
 #pragma unroll
         for (int u = 0; u < BV; ++u)
-          rank_piece<DT>(a, adapter, n0 + 8 * u + lrow, r + cg * 16, dst + BM * kRow + u * 1024,
+          rank_piece<DT>(a, adapter, n0 + 8 * u + lrow, from, dst + BM * kRow + u * 1024,
                          ring_at + (dst - ring) + BM * kRow + u * 1024);
       }
     };
@@ -116,18 +119,21 @@ __global__ __launch_bounds__(64 * NW, 2) void rows_split_kernel(RowsArgs a) {
 #pragma unroll
         for (int u = 0; u < AV; ++u) ring_load(xr, dst + u * 1024, a_off[u] | out, c * kRow);
       } else {   // the rows of this adapter; the others' read as zeros
-        const int e = c - n, d = e / rank_chunks, r = (e - d * rank_chunks) * kRow;
-        const int hbytes = a.ldh * E::size, adapter = __builtin_amdgcn_readfirstlane(list[d]);
+        int which, from;
+        adapters.place(a, c - n, cg, which, from);
+        const int hbytes = a.ldh * E::size, adapter = which < adapters.found ? list[which] : -1;
         const u32x4 hr = descriptor(reinterpret_cast<const char *>(a.h) + row0 * hbytes,
                                     (int64_t)rows * hbytes);
 #pragma unroll
         for (int u = 0; u < AV; ++u) {
           const int row = 8 * u + lrow;
-          const bool in = row < rows && id[u] == adapter && r + cg * 16 < hbytes;
-          ring_load(hr, dst + u * 1024, in ? (uint32_t)(row * hbytes + r + cg * 16) : kOut, 0);
+          const bool in = row < rows && adapter >= 0 && id[u] == adapter && from < hbytes;
+          ring_load(hr, dst + u * 1024, in ? (uint32_t)(row * hbytes + from) : kOut, 0);
         }
       }
     };
+    int chunks = n + adapters.number;
+    int mine = chunks > wave ? (chunks - wave + NW - 1) / NW : 0;   // this wave's chunks
 #pragma unroll
     for (int s = 0; s < S; ++s)
       if (s < mine) load_w(wave + s * NW, ring + s * STAGE);
@@ -140,6 +146,11 @@ __global__ __launch_bounds__(64 * NW, 2) void rows_split_kernel(RowsArgs a) {
 #pragma unroll
     for (int s = 0; s < S; ++s)
       if (s < mine) load_x(wave + s * NW, ring + s * STAGE);
+    if (early) {
+      find_adapters();
+      chunks = n + adapters.number;
+      mine = (chunks - wave + NW - 1) / NW;
+    }
 
     f32x4 acc[TN][TM];
 #pragma unroll

@@ -130,7 +130,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
       }
     }
   };
-  int chunks = n, rank_chunks = 1;
+  int chunks = n;
+  AdapterChunks adapters;
 
   const uint32_t ring =
       (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem + wave * 1024;
@@ -161,21 +162,24 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
     const int lane = fresh_lane(threadIdx.x & 63), lrow = lane >> 3;
     const int cgA = vector_a(lane), cgB = vector_b(lane);
     const uint32_t xd = ring + slot * XS, wd = ring + W0 + slot * WS;
-    const int c = i - n, d = c / rank_chunks, r = (c - d * rank_chunks) * kRow;
-    const int id = __builtin_amdgcn_readfirstlane(list[d]);
     const int hbytes = a.ldh * E::size;   // (columns past the rank hold zeros)
     const u32x4 hr = descriptor(reinterpret_cast<const char *>(a.h) + row0 * hbytes,
                                 (int64_t)rows * hbytes);
+    int which, at;
+    adapters.place(a, i - n, cgA, which, at);
+    const int ida = which < adapters.found ? list[which] : -1;
 #pragma unroll
     for (int u = 0; u < AV; ++u) {
       const int row = 8 * (u * NW + wave) + lrow;
-      const bool in = row_id[FC ? u : 0] == id && r + cgA * 16 < hbytes;
-      ring_load(hr, xd + u * (NW * 1024), in ? (uint32_t)(row * hbytes + r + cgA * 16) : kOut, 0);
+      const bool in = ida >= 0 && row_id[FC ? u : 0] == ida && at < hbytes;
+      ring_load(hr, xd + u * (NW * 1024), in ? (uint32_t)(row * hbytes + at) : kOut, 0);
     }
+    adapters.place(a, i - n, cgB, which, at);
+    const int idb = which < adapters.found ? list[which] : -1;
 #pragma unroll
     for (int u = 0; u < BV; ++u)
-      rank_piece<DT>(a, id, n0 + 8 * (u * NW + wave) + lrow, r + cgB * 16,
-                     wd + u * (NW * 1024), smem + W0 + slot * WS + (wave + u * NW) * 1024);
+      rank_piece<DT>(a, idb, n0 + 8 * (u * NW + wave) + lrow, at, wd + u * (NW * 1024),
+                     smem + W0 + slot * WS + (wave + u * NW) * 1024);
   };
 
   f32x4 acc[WTM][WTN];
@@ -196,8 +200,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
     asm volatile("s_barrier" ::: "memory");   // (and every wave has read its last stage)
     if constexpr (FC) {
       if (a.ids) {
-        rank_chunks = (a.rank * E::size + kRow - 1) / kRow;
-        chunks = n + __builtin_amdgcn_readfirstlane(list_len) * rank_chunks;
+        adapters.set<DT>(a, __builtin_amdgcn_readfirstlane(list_len));
+        chunks = n + adapters.number;
       }
     }
 #pragma unroll
