@@ -100,6 +100,36 @@ __device__ __forceinline__ void rank_piece(const RowsArgs &a, int adapter, int c
   }
 }
 
+// Output (row, ch) of an adapted FC before bias and activation, by itself.  In an
+// adapter's chunk the rows of other adapters meet its matrix with zeros, and
+// zero times an infinity or NaN in that matrix is NaN: a NaN in a tile with
+// adapters is worked out again from what the row itself names.
+template <int DT>
+__device__ __forceinline__ float own_output(const RowsArgs &a, int64_t row, int ch) {
+  using E = Elem<DT>;
+  using raw = typename E::raw;
+  constexpr int V = 16 / E::size;
+  float s = 0.f;
+  const int id = a.ids[row];
+  if ((uint32_t)id < (uint32_t)a.adapters) {
+    const raw *h = reinterpret_cast<const raw *>(a.h) + row * a.ldh;
+    const raw *b = reinterpret_cast<const raw *>(a.b) + ((int64_t)id * a.n + ch) * a.rank;
+#pragma nounroll
+    for (int r = 0; r < a.rank; ++r) s = fmaf(E::to_f32(h[r]), E::to_f32(b[r]), s);
+  }
+  const raw *x = reinterpret_cast<const raw *>(a.x) + row * a.ldx;
+  const raw *w = reinterpret_cast<const raw *>(a.w) + (int64_t)ch * a.k;
+#pragma nounroll
+  for (int k = 0; k < a.k && s == s; k += V) {   // (k % V == 0; a NaN stays)
+    float xv[V], wv[V];
+    load_elems<DT, V>(x, k, xv);
+    load_elems<DT, V>(w, k, wv);
+#pragma unroll
+    for (int e = 0; e < V; ++e) s = fmaf(xv[e], wv[e], s);
+  }
+  return s;
+}
+
 // Inclusive prefix sum over the wave.
 __device__ __forceinline__ int wave_prefix(int v) {
 #define SPAROA_DPP_ADD(ctrl, rows) \

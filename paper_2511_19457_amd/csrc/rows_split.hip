@@ -210,6 +210,13 @@ __global__ __launch_bounds__(64 * NW, 2) void rows_split_kernel(RowsArgs a) {
       }
       const int r = 16 * t + rl, ch = n0 + 16 * b + 4 * q;
       if (r >= rows || ch >= (SHRINK ? a.ldy : a.n)) continue;
+      if constexpr (FC) {
+        const float sum = (v[0] + v[1]) + (v[2] + v[3]);
+        if (adapters.found && sum != sum)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (v[e] != v[e] && ch + e < a.n) v[e] = own_output<DT>(a, row0 + r, ch + e);
+      }
       const int64_t to = (row0 + r) * a.ldy + ch;
       if constexpr (SHRINK) {   // (columns past the rank, to ldy, are written as zeros)
         if (a.ids[row0 + r] != seg) continue;

@@ -355,6 +355,33 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
       }
   };
 
+  // Outputs that are NaN where the tile has adapters, worked out by themselves:
+  // one accumulator after the other takes the first one's place.
+  auto mend = [&](int n0, int64_t row0, int rows) __attribute__((always_inline)) {
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < WTM * WTN; ++i) {
+      const f32x4 v = acc[i / WTN][i % WTN];
+      sum += (v[0] + v[1]) + (v[2] + v[3]);
+    }
+    if (!__ballot(sum != sum)) return;
+    const int lane = threadIdx.x & 63, r0 = wm * WTM * 16 + (lane & 15);
+    const int c0 = n0 + wn * WTN * 16 + 8 * (lane >> 4);
+#pragma nounroll
+    for (int i = 0; i < WTM * WTN; ++i) {
+      const int b = i % WTN, r = r0 + i / WTN * 16;
+      const int c = c0 + 64 * (b >> 2) + 32 * (b >> 1 & 1) + 4 * (b & 1);
+      f32x4 v = acc[0][0];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (v[e] != v[e] && r < rows && c + e < a.n) v[e] = own_output<DT>(a, row0 + r, c + e);
+#pragma unroll
+      for (int j = 0; j + 1 < WTM * WTN; ++j)
+        acc[j / WTN][j % WTN] = acc[(j + 1) / WTN][(j + 1) % WTN];
+      acc[WTM - 1][WTN - 1] = v;
+    }
+  };
+
   // ---- tile by tile.  The next tile's first chunks are sent for before the
   // epilogue, and the rows of the tile behind it before the stores, which are
   // then the newest operations: K starts when the chunks have landed, under
@@ -379,6 +406,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
     else run(std::false_type{});
     const int seg = tl.seg, n0_ = n0, rows_ = rows;
     const int64_t row0_ = row0;
+    const int found = adapters.found;
     const bool more = nt.end != 0;
     if (more) {
       tl = nt;
@@ -387,6 +415,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
       if (nt.end) fetch(nt);
     }
     if (busy) {
+      if constexpr (FC)
+        if (found) mend(n0_, row0_, rows_);
       if (whole) finish(std::true_type{}, seg, n0_, row0_, rows_);
       else if constexpr (MODE != kRowsDown) finish(std::false_type{}, seg, n0_, row0_, rows_);
     }
