@@ -69,35 +69,38 @@ struct AdapterChunks {
 };
 
 // Bytes [at, at + 16) of row ch of an adapter's second matrix b [n][rank], zeros
-// past the rank and past n, to LDS at lds + 16 lane (`to` the same as a
-// pointer); adapter -1: zeros.  Rows that start on 16 bytes go there by
-// themselves (pack > 1: all of b below 2 GiB); others pass through registers,
-// element by element: their own waits then cover every load before them, and
-// nothing but adapters' chunks comes behind.
+// past the rank and past n, to LDS; adapter -1: zeros.  Where b's rows start on
+// 16 bytes they go there by themselves (pack > 1: all of b below 2 GiB), to
+// lds + 16 lane.
 template <int DT>
-__device__ __forceinline__ void rank_piece(const RowsArgs &a, int adapter, int ch, int at,
-                                           uint32_t lds, char *to) {
+__device__ __forceinline__ void rank_vector(const RowsArgs &a, int adapter, int ch, int at,
+                                            uint32_t lds) {
+  const int bytes = a.rank * Elem<DT>::size;
+  const bool in = adapter >= 0 && ch < a.n && at < bytes;
+  if (a.pack > 1) {
+    const u32x4 br = descriptor(a.b, (int64_t)a.adapters * a.n * bytes);
+    ring_load(br, lds, in ? (uint32_t)(adapter * a.n + ch) * (uint32_t)bytes + at : kOut, 0);
+  } else {   // (the adapter is alike in every lane)
+    const int id = __builtin_amdgcn_readfirstlane(adapter < 0 ? 0 : adapter);
+    const u32x4 br = descriptor(reinterpret_cast<const char *>(a.b) + (int64_t)id * a.n * bytes,
+                                (int64_t)a.n * bytes);
+    ring_load(br, lds, in ? (uint32_t)ch * (uint32_t)bytes + at : kOut, 0);
+  }
+}
+// Others pass through registers, element by element: their own waits then
+// cover every load before them, and nothing but adapters' chunks comes behind.
+template <int DT>
+__device__ __forceinline__ void rank_elements(const RowsArgs &a, int adapter, int ch, int at,
+                                              char *to) {
   using raw = typename Elem<DT>::raw;
   constexpr int S = Elem<DT>::size;
   const int bytes = a.rank * S;
   const bool in = adapter >= 0 && ch < a.n && at < bytes;
-  if (bytes % 16 == 0) {
-    if (a.pack > 1) {
-      const u32x4 br = descriptor(a.b, (int64_t)a.adapters * a.n * bytes);
-      ring_load(br, lds, in ? (uint32_t)(adapter * a.n + ch) * (uint32_t)bytes + at : kOut, 0);
-    } else {   // (the adapter is alike in every lane)
-      const int id = __builtin_amdgcn_readfirstlane(adapter < 0 ? 0 : adapter);
-      const u32x4 br = descriptor(reinterpret_cast<const char *>(a.b) + (int64_t)id * a.n * bytes,
-                                  (int64_t)a.n * bytes);
-      ring_load(br, lds, in ? (uint32_t)ch * (uint32_t)bytes + at : kOut, 0);
-    }
-  } else {
-    const raw *row = reinterpret_cast<const raw *>(a.b) + ((int64_t)adapter * a.n + ch) * a.rank;
-    raw v[16 / S];
+  const raw *row = reinterpret_cast<const raw *>(a.b) + ((int64_t)adapter * a.n + ch) * a.rank;
+  raw v[16 / S];
 #pragma unroll
-    for (int e = 0; e < 16 / S; ++e) v[e] = in && at + e * S < bytes ? row[at / S + e] : (raw)0;
-    __builtin_memcpy(__builtin_assume_aligned(to + 16 * (threadIdx.x & 63), 16), v, 16);
-  }
+  for (int e = 0; e < 16 / S; ++e) v[e] = in && at + e * S < bytes ? row[at / S + e] : (raw)0;
+  __builtin_memcpy(__builtin_assume_aligned(to + 16 * (threadIdx.x & 63), 16), v, 16);
 }
 
 // Output (row, ch) of an adapted FC before bias and activation, by itself.  In an

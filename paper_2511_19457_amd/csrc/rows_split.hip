@@ -107,10 +107,16 @@ __global__ __launch_bounds__(64 * NW, 2) void rows_split_kernel(RowsArgs a) {
         int which, from;
         adapters.place(a, c - n, cg, which, from);
         const int adapter = which < adapters.found ? list[which] : -1;
+        if (a.rank * E::size % 16 == 0) {
 #pragma unroll
-        for (int u = 0; u < BV; ++u)
-          rank_piece<DT>(a, adapter, n0 + 8 * u + lrow, from, dst + BM * kRow + u * 1024,
-                         ring_at + (dst - ring) + BM * kRow + u * 1024);
+          for (int u = 0; u < BV; ++u)
+            rank_vector<DT>(a, adapter, n0 + 8 * u + lrow, from, dst + BM * kRow + u * 1024);
+        } else {
+#pragma nounroll
+          for (int u = 0; u < BV; ++u)
+            rank_elements<DT>(a, adapter, n0 + 8 * u + lrow, from,
+                              ring_at + (dst - ring) + BM * kRow + u * 1024);
+        }
       }
     };
     auto load_x = [&](int c, uint32_t dst) __attribute__((always_inline)) {
