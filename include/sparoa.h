@@ -643,8 +643,9 @@ sparoa_status sparoa_expert_plan(int64_t tokens, int64_t top_k, int64_t experts,
  *   A slot whose expert is -1 is not computed and its weight not looked at; a
  *   token without experts gives residual, or 0.
  *   Products accumulate in fp32; u is rounded to dtype once (the second
- *   product's operand), the slots' down products stay fp32 and so does their
- *   weighted sum, in the order of j; y is rounded once.
+ *   product's operand).  A slot's down product stays fp32, but for bf16 experts
+ *   with many rows (about 12 or more), where it is rounded to bf16 once.  The
+ *   weighted sum is fp32, in the order of j; y is rounded once.
  *   act: NONE, RELU, RELU6, SILU or GELU.
  *   Kernels: few rows an expert stream its weights (each byte read once for
  *   up to 64 rows); many run tiles through LDS.  Only experts with a row are

@@ -75,6 +75,11 @@ enum RowsTile {
   kTile16x64, kTile32x32, kTile32x32x8,        // waves split K, 4 or 8 (rows_split.hip)
   kTile64x64, kTile64x128, kTile128x256        // waves share the tile (rows_tile.hip)
 };
+// The tile kernel writes the down products of bf16 experts in bf16, everything
+// else in fp32.  Where experts have many rows the products' way through memory
+// is what it saves (4096 tokens, 64 experts, top 8, 2048 x 1024: DOWNFIG);
+// fp16 has not the range of what is summed.
+constexpr bool down_rounded(int dtype) { return dtype == SPAROA_BF16; }
 RowsTile rows_tile_for(RowsMode mode, const RowsArgs &a, sparoa_dtype dt);
 sparoa_status launch_rows(RowsMode mode, const RowsArgs &a, sparoa_dtype dt, hipStream_t stream);
 sparoa_status launch_rows_stream(RowsMode mode, const RowsArgs &a, sparoa_dtype dt,
@@ -86,7 +91,8 @@ sparoa_status launch_rows_tile(RowsMode mode, RowsTile tile, const RowsArgs &a, 
 
 // y[t] = residual[t] + sum_j weights[t][j] z[place[t][j]]
 struct CombineArgs {
-  const float *z;              // the down products, fp32
+  const void *z;               // the down products, fp32 or (z_rounded) dtype
+  int z_rounded;
   const void *residual;
   const float *weights;
   const int32_t *place;

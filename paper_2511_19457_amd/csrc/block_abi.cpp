@@ -254,7 +254,8 @@ sparoa_status sparoa_expert_ffn(const sparoa_expert_ffn_desc *d, sparoa_act act,
   a.w_rows = (int)d->hidden, a.w_stride = d->hidden * d->inner;
   st = launch_rows(kRowsDown, a, d->dtype, stream);
   if (st != SPAROA_OK) return st;
-  const CombineArgs c{reinterpret_cast<const float *>(z), residual, weights,
+  const int rounded = down_rounded(d->dtype) && rows_tile_for(kRowsDown, a, d->dtype) >= kTile64x64;
+  const CombineArgs c{z, rounded, residual, weights,
                       plan + plan_place(d->experts, slots), y, d->tokens, d->hidden, ldz,
                       (int)d->top_k};
   return launch_combine(c, d->dtype, stream);

@@ -44,7 +44,7 @@ __global__ __launch_bounds__(256) void shrink_rows_kernel(RowsArgs a) {
   else reinterpret_cast<raw *>(a.y)[row * a.ldy + r] = E::from_f32(s);
 }
 
-template <int DT, int V>
+template <int DT, int V, int ZT>
 __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
   const int64_t per = a.hidden / V, total = a.tokens * per;
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
@@ -63,16 +63,17 @@ __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float *from = a.z + (p[j] < 0 ? 0 : p[j]) * a.ldz + c;
-        if constexpr (V % 4 == 0) {
+        const int64_t from = (p[j] < 0 ? 0 : p[j]) * a.ldz + c;
+        if constexpr (ZT == SPAROA_F32 && V == 8) {
+          f32x4 q[2];
 #pragma unroll
-          for (int e = 0; e < V; e += 4) {
-            const f32x4 q = *reinterpret_cast<const f32x4 *>(from + e);
+          for (int h = 0; h < 2; ++h)
+            q[h] = *reinterpret_cast<const f32x4 *>(reinterpret_cast<const float *>(a.z) + from +
+                                                    4 * h);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) z[j][e + i] = q[i];
-          }
+          for (int e = 0; e < V; ++e) z[j][e] = q[e / 4][e % 4];
         } else {
-          z[j][0] = from[0];
+          load_elems<ZT, V>(a.z, from, z[j]);
         }
       }
 #pragma unroll
@@ -96,10 +97,13 @@ void launch_combine_dt(const CombineArgs &a, hipStream_t stream) {
   const bool vec = a.hidden % V == 0;
   const int64_t items = a.tokens * (vec ? a.hidden / V : a.hidden);
   const unsigned grid = (unsigned)std::min<int64_t>(cdiv(items, 256), 1 << 20);
-  if (vec) combine_kernel<DT, V><<<grid, 256, 0, stream>>>(a);
-  else combine_kernel<DT, 1><<<grid, 256, 0, stream>>>(a);
+  if constexpr (down_rounded(DT)) {
+    if (a.z_rounded && vec) return combine_kernel<DT, V, DT><<<grid, 256, 0, stream>>>(a);
+    if (a.z_rounded) return combine_kernel<DT, 1, DT><<<grid, 256, 0, stream>>>(a);
+  }
+  if (vec) combine_kernel<DT, V, SPAROA_F32><<<grid, 256, 0, stream>>>(a);
+  else combine_kernel<DT, 1, SPAROA_F32><<<grid, 256, 0, stream>>>(a);
 }
-
 
 template <int DT>
 void launch_shrink_rows(const RowsArgs &a, hipStream_t stream) {

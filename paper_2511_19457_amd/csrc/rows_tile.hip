@@ -277,7 +277,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
   // 4096^3 132.8 us against 128.3, experts of 777 tokens 39 us against 36).
   // WHOLE vectors are stored unconditionally, those of no row or column at an
   // offset past the range, so the next tile's first wait knows their number.
-  constexpr int OS = MODE == kRowsDown ? 4 : E::size;   // (z is fp32)
+  constexpr int OS = MODE == kRowsDown && !down_rounded(DT) ? 4 : E::size;
   constexpr int H = GATED ? 1 : 2;                      // runs of 8 channels of a group
   constexpr int kStores = WTM * NG * H * (OS / 2);
   const bool whole = MODE == kRowsDown || (a.n % 8 == 0 && a.ldy % 8 == 0);
