@@ -121,17 +121,43 @@ RowsTile rows_tile_for(RowsMode mode, const RowsArgs &a, sparoa_dtype dt) {
   if (a.k % v || a.ldx % v) return kRowsStream;
   const int64_t wide = (int64_t)a.n * (mode == kRowsUpGated ? 2 : 1);
   if (mode == kRowsFc) {
+    // Few tiles: the waves split K, 8 of them (128 KB of rings) where every CU has
+    // one tile, 4 where it has more.  bf16 (us): 96 x 4096 x 6144 (t32 576) 28.8
+    // with 4 waves, 32.8 with 8, 22.6 in 64 x 64 tiles; 500 x 4096 x 1024 (512)
+    // 20.1 / 26.5 / 22.1; 32 x 4096 x 4096 (128) 12.0 / 11.4 / 21.0.  fp32, whose MFMAs take 16
+    // times as long: 1125 x 2208 x 424 (504) 27.9 / 31.4 / 49.6, 600 x 2048 x 2048
+    // (1216) 63.1 / 70.0 / 73.3, 2048 x 1024 x 1024 (2048) 57.8 / 68.9 / 43.5.
     const int64_t t32 = cdiv(a.rows, 32) * cdiv(wide, 32), t64 = cdiv(a.rows, 64) * cdiv(wide, 64);
-    if (a.rows <= 96 || t64 < (f32 ? 256 : 128)) return t32 <= 256 ? kTile32x32x8 : kTile32x32;
-    if (t64 <= 384) return kTile64x64;
-    // whole rounds of one tile a CU, or nearly
-    const int64_t t256 = cdiv(a.rows, 128) * cdiv(wide, 256);
-    return !f32 && 4 * t256 >= 3 * 256 * cdiv(t256, 256) ? kTile128x256 : kTile64x128;
+    if (t32 <= 256) return kTile32x32x8;
+    if (t32 <= (f32 ? 1280 : 512)) return kTile32x32;
+    // one 64 x 64 tile a CU: 1000 x 4096 x 1024 23.4 us against 28.9 in 64 x 128
+    // (300 x 4096 x 4096, 320 tiles: 34.0 / 29.4); fp32 two (2048 x 1024 x 1024
+    // 43.5 / 45.9, 4096 x 1024 x 1024 81.8 / 76.0)
+    if (t64 <= (f32 ? 512 : 256)) return kTile64x64;
+    if (f32) return kTile64x128;
+    // Rounds over the CUs, in 10 ns: one 128 x 256 tile a CU takes 0.82 us a chunk
+    // of K and 4 us besides, up to two of 64 x 128 take 0.35 each and 3.  4068 x
+    // 3208 x 2248: 107.6 us against 115.1, 3000 x 5000 x 1504 79.2 / 109.3, 2048^3
+    // 33.5 / 26.9, 600 x 4096 x 4096 51.2 / 37.8.
+    const int64_t chunks = cdiv(a.k * elem_size(dt), 128);
+    const int64_t large = cdiv(a.rows, 128) * cdiv(wide, 256);
+    const int64_t small = cdiv(a.rows, 64) * cdiv(wide, 128);
+    return cdiv(large, 256) * (82 * chunks + 400) <=
+                   cdiv(small, 256) * 35 * chunks + cdiv(small, 512) * 300
+               ? kTile128x256 : kTile64x128;
   }
+  // Experts, by their average rows (us, 16-bit unless it says fp32).  Few: bound
+  // by the weights' stream (64 experts of 2048 x 1024 gated, 4 rows each: 142
+  // against 156 in 64 x 64 tiles, 20 rows 204 / 177); fp32 products are slow
+  // enough for 64 rows (16 experts of 1024 x 1024, 50 rows: 68 / 85, 125 rows
+  // 128 / 124).  Then tiles that grow with the rows (64 experts: 50 rows 209 in
+  // 64 x 64 / 203 in 64 x 128, 125 rows 267 in 64 x 128 / 229 in 128 x 256), the
+  // largest where there is one for every other CU (16 experts of 1024 x 2048, 80
+  // rows: 46 / 59).
   const int64_t used = std::min<int64_t>(a.experts, a.rows), per = a.rows / used;
-  if (per <= 12) return kTile16x64;
+  if (per <= (f32 ? 64 : 12)) return kTile16x64;
+  if (f32) return used * cdiv(per, 64) * cdiv(wide, 128) >= 1024 ? kTile64x128 : kTile64x64;
   if (per < 48) return kTile64x64;
-  if (f32) return per >= 256 ? kTile64x128 : kTile64x64;
   return per >= 96 && used * cdiv(per, 128) * cdiv(wide, 256) >= 128 ? kTile128x256 : kTile64x128;
 }
 
