@@ -44,6 +44,8 @@ __global__ __launch_bounds__(256) void shrink_rows_kernel(RowsArgs a) {
   else reinterpret_cast<raw *>(a.y)[row * a.ldy + r] = E::from_f32(s);
 }
 
+// The weighted sum of a token's slots: a lane has V channels of a token.  Bound
+// by HBM: 32768 slots of 2048 bf16 28 us (168 MB, 6.0 TB/s), in fp32 57 us.
 template <int DT, int V, int ZT>
 __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
   const int64_t per = a.hidden / V, total = a.tokens * per;

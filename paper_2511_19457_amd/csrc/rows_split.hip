@@ -8,7 +8,9 @@
 // chunks behind K's, as in the tile kernel; their first product (shrink: h =
 // scale_a A_a x) is a tile of its own for every adapter among the rows.
 // Bound by the latency of a chain of chunks (few rows in all), or by the
-// weights' stream (experts that serve few rows each).
+// weights' stream (experts that serve few rows each).  bf16, 64 experts gated,
+// 2048 x 1024, top 8: 64 tokens 97 + 51 us for 805 MB of weights (5.4 TB/s),
+// one token 13.4 + 7.4 us for 100 MB; FC of 32 x 4096 x 4096 11.4 us.
 #include <algorithm>
 
 #include "rows_ring.h"
