@@ -42,18 +42,17 @@ __device__ __forceinline__ float row_sum(float v, float (*red)[16], int &turn) {
   return v;
 }
 
-// A row in registers: TPR threads, VPT vectors of 16 bytes each (cols a
-// multiple of a vector).  TPR = 64: a wave per row, four rows a work-group.  A
+// A row in registers: TPR threads, VPT pieces of V elements each: vectors of 16
+// bytes, or single elements where cols is no multiple of a vector.  TPR = 64: a wave per row, four rows a work-group.  A
 // work-group walks rows.  KEEP (where the registers allow it): the next row's y
 // and r are sent for before the current one is summed, and the weights, biases
 // and a gate that all rows share stay in registers from the first row on.
 // 8192 x 4096 bf16: 53.6 us (5.0 TB/s); a work-group a row, its weights read
 // again and behind the sums, 75.
-template <int DT, int TPR, int VPT, bool KEEP>
+template <int DT, int V, int TPR, int VPT, bool KEEP>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_rows_kernel(NormArgs a) {
   using E = Elem<DT>;
   using raw = typename E::raw;
-  constexpr int V = 16 / E::size;
   constexpr int RPW = TPR >= 256 ? 1 : 256 / TPR;   // rows per work-group
   __shared__ float red[2][16];
   const int t = TPR >= 256 ? threadIdx.x : threadIdx.x % TPR;
@@ -61,15 +60,14 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_rows_kernel(NormAr
   int turn = 0;
   const float inv = 1.f / (float)cols;
 
-  union Q {
-    uint4 q;
+  struct alignas(V * E::size) Q {
     raw e[V];
   };
   auto load = [&](Q (&d)[VPT], const void *p, int64_t at) __attribute__((always_inline)) {
     const raw *src = reinterpret_cast<const raw *>(p) + at;
 #pragma unroll
     for (int u = 0; u < VPT; ++u)   // (lanes past the row read its last vector, unused)
-      d[u].q = *reinterpret_cast<const uint4 *>(src + min(t + u * TPR, nv - 1) * V);
+      d[u] = *reinterpret_cast<const Q *>(src + min(t + u * TPR, nv - 1) * V);
   };
   const int64_t step = (int64_t)gridDim.x * RPW;
   int64_t row = (int64_t)blockIdx.x * RPW + (TPR >= 256 ? 0 : threadIdx.x / TPR);
@@ -145,7 +143,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_rows_kernel(NormAr
         Q o;
 #pragma unroll
         for (int e = 0; e < V; ++e) o.e[e] = E::from_f32(v[u][e]);
-        if (t + u * TPR < nv) *reinterpret_cast<uint4 *>(dst + (t + u * TPR) * V) = o.q;
+        if (t + u * TPR < nv) *reinterpret_cast<Q *>(dst + (t + u * TPR) * V) = o;
       }
     };
 
@@ -187,8 +185,76 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_rows_kernel(NormAr
   }
 }
 
-// Any row length and alignment: element by element, a work-group per row, its
-// elements read again for each statistic and computed again for the stores,
+// A row in LDS (fp32, cols * 4 bytes), any row length: for rows that are no
+// multiple of a vector and too long for single elements in registers.  A thread
+// keeps to its own columns, so only the sums need barriers.  1227 x 6811 fp16 36
+// us, element by element from memory 81; 2000 x 3001 bf16 36, in registers 27.
+constexpr int kLdsThreads = 512, kLdsCols = 16384;   // (64 KB)
+template <int DT>
+__global__ __launch_bounds__(kLdsThreads) void norm_lds_kernel(NormArgs a) {
+  using E = Elem<DT>;
+  using raw = typename E::raw;
+  extern __shared__ float v[];
+  __shared__ float red[2][16];
+  int turn = 0;
+  const int t = threadIdx.x, cols = (int)a.cols;
+  const float inv = 1.f / (float)cols;
+  const raw *gate = reinterpret_cast<const raw *>(a.gate);
+  // f(column, v[column]) of this thread's columns, several loads in flight
+  auto each = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll 8
+    for (int c = t; c < cols; c += kLdsThreads) v[c] = f(c, v[c]);
+  };
+  // v <- (v - mean) / deviation, the weights' and biases' part left to the caller
+  auto stats = [&](int kind, float &mean, float &k) __attribute__((always_inline)) {
+    mean = 0.f;
+    if (kind == SPAROA_NORM_LAYER) {
+      float s = 0.f;
+#pragma unroll 8
+      for (int c = t; c < cols; c += kLdsThreads) s += v[c];
+      mean = row_sum<kLdsThreads>(s, red, turn) * inv;
+    }
+    float s = 0.f;
+#pragma unroll 8
+    for (int c = t; c < cols; c += kLdsThreads) {
+      const float d = v[c] - mean;
+      s += d * d;
+    }
+    k = 1.f / sqrtf(row_sum<kLdsThreads>(s, red, turn) * inv + a.eps);
+  };
+  auto at = [&](const void *p, int64_t i) __attribute__((always_inline)) {
+    return E::to_f32(reinterpret_cast<const raw *>(p)[i]);
+  };
+  const bool post = a.y && a.post != SPAROA_NORM_NONE, pre = a.pre != SPAROA_NORM_NONE;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const int64_t base = row * a.cols, g0 = a.gate ? row / a.gate_rows * a.cols : 0;
+    if (a.y) each([&](int c, float) { return at(a.y, base + c); });
+    else each([&](int, float) { return 0.f; });
+    float mean, k;
+    if (post) {
+      stats(a.post, mean, k);
+      each([&](int c, float x) { return (x - mean) * k; });
+      if (a.post_w) each([&](int c, float x) { return x * at(a.post_w, c); });
+      if (a.post_b) each([&](int c, float x) { return x + at(a.post_b, c); });
+    }
+    if (a.gate) each([&](int c, float x) { return x * E::to_f32(gate[g0 + c]); });
+    if (a.r) each([&](int c, float x) { return fmaf(a.scale, at(a.r, base + c), x); });
+    raw *ro = reinterpret_cast<raw *>(a.r_out), *no = reinterpret_cast<raw *>(a.n_out);
+    if (ro)
+#pragma unroll 8
+      for (int c = t; c < cols; c += kLdsThreads) ro[base + c] = E::from_f32(v[c]);
+    if (!pre) continue;
+    stats(a.pre, mean, k);
+    each([&](int c, float x) { return (x - mean) * k; });
+    if (a.pre_w) each([&](int c, float x) { return x * at(a.pre_w, c); });
+    if (a.pre_b) each([&](int c, float x) { return x + at(a.pre_b, c); });
+#pragma unroll 8
+    for (int c = t; c < cols; c += kLdsThreads) no[base + c] = E::from_f32(v[c]);
+  }
+}
+
+// Rows longer than that: element by element, a work-group per row,
+// its elements read again for each statistic and computed again for the stores,
 // which come last (so outputs may take an input's place).
 template <int DT>
 __global__ __launch_bounds__(256) void norm_any_kernel(NormArgs a) {
@@ -251,27 +317,36 @@ __global__ __launch_bounds__(256) void norm_any_kernel(NormArgs a) {
   }
 }
 
-template <int DT, int TPR, int VPT, bool KEEP>
+template <int DT, int V, int TPR, int VPT, bool KEEP>
 void launch_rows(const NormArgs &a, hipStream_t stream) {
   constexpr int RPW = TPR >= 256 ? 1 : 256 / TPR;
   const int64_t groups = cdiv(a.rows, RPW);
   const unsigned grid = (unsigned)std::min<int64_t>(groups, kWalkers * (TPR > 256 ? 1024 / TPR : 4));
-  norm_rows_kernel<DT, TPR, VPT, KEEP><<<grid, TPR > 256 ? TPR : 256, 0, stream>>>(a);
+  norm_rows_kernel<DT, V, TPR, VPT, KEEP><<<grid, TPR > 256 ? TPR : 256, 0, stream>>>(a);
 }
 
 template <int DT>
 void launch_dt(const NormArgs &a, hipStream_t stream) {
   constexpr int V = 16 / Elem<DT>::size;
-  const int64_t nv = a.cols / V;
-  if (a.cols % V || nv > 4096)
+  const bool vec = a.cols % V == 0;
+  const int64_t nv = vec ? a.cols / V : a.cols;
+  if (nv > (vec ? 4096 : kLdsCols))
     norm_any_kernel<DT><<<(unsigned)std::min<int64_t>(a.rows, 1 << 20), 256, 0, stream>>>(a);
-  else if (nv <= 64) launch_rows<DT, 64, 1, true>(a, stream);
-  else if (nv <= 128) launch_rows<DT, 64, 2, true>(a, stream);
-  else if (nv <= 256) launch_rows<DT, 256, 1, true>(a, stream);
-  else if (nv <= 512) launch_rows<DT, 256, 2, true>(a, stream);
-  else if (nv <= 1024) launch_rows<DT, 512, 2, true>(a, stream);
-  else if (nv <= 2048) launch_rows<DT, 1024, 2, false>(a, stream);
-  else launch_rows<DT, 1024, 4, false>(a, stream);
+  else if (!vec) {
+    if (nv <= 256) launch_rows<DT, 1, 64, 4, true>(a, stream);
+    else if (nv <= 1024) launch_rows<DT, 1, 256, 4, true>(a, stream);
+    else if (nv <= 4096) launch_rows<DT, 1, 512, 8, false>(a, stream);
+    else   // (more in registers spill)
+      norm_lds_kernel<DT><<<(unsigned)std::min<int64_t>(a.rows, 1 << 20), kLdsThreads,
+                            (unsigned)(4 * nv), stream>>>(a);
+  }
+  else if (nv <= 64) launch_rows<DT, V, 64, 1, true>(a, stream);
+  else if (nv <= 128) launch_rows<DT, V, 64, 2, true>(a, stream);
+  else if (nv <= 256) launch_rows<DT, V, 256, 1, true>(a, stream);
+  else if (nv <= 512) launch_rows<DT, V, 256, 2, true>(a, stream);
+  else if (nv <= 1024) launch_rows<DT, V, 512, 2, true>(a, stream);
+  else if (nv <= 2048) launch_rows<DT, V, 1024, 2, false>(a, stream);
+  else launch_rows<DT, V, 1024, 4, false>(a, stream);
 }
 
 }  // namespace
