@@ -647,11 +647,12 @@ sparoa_status sparoa_expert_plan(int64_t tokens, int64_t top_k, int64_t experts,
  *   with many rows (about 12 or more), where it is rounded to bf16 once.  The
  *   weighted sum is fp32, in the order of j; y is rounded once.
  *   act: NONE, RELU, RELU6, SILU or GELU.
- *   Kernels: few rows an expert stream its weights (each byte read once for
- *   up to 64 rows); many run tiles through LDS.  Only experts with a row are
- *   read.
+ *   Kernels: few rows an expert stream its weights; many run tiles through
+ *   LDS.  Only experts with a row are multiplied.
  *   Workspace: sparoa_expert_ffn_workspace_size bytes (u and the down
- *   products, tokens * top_k rows); contents on entry do not matter.
+ *   products, tokens * top_k rows; where hidden or inner is no multiple of 16
+ *   bytes and the experts have many rows also x and the matrices with rows
+ *   that are); contents on entry do not matter.
  * Errors: those of the plan's sizes; INVALID_ARG for hidden or inner <= 0, null
  * x/w_up/w_down/weights/plan/y, biases that do not match has_bias, an unknown
  * act; UNSUPPORTED for misaligned pointers, x or one expert's matrix of 2 GiB
@@ -682,8 +683,9 @@ sparoa_status sparoa_expert_ffn(const sparoa_expert_ffn_desc *desc, sparoa_act a
  *   a_a x accumulates in fp32, is scaled in fp32 and kept in fp32 where the
  *   weights are streamed, else rounded to dtype once for the second product.
  *   act: NONE, RELU or RELU6.
- *   Workspace: sparoa_fc_adapted_workspace_size bytes; contents on entry do
- *   not matter.
+ *   Workspace: sparoa_fc_adapted_workspace_size bytes (a_a x; where k is no
+ *   multiple of 16 bytes and m is large also x, w and lora_a with rows that
+ *   are); contents on entry do not matter.
  * Errors: INVALID_ARG for sizes <= 0, null x/w/lora_a/lora_b/scale/
  * adapter_ids/y, bias that does not match has_bias, an unknown act or dtype;
  * UNSUPPORTED for misaligned pointers, rank > 512, rows of x or a matrix of

@@ -89,6 +89,10 @@ sparoa_status launch_rows_split(RowsMode mode, RowsTile tile, const RowsArgs &a,
 sparoa_status launch_rows_tile(RowsMode mode, RowsTile tile, const RowsArgs &a, sparoa_dtype dt,
                                hipStream_t stream);
 
+// Rows of k elements -> rows of pitch elements (a multiple of 8), zeros behind k.
+sparoa_status launch_pad_rows(const void *from, void *to, int64_t rows, int k, int pitch,
+                              sparoa_dtype dt, hipStream_t stream);
+
 // y[t] = residual[t] + sum_j weights[t][j] z[place[t][j]]
 struct CombineArgs {
   const void *z;               // the down products, fp32 or (z_rounded) dtype

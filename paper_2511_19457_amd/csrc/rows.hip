@@ -107,6 +107,26 @@ void launch_combine_dt(const CombineArgs &a, hipStream_t stream) {
   else combine_kernel<DT, 1, SPAROA_F32><<<grid, 256, 0, stream>>>(a);
 }
 
+// A work-group has `per_group` rows, a thread 8 elements of a row at a time.
+template <int DT>
+__global__ __launch_bounds__(256) void pad_rows_kernel(const void *from, void *to, int64_t rows,
+                                                       int k, int pitch, int per_group) {
+  using raw = typename Elem<DT>::raw;
+  const int64_t row0 = (int64_t)blockIdx.x * per_group;
+  const uint32_t vecs = pitch / 8;
+  const uint32_t items = (uint32_t)(rows - row0 < per_group ? rows - row0 : per_group) * vecs;
+  const raw *src = reinterpret_cast<const raw *>(from) + row0 * k;
+  raw *dst = reinterpret_cast<raw *>(to) + row0 * pitch;
+  for (uint32_t i = threadIdx.x; i < items; i += 256) {
+    const uint32_t row = i / vecs, c = (i - row * vecs) * 8;
+    raw v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      v[e] = c + e < (uint32_t)k ? src[(int64_t)row * k + c + e] : (raw)0;
+    __builtin_memcpy(__builtin_assume_aligned(dst + (int64_t)row * pitch + c, 16), v, sizeof v);
+  }
+}
+
 template <int DT>
 void launch_shrink_rows(const RowsArgs &a, hipStream_t stream) {
   constexpr int V = 16 / Elem<DT>::size;
@@ -183,6 +203,20 @@ sparoa_status launch_rows(RowsMode mode, const RowsArgs &a, sparoa_dtype dt, hip
   if (tile == kRowsStream) return launch_rows_stream(mode, a, dt, stream);
   return tile >= kTile64x64 ? launch_rows_tile(mode, tile, a, dt, stream)
                             : launch_rows_split(mode, tile, a, dt, stream);
+}
+
+sparoa_status launch_pad_rows(const void *from, void *to, int64_t rows, int k, int pitch,
+                              sparoa_dtype dt, hipStream_t stream) {
+  // (some 256 pieces a work-group, a row at least, and a grid that fits)
+  const int64_t per = std::max<int64_t>(std::max<int64_t>(1, 256 / (pitch / 8)),
+                                        cdiv(rows, 1 << 24));
+  const unsigned grid = (unsigned)cdiv(rows, per);
+  switch (elem_size(dt)) {
+    case 4: pad_rows_kernel<SPAROA_F32><<<grid, 256, 0, stream>>>(from, to, rows, k, pitch, (int)per); break;
+    default: pad_rows_kernel<SPAROA_F16><<<grid, 256, 0, stream>>>(from, to, rows, k, pitch, (int)per); break;
+  }
+  SPAROA_LAUNCH_CHECK("row products: padded rows");
+  return SPAROA_OK;
 }
 
 sparoa_status launch_combine(const CombineArgs &a, sparoa_dtype dt, hipStream_t stream) {

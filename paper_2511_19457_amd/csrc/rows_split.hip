@@ -23,7 +23,7 @@ __global__ __launch_bounds__(64 * NW, 2) void rows_split_kernel(RowsArgs a) {
   using E = Elem<DT>;
   using raw = typename E::raw;
   constexpr bool GATED = MODE == kRowsUpGated, FC = MODE == kRowsFc;
-  constexpr bool SHRINK = MODE == kRowsShrink;
+  constexpr bool SHRINK = MODE == kRowsShrink, UP = MODE <= kRowsUpGated;
   constexpr int BM = 16 * TM, BN = 16 * TN, OC = GATED ? BN / 2 : BN;
   constexpr int NB = GATED ? TN / 2 : TN;      // blocks of 16 output columns
   constexpr int AV = 2 * TM, BV = 2 * TN, L = AV + BV;   // loads of 8 rows
@@ -217,7 +217,8 @@ __global__ __launch_bounds__(64 * NW, 2) void rows_split_kernel(RowsArgs a) {
         if constexpr (GATED) u += part[((o * TN + 2 * b + 1) * TM + t) * 64 + lane];
       }
       const int r = 16 * t + rl, ch = n0 + 16 * b + 4 * q;
-      if (r >= rows || ch >= (SHRINK ? a.ldy : a.n)) continue;
+      // (u's rows end in zeros, to ldy)
+      if (r >= rows || ch >= (SHRINK || UP ? a.ldy : a.n)) continue;
       if constexpr (FC) {
         const float sum = (v[0] + v[1]) + (v[2] + v[3]);
         if (adapters.found && sum != sum)
@@ -235,7 +236,7 @@ __global__ __launch_bounds__(64 * NW, 2) void rows_split_kernel(RowsArgs a) {
         store_elems<DT, 4>(a.y, to, h);
         continue;
       }
-      const bool whole = a.n % 4 == 0 && a.ldy % 4 == 0;
+      const bool whole = UP || (a.n % 4 == 0 && a.ldy % 4 == 0);
       float g[4], m[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -258,6 +259,7 @@ __global__ __launch_bounds__(64 * NW, 2) void rows_split_kernel(RowsArgs a) {
       for (int e = 0; e < 4; ++e) {
         g[e] = FC ? apply_act(g[e], a.act) : block_act(g[e], a.act);
         if constexpr (GATED) g[e] *= m[e];
+        if constexpr (UP) g[e] = ch + e < a.n ? g[e] : 0.f;
       }
       if (whole) {
         store_elems<DT, 4>(a.y, to, g);

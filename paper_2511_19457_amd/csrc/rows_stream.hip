@@ -1,5 +1,8 @@
 // Row products whose rows start off 16 bytes (k no multiple of a 16-byte
-// vector): any size and alignment.
+// vector) and are few: any size and alignment (many rows are copied to aligned
+// ones first).  Bound by the loads' latency and the shifting: FC of 16 x 6143 x
+// 2048 bf16 38 us with its adapters' product, 21 experts of 278 x 1928 with 11
+// fp16 rows each 53 us.
 //
 // A work-group has a panel of 16 NB output columns of one segment (an
 // expert, or the one matrix of an FC) and 16 MT rows; its waves split K.  A

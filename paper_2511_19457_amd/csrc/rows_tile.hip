@@ -284,7 +284,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
   constexpr int OS = MODE == kRowsDown && !down_rounded(DT) ? 4 : E::size;
   constexpr int H = GATED ? 1 : 2;                      // runs of 8 channels of a group
   constexpr int kStores = WTM * NG * H * (OS / 2);
-  const bool whole = MODE == kRowsDown || (a.n % 8 == 0 && a.ldy % 8 == 0);
+  // (u and z have rows of whole vectors, u's ends in zeros: it may be K's end)
+  const bool whole = MODE <= kRowsDown || (a.n % 8 == 0 && a.ldy % 8 == 0);
   auto finish = [&](auto vectors, int seg, int n0, int64_t row0, int rows)
                     __attribute__((always_inline)) {
     constexpr bool WHOLE = decltype(vectors)::value;
@@ -383,6 +384,11 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
             for (int e = 0; e < 8; ++e)
               v[e] *= acc[0][4 * q + 2 + (e >> 2)][e & 3] + bu[q][e];
           }
+          if constexpr (MODE < kRowsDown) {
+            if (a.n % 8)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) v[e] = col + e < a.n ? v[e] : 0.f;
+          }
           if constexpr (OS == 4 && WHOLE) {
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
@@ -467,7 +473,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
       if constexpr (FC)
         if (found) mend(n0_, row0_, rows_);
       if (whole) finish(std::true_type{}, seg, n0_, row0_, rows_);
-      else if constexpr (MODE != kRowsDown) finish(std::false_type{}, seg, n0_, row0_, rows_);
+      else if constexpr (FC) finish(std::false_type{}, seg, n0_, row0_, rows_);
     }
     stored = busy && whole;
     if (!more) return;
