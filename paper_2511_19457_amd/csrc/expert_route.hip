@@ -473,7 +473,7 @@ unsigned lds_bytes(const RouteArgs &a, int waves, int64_t kept) {
 }
 
 template <int DT, int EPL>
-void launch_route(RouteArgs a, bool one, hipStream_t stream) {
+void launch_route(RouteArgs a, bool one, int waves, hipStream_t stream) {
   const int per = a.experts / a.groups, lanes = per / EPL;
   a.group_lanes = a.groups > 1 && per % EPL == 0 && lanes <= 16 && (lanes & (lanes - 1)) == 0 ? lanes : 0;
   if (one && a.tokens <= 4)
@@ -481,21 +481,24 @@ void launch_route(RouteArgs a, bool one, hipStream_t stream) {
   else if (one)
     route_kernel<DT, EPL, true, kMaxWaves>
         <<<1, 64 * kMaxWaves, lds_bytes(a, kMaxWaves, a.tokens * a.top_k), stream>>>(a);
+  else if (waves == 4)
+    route_kernel<DT, EPL, false, 4>
+        <<<(unsigned)a.blocks, 256, lds_bytes(a, 4, 0), stream>>>(a);
   else
     route_kernel<DT, EPL, false, kMaxWaves>
         <<<(unsigned)a.blocks, 64 * kMaxWaves, lds_bytes(a, kMaxWaves, 0), stream>>>(a);
 }
 template <int DT>
-void launch_route(const RouteArgs &a, bool one, hipStream_t stream) {
-  if (a.experts <= 64) launch_route<DT, 1>(a, one, stream);
-  else if (a.experts <= 128) launch_route<DT, 2>(a, one, stream);
-  else if (a.experts <= 256) launch_route<DT, 4>(a, one, stream);
-  else launch_route<DT, 8>(a, one, stream);
+void launch_route(const RouteArgs &a, bool one, int waves, hipStream_t stream) {
+  if (a.experts <= 64) launch_route<DT, 1>(a, one, waves, stream);
+  else if (a.experts <= 128) launch_route<DT, 2>(a, one, waves, stream);
+  else if (a.experts <= 256) launch_route<DT, 4>(a, one, waves, stream);
+  else launch_route<DT, 8>(a, one, waves, stream);
 }
 
 // Blocks of tokens, a token or more to every wave, at most kPlanBlocks.
-void split_tokens(RouteArgs &a) {
-  a.tokens_per_block = kMaxWaves * cdiv(a.tokens, (int64_t)kMaxWaves * kPlanBlocks);
+void split_tokens(RouteArgs &a, int waves) {
+  a.tokens_per_block = waves * cdiv(a.tokens, (int64_t)waves * kPlanBlocks);
   a.blocks = (int)cdiv(a.tokens, a.tokens_per_block);
   a.blocks_per_group = (int)cdiv(a.blocks, kPlaceGroups);
   a.count_stride = (a.experts + 1 + 3) / 4 * 4;
@@ -506,17 +509,23 @@ void split_tokens(RouteArgs &a) {
 }  // namespace
 
 sparoa_status launch_expert_route(RouteArgs a, sparoa_dtype dt, hipStream_t stream) {
-  split_tokens(a);
-  // one work-group up to four tokens a wave
-  const bool one = a.tokens <= 4 * kMaxWaves;
+  // Work-groups of 4 waves where that spreads a lane's long work over the CUs (64
+  // tokens over 400 experts, top 8: 21.4 us with 16 waves, 16.1 so; over 64
+  // experts 10.3 / 9.6, 1003 over 60 9.9 / 10.6).
+  const int waves = a.tokens <= (a.experts > 64 ? 4 : 1) * kPlanBlocks ? 4 : kMaxWaves;
+  split_tokens(a, waves);
+  // One work-group up to half a token, one or two a wave (us, one launch against
+  // two): 8 tokens over 400 experts 13.1 / 15.0, 16 17.8 / 15.4; 16 over 256 10.0
+  // / 11.1, 32 13.9 / 11.4; 32 over 64 10.2 / 9.6 (top 2: 7.5 / 9.7), 64 15.3 / 9.6.
+  const bool one = a.tokens <= (a.experts > 256 ? 8 : a.experts > 64 ? 16 : 32);
   if (one) {
     a.blocks = 1;
     a.tokens_per_block = a.tokens;
   }
   switch (dt) {
-    case SPAROA_F32: launch_route<SPAROA_F32>(a, one, stream); break;
-    case SPAROA_F16: launch_route<SPAROA_F16>(a, one, stream); break;
-    default: launch_route<SPAROA_BF16>(a, one, stream); break;
+    case SPAROA_F32: launch_route<SPAROA_F32>(a, one, waves, stream); break;
+    case SPAROA_F16: launch_route<SPAROA_F16>(a, one, waves, stream); break;
+    default: launch_route<SPAROA_BF16>(a, one, waves, stream); break;
   }
   SPAROA_LAUNCH_CHECK("expert_route");
   if (one || !a.plan) return SPAROA_OK;
@@ -527,7 +536,7 @@ sparoa_status launch_expert_route(RouteArgs a, sparoa_dtype dt, hipStream_t stre
 }
 
 sparoa_status launch_expert_plan(RouteArgs a, hipStream_t stream) {
-  split_tokens(a);
+  split_tokens(a, kMaxWaves);
   const int64_t slots = a.tokens * a.top_k;
   if (slots <= kOneGroupSlots) {
     a.tokens_per_block = a.tokens;
@@ -552,7 +561,7 @@ size_t expert_plan_workspace(int64_t tokens, int64_t experts) {
   RouteArgs a{};
   a.tokens = tokens;
   a.experts = (int)experts;
-  split_tokens(a);
+  split_tokens(a, 4);   // (16 waves give as many blocks, or fewer)
   return (size_t)a.blocks * (size_t)a.count_stride * 4;
 }
 
