@@ -137,10 +137,20 @@ void launch_shrink_rows(const RowsArgs &a, hipStream_t stream) {
 
 }  // namespace
 
+// 128 x 256 or 64 x 128 tiles (16-bit), by their rounds over the CUs in 10 ns: one
+// large tile a CU takes 0.82 us a chunk of K and `besides` us more, up to two
+// small ones 0.35 each and 3.
+static RowsTile large_or_small(int64_t large, int64_t small, int64_t chunks, int besides) {
+  return cdiv(large, 256) * (82 * chunks + 100 * besides) <=
+                 cdiv(small, 256) * 35 * chunks + cdiv(small, 512) * 300
+             ? kTile128x256 : kTile64x128;
+}
+
 RowsTile rows_tile_for(RowsMode mode, const RowsArgs &a, sparoa_dtype dt) {
   const int v = 16 / (int)elem_size(dt);
   const bool f32 = dt == SPAROA_F32;
   if (a.k % v || a.ldx % v) return kRowsStream;
+  const int64_t chunks = cdiv(a.k * elem_size(dt), 128);
   const int64_t wide = (int64_t)a.n * (mode == kRowsUpGated ? 2 : 1);
   if (mode == kRowsFc) {
     // Few tiles: the waves split K, 8 of them (128 KB of rings) where every CU has
@@ -157,30 +167,25 @@ RowsTile rows_tile_for(RowsMode mode, const RowsArgs &a, sparoa_dtype dt) {
     // 43.5 / 45.9, 4096 x 1024 x 1024 81.8 / 76.0)
     if (t64 <= (f32 ? 512 : 256)) return kTile64x64;
     if (f32) return kTile64x128;
-    // Rounds over the CUs, in 10 ns: one 128 x 256 tile a CU takes 0.82 us a chunk
-    // of K and 4 us besides, up to two of 64 x 128 take 0.35 each and 3.  4068 x
-    // 3208 x 2248: 107.6 us against 115.1, 3000 x 5000 x 1504 79.2 / 109.3, 2048^3
-    // 33.5 / 26.9, 600 x 4096 x 4096 51.2 / 37.8.
-    const int64_t chunks = cdiv(a.k * elem_size(dt), 128);
-    const int64_t large = cdiv(a.rows, 128) * cdiv(wide, 256);
-    const int64_t small = cdiv(a.rows, 64) * cdiv(wide, 128);
-    return cdiv(large, 256) * (82 * chunks + 400) <=
-                   cdiv(small, 256) * 35 * chunks + cdiv(small, 512) * 300
-               ? kTile128x256 : kTile64x128;
+    // 4068 x 3208 x 2248: 107.6 us in 128 x 256 against 115.1 in 64 x 128, 3000 x
+    // 5000 x 1504 79.2 / 109.3, 2048^3 33.5 / 26.9, 600 x 4096 x 4096 51.2 / 37.8.
+    return large_or_small(cdiv(a.rows, 128) * cdiv(wide, 256), cdiv(a.rows, 64) * cdiv(wide, 128),
+                          chunks, 4);
   }
   // Experts, by their average rows (us, 16-bit unless it says fp32).  Few: bound
   // by the weights' stream (64 experts of 2048 x 1024 gated, 4 rows each: 142
   // against 156 in 64 x 64 tiles, 20 rows 204 / 177); fp32 products are slow
   // enough for 64 rows (16 experts of 1024 x 1024, 50 rows: 68 / 85, 125 rows
-  // 128 / 124).  Then tiles that grow with the rows (64 experts: 50 rows 209 in
-  // 64 x 64 / 203 in 64 x 128, 125 rows 267 in 64 x 128 / 229 in 128 x 256), the
-  // largest where there is one for every other CU (16 experts of 1024 x 2048, 80
-  // rows: 46 / 59).
+  // 128 / 124).  Then tiles that grow with the rows (64 experts, 50 rows: 209 in
+  // 64 x 64 / 203 in 64 x 128; 80 rows 230 in 64 x 128 / 213 in 128 x 256; 16
+  // experts of 1024 x 2048, 80 rows: 46 / 59; 81 of 264 x 384 gated, 225 rows,
+  // short K: 55 / 61).
   const int64_t used = std::min<int64_t>(a.experts, a.rows), per = a.rows / used;
   if (per <= (f32 ? 64 : 12)) return kTile16x64;
   if (f32) return used * cdiv(per, 64) * cdiv(wide, 128) >= 1024 ? kTile64x128 : kTile64x64;
   if (per < 48) return kTile64x64;
-  return per >= 96 && used * cdiv(per, 128) * cdiv(wide, 256) >= 128 ? kTile128x256 : kTile64x128;
+  return large_or_small(used * cdiv(per, 128) * cdiv(wide, 256),
+                        used * cdiv(per, 64) * cdiv(wide, 128), chunks, 10);
 }
 
 sparoa_status launch_rows(RowsMode mode, const RowsArgs &a, sparoa_dtype dt, hipStream_t stream) {
@@ -212,8 +217,12 @@ sparoa_status launch_pad_rows(const void *from, void *to, int64_t rows, int k, i
                                         cdiv(rows, 1 << 24));
   const unsigned grid = (unsigned)cdiv(rows, per);
   switch (elem_size(dt)) {
-    case 4: pad_rows_kernel<SPAROA_F32><<<grid, 256, 0, stream>>>(from, to, rows, k, pitch, (int)per); break;
-    default: pad_rows_kernel<SPAROA_F16><<<grid, 256, 0, stream>>>(from, to, rows, k, pitch, (int)per); break;
+    case 4:
+      pad_rows_kernel<SPAROA_F32><<<grid, 256, 0, stream>>>(from, to, rows, k, pitch, (int)per);
+      break;
+    default:   // (bits, whichever 16-bit type)
+      pad_rows_kernel<SPAROA_F16><<<grid, 256, 0, stream>>>(from, to, rows, k, pitch, (int)per);
+      break;
   }
   SPAROA_LAUNCH_CHECK("row products: padded rows");
   return SPAROA_OK;
