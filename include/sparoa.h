@@ -644,8 +644,9 @@ sparoa_status sparoa_expert_plan(int64_t tokens, int64_t top_k, int64_t experts,
  *   token without experts gives residual, or 0.
  *   Products accumulate in fp32; u is rounded to dtype once (the second
  *   product's operand).  A slot's down product stays fp32, but for bf16 experts
- *   with many rows (about 12 or more), where it is rounded to bf16 once.  The
- *   weighted sum is fp32, in the order of j; y is rounded once.
+ *   with many rows (more than 12) and top_k > 1, where it is rounded once to 9
+ *   bits behind the point (8 channels share an exponent).  The weighted sum is fp32, in the
+ *   order of j; y is rounded once.
  *   act: NONE, RELU, RELU6, SILU or GELU.
  *   Kernels: few rows an expert stream its weights; many run tiles through
  *   LDS.  Only experts with a row are multiplied.

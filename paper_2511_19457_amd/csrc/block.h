@@ -68,18 +68,13 @@ struct RowsArgs {
   int h_f32;                   // h is fp32 whatever the dtype
   int col_groups;              // (set by the tile launcher)
 };
-enum RowsMode { kRowsUp, kRowsUpGated, kRowsDown, kRowsFc, kRowsShrink };
+enum RowsMode { kRowsUp, kRowsUpGated, kRowsDownScaled, kRowsDown, kRowsFc, kRowsShrink };
 // Kernel and tile (rows x weight rows) of a product (rows.hip).
 enum RowsTile {
   kRowsStream,       // rows of x or w that start off 16 bytes (rows_stream.hip)
   kTile16x64, kTile32x32, kTile32x32x8,        // 4 waves split K, or 8 (rows_split.hip)
   kTile64x64, kTile64x128, kTile128x256        // waves share the tile (rows_tile.hip)
 };
-// The tile kernel writes the down products of bf16 experts in bf16, everything
-// else in fp32.  Where experts have many rows the products' way through memory
-// is what it saves (4096 tokens, 64 experts, top 8, 2048 x 1024: a pass 582 -> 542 us);
-// fp16 has not the range of what is summed.
-constexpr bool down_rounded(int dtype) { return dtype == SPAROA_BF16; }
 RowsTile rows_tile_for(RowsMode mode, const RowsArgs &a, sparoa_dtype dt);
 sparoa_status launch_rows(RowsMode mode, const RowsArgs &a, sparoa_dtype dt, hipStream_t stream);
 sparoa_status launch_rows_stream(RowsMode mode, const RowsArgs &a, sparoa_dtype dt,
@@ -95,8 +90,8 @@ sparoa_status launch_pad_rows(const void *from, void *to, int64_t rows, int k, i
 
 // y[t] = residual[t] + sum_j weights[t][j] z[place[t][j]]
 struct CombineArgs {
-  const void *z;               // the down products, fp32 or (z_rounded) dtype
-  int z_rounded;
+  const void *z;               // the down products, fp32 or scaled (kRowsDownScaled)
+  int z_scaled;
   const void *residual;
   const float *weights;
   const int32_t *place;

@@ -84,6 +84,38 @@ __device__ __forceinline__ u32x4 pack8(const float (&v)[8]) {
   return w;
 }
 
+// Eight numbers in 16 bytes: fp16 multiples of 2^(code - 127), the largest of them
+// in [1, 4), the last bit of each one a bit of the code (so 9 bits behind the
+// point, rounded).  A block with an infinity or NaN keeps it and has code 0: plain
+// fp16.
+__device__ __forceinline__ u32x4 pack_scaled8(const float (&v)[8]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+  const uint32_t top = m >> 23, code = top == 255 ? 0u : min(max(top, 1u), 253u);
+  const float scale = __uint_as_float(code ? (254 - code) << 23 : 0x3F800000u);
+  const uint32_t half = code ? 0x00010001u : 0u, spread = code | code << 15;
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t p = Elem<SPAROA_F16>::pack2(v[2 * i] * scale, v[2 * i + 1] * scale) + half;
+    w[i] = (p & 0xFFFEFFFEu) | (spread >> (2 * i) & 0x00010001u);
+  }
+  return w;
+}
+__device__ __forceinline__ void unpack_scaled8(u32x4 w, float (&v)[8]) {
+  uint32_t s = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s |= (w[i] & 0x00010001u) << (2 * i);
+  const uint32_t code = (s | s >> 15) & 255u;
+  const float scale = __uint_as_float(code ? code << 23 : 0x3F800000u);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t h = (e & 1 ? w[e / 2] >> 16 : w[e / 2]) & 0xFFFEu;
+    v[e] = Elem<SPAROA_F16>::to_f32((uint16_t)h) * scale;
+  }
+}
+
 // The distinct values in [0, limit) among id[b] of every lane, in order, to LDS
 // list; the whole wave.  Returns their number.
 template <int BATCHES>

@@ -45,8 +45,8 @@ __global__ __launch_bounds__(256) void shrink_rows_kernel(RowsArgs a) {
 }
 
 // The weighted sum of a token's slots: a lane has V channels of a token.  Bound
-// by HBM: 32768 slots of 2048 bf16 28 us (168 MB, 6.0 TB/s), in fp32 57 us.
-template <int DT, int V, int ZT>
+// by HBM: 32768 slots of 2048 in fp32 57 us (302 MB, 5.3 TB/s).
+template <int DT, int V>
 __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
   const int64_t per = a.hidden / V, total = a.tokens * per;
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
@@ -66,7 +66,7 @@ __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const int64_t from = (p[j] < 0 ? 0 : p[j]) * a.ldz + c;
-        if constexpr (ZT == SPAROA_F32 && V == 8) {
+        if constexpr (V == 8) {
           f32x4 q[2];
 #pragma unroll
           for (int h = 0; h < 2; ++h)
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
 #pragma unroll
           for (int e = 0; e < V; ++e) z[j][e] = q[e / 4][e % 4];
         } else {
-          load_elems<ZT, V>(a.z, from, z[j]);
+          load_elems<SPAROA_F32, V>(a.z, from, z[j]);
         }
       }
 #pragma unroll
@@ -93,18 +93,72 @@ __global__ __launch_bounds__(256) void combine_kernel(CombineArgs a) {
   }
 }
 
+// The same of scaled products: a lane has 8 channels, the last of a row fewer.  28
+// us (168 MB, 6.0 TB/s).
+template <int DT>
+__global__ __launch_bounds__(256) void combine_scaled_kernel(CombineArgs a) {
+  using E = Elem<DT>;
+  using raw = typename E::raw;
+  const int64_t per = a.ldz / 8, total = a.tokens * per;
+  const u32x4 *zs = reinterpret_cast<const u32x4 *>(a.z);
+  const bool whole = a.hidden % 8 == 0;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
+    const int64_t t = i / per, v = i - t * per;
+    float s[8] = {};
+    for (int j0 = 0; j0 < a.top_k; j0 += 8) {   // eight rows in flight
+      int p[8];
+      float w[8];
+      u32x4 z[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int64_t slot = t * a.top_k + (j0 + j < a.top_k ? j0 + j : 0);
+        p[j] = j0 + j < a.top_k ? a.place[slot] : -1;
+        w[j] = a.weights[slot];
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) z[j] = zs[(p[j] < 0 ? 0 : p[j]) * per + v];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {   // no expert: neither weight nor row is looked at
+        float x[8];
+        unpack_scaled8(z[j], x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] = p[j] < 0 ? s[e] : fmaf(w[j], x[e], s[e]);
+      }
+    }
+    const int64_t at = t * a.hidden + 8 * v;
+    if (whole) {
+      if (a.residual) {
+        float r[8];
+        load_elems<DT, 8>(a.residual, at, r);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[e] += r[e];
+      }
+      store_elems<DT, 8>(a.y, at, s);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (8 * v + e < a.hidden) {
+          if (a.residual) s[e] += E::to_f32(reinterpret_cast<const raw *>(a.residual)[at + e]);
+          reinterpret_cast<raw *>(a.y)[at + e] = E::from_f32(s[e]);
+        }
+    }
+  }
+}
+
 template <int DT>
 void launch_combine_dt(const CombineArgs &a, hipStream_t stream) {
   constexpr int V = 16 / Elem<DT>::size;
   const bool vec = a.hidden % V == 0;
   const int64_t items = a.tokens * (vec ? a.hidden / V : a.hidden);
   const unsigned grid = (unsigned)std::min<int64_t>(cdiv(items, 256), 1 << 20);
-  if constexpr (down_rounded(DT)) {
-    if (a.z_rounded && vec) return combine_kernel<DT, V, DT><<<grid, 256, 0, stream>>>(a);
-    if (a.z_rounded) return combine_kernel<DT, 1, DT><<<grid, 256, 0, stream>>>(a);
-  }
-  if (vec) combine_kernel<DT, V, SPAROA_F32><<<grid, 256, 0, stream>>>(a);
-  else combine_kernel<DT, 1, SPAROA_F32><<<grid, 256, 0, stream>>>(a);
+  if constexpr (DT == SPAROA_BF16)
+    if (a.z_scaled) {
+      const unsigned groups =
+          (unsigned)std::min<int64_t>(cdiv(a.tokens * (a.ldz / 8), 256), 1 << 20);
+      return combine_scaled_kernel<DT><<<groups, 256, 0, stream>>>(a);
+    }
+  if (vec) combine_kernel<DT, V><<<grid, 256, 0, stream>>>(a);
+  else combine_kernel<DT, 1><<<grid, 256, 0, stream>>>(a);
 }
 
 // A work-group has `per_group` rows, a thread 8 elements of a row at a time.
@@ -205,6 +259,8 @@ sparoa_status launch_rows(RowsMode mode, const RowsArgs &a, sparoa_dtype dt, hip
                    : launch_rows_split(mode, kTile16x64, a, dt, stream);
   }
   const RowsTile tile = rows_tile_for(mode, a, dt);
+  if (mode == kRowsDownScaled && tile < kTile64x64)
+    return fail(SPAROA_ERR_UNSUPPORTED, "row products: scaled outputs of few rows");
   if (tile == kRowsStream) return launch_rows_stream(mode, a, dt, stream);
   return tile >= kTile64x64 ? launch_rows_tile(mode, tile, a, dt, stream)
                             : launch_rows_split(mode, tile, a, dt, stream);

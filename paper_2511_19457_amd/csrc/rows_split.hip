@@ -303,6 +303,7 @@ void launch_dt(RowsMode mode, RowsTile tile, const RowsArgs &a, hipStream_t stre
   switch (mode) {
     case kRowsUp: return launch_mode<DT, kRowsUp>(tile, a, stream);
     case kRowsUpGated: return launch_mode<DT, kRowsUpGated>(tile, a, stream);
+    case kRowsDownScaled: return;   // (tile kernel only)
     case kRowsDown: return launch_mode<DT, kRowsDown>(tile, a, stream);
     case kRowsFc: return launch_mode<DT, kRowsFc>(tile, a, stream);
     case kRowsShrink: return launch_shrink<DT>(a, stream);

@@ -323,6 +323,7 @@ void launch_dt(RowsMode mode, const RowsArgs &a, hipStream_t stream) {
   switch (mode) {
     case kRowsUp: return launch_mode<DT, kRowsUp>(a, stream);
     case kRowsUpGated: return launch_mode<DT, kRowsUpGated>(a, stream);
+    case kRowsDownScaled: return;   // (tile kernel only)
     case kRowsDown: return launch_mode<DT, kRowsDown>(a, stream);
     case kRowsFc: return launch_mode<DT, kRowsFc>(a, stream);
     case kRowsShrink: return launch_mode<DT, kRowsShrink>(a, stream);

@@ -281,7 +281,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
   // 4096^3 132.8 us against 128.3, experts of 777 tokens 39 us against 36).
   // WHOLE vectors are stored unconditionally, those of no row or column at an
   // offset past the range, so the next tile's first wait knows their number.
-  constexpr int OS = MODE == kRowsDown && !down_rounded(DT) ? 4 : E::size;
+  constexpr bool SCALED = MODE == kRowsDownScaled;
+  constexpr int OS = MODE == kRowsDown ? 4 : E::size;
   constexpr int H = GATED ? 1 : 2;                      // runs of 8 channels of a group
   constexpr int kStores = WTM * NG * H * (OS / 2);
   // (u and z have rows of whole vectors, u's ends in zeros: it may be K's end)
@@ -355,7 +356,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
 #pragma unroll
           for (int i = 0; i < NG * H * 8; ++i)
             o[i / (8 * H)][i / 8 % H][i % 8] = apply_act(o[i / (8 * H)][i / 8 % H][i % 8], a.act);
-      } else if constexpr (MODE != kRowsDown) {
+      } else if constexpr (MODE <= kRowsUpGated) {
         // (a branch for all of the values, not one for each)
         auto all = [&](auto act) __attribute__((always_inline)) {
 #pragma unroll
@@ -384,7 +385,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
             for (int e = 0; e < 8; ++e)
               v[e] *= acc[0][4 * q + 2 + (e >> 2)][e & 3] + bu[q][e];
           }
-          if constexpr (MODE < kRowsDown) {
+          if constexpr (MODE <= kRowsDown) {
             if (a.n % 8)
 #pragma unroll
               for (int e = 0; e < 8; ++e) v[e] = col + e < a.n ? v[e] : 0.f;
@@ -397,7 +398,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
                                                      in ? at * 4 + 16 * p : kOut, 0, 0);
             }
           } else if constexpr (WHOLE) {
-            __builtin_amdgcn_raw_buffer_store_b128(pack8<DT>(v), yr, in ? at * 2 : kOut, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b128(SCALED ? pack_scaled8(v) : pack8<DT>(v), yr,
+                                                   in ? at * 2 : kOut, 0, 0);
           } else {
             raw *y = reinterpret_cast<raw *>(a.y) + y0;
 #pragma unroll
@@ -512,6 +514,9 @@ sparoa_status launch_dt(RowsMode mode, RowsTile tile, const RowsArgs &a, hipStre
   switch (mode) {
     case kRowsUp: return launch_mode<DT, kRowsUp>(tile, a, stream);
     case kRowsUpGated: return launch_mode<DT, kRowsUpGated>(tile, a, stream);
+    case kRowsDownScaled:
+      if constexpr (DT == SPAROA_BF16) return launch_mode<DT, kRowsDownScaled>(tile, a, stream);
+      return fail(SPAROA_ERR_UNSUPPORTED, "row products: scaled outputs are for bf16");
     case kRowsDown: return launch_mode<DT, kRowsDown>(tile, a, stream);
     default: return launch_mode<DT, kRowsFc>(tile, a, stream);
   }
