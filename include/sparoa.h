@@ -681,6 +681,8 @@ sparoa_status sparoa_expert_ffn(const sparoa_expert_ffn_desc *desc, sparoa_act a
  *   [adapters], adapter_ids int32 [m].  Rows of one adapter need not be
  *   consecutive (they cost least when they are).  Adapters of smaller rank
  *   are padded with zero rows of lora_a.
+ *   An infinity or NaN in a row of x or in an adapter stays with the rows it is
+ *   of.
  *   a_a x accumulates in fp32, is scaled in fp32 and kept in fp32 where the
  *   weights are streamed, else rounded to dtype once for the second product.
  *   act: NONE, RELU or RELU6.

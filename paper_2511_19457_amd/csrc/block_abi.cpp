@@ -84,9 +84,11 @@ sparoa_status check_ffn(const sparoa_expert_ffn_desc *d) {
     return fail(SPAROA_ERR_INVALID_ARG, "expert_ffn: sizes must be > 0");
   const int64_t size = elem_size(d->dtype);
   // (a tile's rows of u and of the fp32 down products are addressed with 31 bits)
-  if (!below_2gib(256, d->inner, 4) || !below_2gib(256, d->hidden, 4) || !below_2gib(d->tokens, d->hidden, size) ||
+  if (!below_2gib(256, d->inner, 4) || !below_2gib(256, d->hidden, 4) ||
+      !below_2gib(d->tokens, d->hidden, size) ||
       !below_2gib(d->inner * (d->gated ? 2 : 1), d->hidden, size))
-    return fail(SPAROA_ERR_UNSUPPORTED, "expert_ffn: x or an expert's matrix of 2 GiB or more, or rows too long");
+    return fail(SPAROA_ERR_UNSUPPORTED,
+                "expert_ffn: x or an expert's matrix of 2 GiB or more, or rows too long");
   if (!product_ok(d->tokens * d->top_k, round8(d->inner) + round8(d->hidden), 4) ||
       !product_ok(d->experts, 2 * d->inner * size, d->hidden))
     return fail(SPAROA_ERR_INVALID_ARG, "expert_ffn: sizes too large");

@@ -128,7 +128,8 @@ __global__ __launch_bounds__(kNT, 2) void rows_stream_kernel(RowsArgs a) {
 
   // experts: the blockIdx.y-th that has rows, its rows tile by tile; else
   // tiles of rows, every gridDim.y-th
-  const int64_t groups = EXPERTS ? uniform_word(a.plan + a.experts + 1) : (a.rows + 16 * MT - 1) / (16 * MT);
+  const int64_t groups = EXPERTS ? uniform_word(a.plan + a.experts + 1)
+                                 : (a.rows + 16 * MT - 1) / (16 * MT);
   for (int64_t group = blockIdx.y; group < groups; group += gridDim.y) {
     int64_t s0, s1;
     int seg = 0, items = 1;
@@ -252,10 +253,8 @@ __global__ __launch_bounds__(kNT, 2) void rows_stream_kernel(RowsArgs a) {
           if constexpr (MODE == kRowsShrink) {
             if (a.ids[p] != seg) continue;
             v *= a.scale[seg];
-            for (int e = 0; e < 4 && ch + e < a.n; ++e) {
-              if (a.h_f32) reinterpret_cast<float *>(a.y)[p * a.ldy + ch + e] = v[e];
-              else reinterpret_cast<typename E::raw *>(a.y)[p * a.ldy + ch + e] = E::from_f32(v[e]);
-            }
+            for (int e = 0; e < 4 && ch + e < a.n; ++e)   // (h is fp32 here)
+              reinterpret_cast<float *>(a.y)[p * a.ldy + ch + e] = v[e];
             continue;
           }
           if constexpr (MODE == kRowsDown) {   // fp32: what the weighted sum adds up

@@ -14,7 +14,7 @@
 // Bound by the matrix pipe and what feeds it: FC of 4096^3 bf16 128 us (1.07
 // PFLOP/s; 100 us with K's loads left out, 64 us at the pipe's rate), the MFMAs
 // busy half of the cycles; 4096 tokens over 64 experts (2048 x 1024 gated, top
-// 8) 295 us up, 175 us down.
+// 8) 295 us up, 179 us down.
 // Work-groups are dealt round-robin to the 8 XCDs: XCD i takes the i-th run of
 // tiles, column tiles innermost, so the tiles of one expert share an L2.
 #include <algorithm>
