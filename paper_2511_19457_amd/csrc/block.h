@@ -42,7 +42,7 @@ sparoa_status launch_expert_plan(RouteArgs a, hipStream_t stream);
 size_t expert_plan_workspace(int64_t tokens, int64_t experts);
 
 // Products of gathered or consecutive rows with the weights of their segment
-// (rows_gemm.hip): y[p] = epilogue(W_s x[p]), rows p of segment s.
+// (rows*.hip): y[p] = epilogue(W_s x[p]), rows p of segment s.
 //   experts: segments are the plan's experts, weights w + s * w_stride;
 //            up: x rows gathered through order; down: consecutive.
 //   fc:      one segment of `rows` consecutive rows, low-rank adapters.
