@@ -1,0 +1,85 @@
+"""What the experts' products promise of their roundings (sparoa_expert_ffn).
+
+u is made exact here (each row of w_up copies one feature of x, no activation),
+so that a down product's error is its fp32 sum's and its own rounding's.  The
+residual is minus the exact output rounded to the dtype: what is left over is
+some 2^-8 of the output, and its last rounding hides nothing.
+
+Tolerance of a down product z, its terms' absolute sum s: fp32 sums 1e-5 s (the
+framework's bound), 2^-10 |z| where it goes to the weighted sum as 9 bits behind
+the point (bf16, many rows, top_k > 1).  The weighted sum and the residual add 1e-5
+of their terms, the result one rounding of what is left."""
+import numpy as np
+import pytest
+import torch
+
+import synth
+from tests import test_gpu_expert_ffn as ffn
+
+pytestmark = pytest.mark.gpu
+
+DT, U, TINY, SUM = ffn.DT, ffn.U, ffn.TINY, ffn.SUM
+
+
+def call(x, w_up, w_down, idx, weights, residual=None, act="none", gated=False):
+    from paper_2511_19457_amd import abi
+    dev = torch.device("cuda")
+    t, k, e = x.shape[0], idx.shape[1], w_up.shape[0]
+    d = abi.expert_ffn_desc(t, k, e, x.shape[1], w_down.shape[2], x.dtype, gated=gated)
+    plan = torch.empty(abi.sparoa_expert_plan_words(t, k, e), dtype=torch.int32, device=dev)
+    abi.sparoa_expert_plan(t, k, e, torch.from_numpy(idx).to(dev), plan, torch.empty(
+        abi.sparoa_expert_plan_workspace_size(t, k, e), dtype=torch.uint8, device=dev))
+    ws = torch.full((abi.sparoa_expert_ffn_workspace_size(d),), 255, dtype=torch.uint8, device=dev)
+    y = torch.full_like(x, float("nan"), device=dev)
+    abi.sparoa_expert_ffn(d, getattr(abi, "ACT_" + act.upper()), x.to(dev), w_up.to(dev), None,
+                          w_down.to(dev), None, torch.from_numpy(weights).to(dev), plan,
+                          None if residual is None else residual.to(dev), y, ws)
+    return y.double().cpu().numpy()
+
+
+def copies(e, inner, hidden, dt, seed):
+    """w_up [e, inner, hidden] whose rows pick one feature each, and which."""
+    pick = np.random.default_rng(seed).integers(0, hidden, (e, inner))
+    w = torch.zeros(e, inner, hidden, dtype=DT[dt])
+    w.scatter_(2, torch.from_numpy(pick)[:, :, None], 1.0)
+    return w, pick
+
+
+def left_over(t, e, k, hidden, inner, dt, seed, scaled=False, channels=None):
+    """(what the call leaves, what it should, its bound, the exact output)."""
+    x = synth.normal((t, hidden), dt, 9970 + seed)
+    w_up, pick = copies(e, inner, hidden, dt, seed)
+    w_down = synth.normal((e, hidden, inner), "f32", 9980 + seed, std=inner ** -0.5)
+    if channels is not None:
+        w_down *= channels[:, None]
+    w_down = w_down.to(DT[dt])
+    idx = ffn.choices(t, k, e, "even", seed)
+    weights = (np.random.default_rng(seed).random((t, k)) + 0.5).astype(np.float32)
+    xs, wd = x.double().numpy(), w_down.double().numpy()
+    y, err = np.zeros((t, hidden)), np.zeros((t, hidden))
+    for i in range(e):
+        tok, j = np.nonzero(idx == i)
+        u, w = xs[tok][:, pick[i]], weights[tok, j].astype(np.float64)[:, None]
+        z, s = u @ wd[i].T, np.abs(u) @ np.abs(wd[i]).T
+        np.add.at(y, tok, w * z)
+        np.add.at(err, tok, w * (2 * SUM * s + (2.0 ** -10 * np.abs(z) if scaled else 0.0)))
+    residual = torch.from_numpy(-y).to(DT[dt])
+    want = y + residual.double().numpy()
+    err += SUM * np.abs(y)
+    got = call(x, w_up, w_down, idx, weights, residual)
+    return got, want, err + U[dt] * (np.abs(want) + err) + TINY[dt], y
+
+
+SCALED = [(600, 4, 2, 128, 64), (600, 4, 2, 131, 61), (3000, 8, 8, 256, 64)]
+
+
+@pytest.mark.parametrize("shape", SCALED)
+def test_scaled_down_products_round_once_without_bias(shape):
+    """Each within half of its last bit, and all of them together as often up as
+    down: 10^5 and more roundings of 2^-10 / sqrt 3 at most move the sum by less
+    than 1e-5 of itself (5 deviations)."""
+    got, want, bound, y = left_over(*shape, "bf16", 2, scaled=True)
+    bad = ~(np.abs(got - want) <= bound)
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:3].tolist())
+    gain = ((got - want) * y).sum() / (y * y).sum()
+    assert abs(gain) < 5 * 2.0 ** -10 / 3 ** 0.5 / y.size ** 0.5 + 1e-6, gain
