@@ -84,9 +84,10 @@ __device__ __forceinline__ u32x4 pack8(const float (&v)[8]) {
   return w;
 }
 
-// Eight numbers in 16 bytes: fp16 multiples of 2^(code - 127), the largest of them
-// in [1, 4), the last bit of each one a bit of the code (so 9 bits behind the
-// point).  Rounded once: cut to fp16's 10 bits, half of the last bit kept added,
+// Eight numbers in 16 bytes: fp16 multiples of 2^(code - 141), the largest of them
+// in [2^14, 2^15], the last bit of each one a bit of the code (so 9 bits behind the
+// point, for numbers down to 2^-28 of the largest; one below that is off by 2^-38 of
+// the largest at most).  Rounded once: cut to fp16's 10 bits, half of the last bit kept added,
 // cut there (a tie goes up, but the 13 bits cut first make ties rare; rounded to 10
 // bits first, every other number would be one and all of them grow by 3.5e-4).
 // A block with an infinity or NaN keeps it and has code 0: plain fp16.
@@ -94,8 +95,8 @@ __device__ __forceinline__ u32x4 pack_scaled8(const float (&v)[8]) {
   uint32_t m = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(v[e]) & 0x7FFFFFFFu);
-  const uint32_t top = m >> 23, code = top == 255 ? 0u : min(max(top, 1u), 253u);
-  const float scale = __uint_as_float(code ? (254 - code) << 23 : 0x3F800000u);
+  const uint32_t top = m >> 23, code = top == 255 ? 0u : max(top, 15u);
+  const float scale = __uint_as_float(code ? (268 - code) << 23 : 0x3F800000u);
   const uint32_t half = code ? 0x00010001u : 0u, spread = code | code << 15;
   u32x4 w;
 #pragma unroll
@@ -112,7 +113,7 @@ __device__ __forceinline__ void unpack_scaled8(u32x4 w, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) s |= (w[i] & 0x00010001u) << (2 * i);
   const uint32_t code = (s | s >> 15) & 255u;
-  const float scale = __uint_as_float(code ? code << 23 : 0x3F800000u);
+  const float scale = __uint_as_float(code ? (code - 14) << 23 : 0x3F800000u);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const uint32_t h = (e & 1 ? w[e / 2] >> 16 : w[e / 2]) & 0xFFFEu;

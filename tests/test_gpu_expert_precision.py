@@ -7,7 +7,9 @@ some 2^-8 of the output, and its last rounding hides nothing.
 
 Tolerance of a down product z, its terms' absolute sum s: fp32 sums 1e-5 s (the
 framework's bound), 2^-10 |z| where it goes to the weighted sum as 9 bits behind
-the point (bf16, many rows, top_k > 1).  The weighted sum and the residual add 1e-5
+the point (bf16, many rows, top_k > 1), and 2^-38 of the largest of its 8 channels
+where that is more (half of a subnormal fp16's last bit but one, 2^-24, where the
+largest is 2^14 or more).  The weighted sum and the residual add 1e-5
 of their terms, the result one rounding of what is left."""
 import numpy as np
 import pytest
@@ -62,7 +64,12 @@ def left_over(t, e, k, hidden, inner, dt, seed, scaled=False, channels=None):
         u, w = xs[tok][:, pick[i]], weights[tok, j].astype(np.float64)[:, None]
         z, s = u @ wd[i].T, np.abs(u) @ np.abs(wd[i]).T
         np.add.at(y, tok, w * z)
-        np.add.at(err, tok, w * (2 * SUM * s + (2.0 ** -10 * np.abs(z) if scaled else 0.0)))
+        own = 2 * SUM * s
+        if scaled:
+            size = np.abs(np.pad(z, ((0, 0), (0, -hidden % 8)))).reshape(len(tok), -1, 8)
+            top = np.repeat(size.max(2), 8, 1)[:, :hidden]
+            own += np.maximum(2.0 ** -10 * np.abs(z), 2.0 ** -38 * top)
+        np.add.at(err, tok, w * own)
     residual = torch.from_numpy(-y).to(DT[dt])
     want = y + residual.double().numpy()
     err += SUM * np.abs(y)
@@ -83,3 +90,14 @@ def test_scaled_down_products_round_once_without_bias(shape):
     assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:3].tolist())
     gain = ((got - want) * y).sum() / (y * y).sum()
     assert abs(gain) < 5 * 2.0 ** -10 / 3 ** 0.5 / y.size ** 0.5 + 1e-6, gain
+
+
+@pytest.mark.parametrize("shape", SCALED[:2])
+@pytest.mark.parametrize("power", [-90, 0, 60])
+def test_scaled_channels_of_unlike_size(shape, power):
+    """Channels 2^26 below their neighbours have their 9 bits too."""
+    down = 2.0 ** np.array([0.0, -20.0, -10.0, -26.0, 0.0, -17.0, -24.0, -22.0])
+    channels = torch.from_numpy(np.resize(down, shape[3]) * 2.0 ** power).float()
+    got, want, bound, _ = left_over(*shape, "bf16", 3, scaled=True, channels=channels)
+    bad = ~(np.abs(got - want) <= bound)
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:3].tolist())
