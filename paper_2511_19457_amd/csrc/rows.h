@@ -90,14 +90,28 @@ __device__ __forceinline__ u32x4 pack8(const float (&v)[8]) {
 // the largest at most).  Rounded once: cut to fp16's 10 bits, half of the last bit kept added,
 // cut there (a tie goes up, but the 13 bits cut first make ties rare; rounded to 10
 // bits first, every other number would be one and all of them grow by 3.5e-4).
-// A block with an infinity or NaN keeps it and has code 0: plain fp16.
-__device__ __forceinline__ u32x4 pack_scaled8(const float (&v)[8]) {
+// An infinity or NaN stays one by itself: the code is that of the largest finite
+// number, so its neighbours keep their bits.
+__device__ __forceinline__ u32x4 pack_scaled8(const float (&from)[8]) {
+  float v[8];
   uint32_t m = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) m = max(m, __float_as_uint(v[e]) & 0x7FFFFFFFu);
-  const uint32_t top = m >> 23, code = top == 255 ? 0u : max(top, 15u);
-  const float scale = __uint_as_float(code ? (268 - code) << 23 : 0x3F800000u);
-  const uint32_t half = code ? 0x00010001u : 0u, spread = code | code << 15;
+  for (int e = 0; e < 8; ++e) {
+    v[e] = from[e];
+    m = max(m, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+  }
+  if (m >= 0x7F800000u) {
+    m = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t b = __float_as_uint(v[e]) & 0x7FFFFFFFu;
+      m = b < 0x7F800000u ? max(m, b) : m;
+      // (a NaN of all ones would not survive the rounding's carry)
+      v[e] = b > 0x7F800000u ? __uint_as_float(0x7FC00000u) : v[e];
+    }
+  }
+  const uint32_t code = max(m >> 23, 15u), half = 0x00010001u, spread = code | code << 15;
+  const float scale = __uint_as_float((268 - code) << 23);
   u32x4 w;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -112,8 +126,7 @@ __device__ __forceinline__ void unpack_scaled8(u32x4 w, float (&v)[8]) {
   uint32_t s = 0;
 #pragma unroll
   for (int i = 0; i < 4; ++i) s |= (w[i] & 0x00010001u) << (2 * i);
-  const uint32_t code = (s | s >> 15) & 255u;
-  const float scale = __uint_as_float(code ? (code - 14) << 23 : 0x3F800000u);
+  const float scale = __uint_as_float((((s | s >> 15) & 255u) - 14u) << 23);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const uint32_t h = (e & 1 ? w[e / 2] >> 16 : w[e / 2]) & 0xFFFEu;

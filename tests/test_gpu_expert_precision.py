@@ -101,3 +101,35 @@ def test_scaled_channels_of_unlike_size(shape, power):
     got, want, bound, _ = left_over(*shape, "bf16", 3, scaled=True, channels=channels)
     bad = ~(np.abs(got - want) <= bound)
     assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:3].tolist())
+
+
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan"), "all ones",
+                                   "all ones, negative"])
+def test_scaled_neighbours_of_an_infinity_or_nan(value):
+    """Channels of one number each (z = x[0] w), so that what stands beside the
+    infinity or NaN is exact: large, small and ordinary ones keep their bits."""
+    t, e, k, hidden, inner = 200, 2, 2, 64, 64
+    x = torch.ones(t, hidden, dtype=torch.bfloat16)
+    w_up = torch.zeros(e, inner, hidden, dtype=torch.bfloat16)
+    w_up[:, 0, 0] = 1.0
+    rows = torch.tensor([1.0, 1e5, -7e4, 1e-3, 1.5, -1e5, 98304.0, 0.01]).repeat(hidden // 8)
+    rows[8:16] *= 2.0 ** -60
+    rows[16:24] = torch.tensor([1e-8, 2e-8, -3e-8, 0.0, 5e-8, 1e-8, 1e-8, 1e-8])
+    rows[24:32] *= 2.0 ** 100
+    w_down = torch.zeros(e, hidden, inner, dtype=torch.bfloat16)
+    w_down[:, :, 0] = rows.to(torch.bfloat16)
+    at = torch.arange(hidden) % 8 == torch.arange(hidden) // 8      # one channel of each block
+    if isinstance(value, str):
+        w_down.view(torch.int16)[1, at, 0] = 0x7FFF if value == "all ones" else -1
+    else:
+        w_down[1, at, 0] = value
+    idx = np.tile(np.array([[0, 1]], np.int32), (t, 1))
+    weights = np.full((t, k), 0.5, np.float32)
+    got = call(x, w_up, w_down, idx, weights)
+    want = w_down[0, :, 0].double().numpy()           # 0.5 z + 0.5 z, bf16 numbers: exact
+    at = at.numpy()
+    assert np.array_equal(got[:, ~at], np.tile(want[~at], (t, 1)))
+    if not isinstance(value, str) and value == value:
+        assert (got[:, at] == value).all()
+    else:
+        assert np.isnan(got[:, at]).all()
