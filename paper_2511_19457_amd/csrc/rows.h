@@ -87,9 +87,10 @@ __device__ __forceinline__ u32x4 pack8(const float (&v)[8]) {
 // Eight numbers in 16 bytes: fp16 multiples of 2^(code - 141), the largest of them
 // in [2^14, 2^15], the last bit of each one a bit of the code (so 9 bits behind the
 // point, for numbers down to 2^-28 of the largest; one below that is off by 2^-38 of
-// the largest at most).  Rounded once: cut to fp16's 10 bits, half of the last bit kept added,
-// cut there (a tie goes up, but the 13 bits cut first make ties rare; rounded to 10
-// bits first, every other number would be one and all of them grow by 3.5e-4).
+// the largest at most).  Rounded once: cut to fp16's 10 bits, half of the last bit
+// kept added, cut there (a tie goes up, but the 13 bits cut first make ties rare;
+// rounded to 10 bits first, every other number would be one and all of them grow by
+// 3.5e-4).
 // An infinity or NaN stays one by itself: the code is that of the largest finite
 // number, so its neighbours keep their bits.
 __device__ __forceinline__ u32x4 pack_scaled8(const float (&from)[8]) {
@@ -100,14 +101,17 @@ __device__ __forceinline__ u32x4 pack_scaled8(const float (&from)[8]) {
     v[e] = from[e];
     m = max(m, __float_as_uint(v[e]) & 0x7FFFFFFFu);
   }
-  if (m >= 0x7F800000u) {
+  if (m >= 0x7F000000u) {   // (2^127; seldom)
     m = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const uint32_t b = __float_as_uint(v[e]) & 0x7FFFFFFFu;
       m = b < 0x7F800000u ? max(m, b) : m;
-      // (a NaN of all ones would not survive the rounding's carry)
-      v[e] = b > 0x7F800000u ? __uint_as_float(0x7FC00000u) : v[e];
+      // a NaN of all ones would not survive the rounding's carry, nor a finite
+      // number the one to 2^128: the largest of 9 bits takes its place
+      if (b > 0x7F800000u) v[e] = __uint_as_float(0x7FC00000u);
+      else if (b > 0x7F7FC000u && b < 0x7F800000u)
+        v[e] = copysignf(__uint_as_float(0x7F7FC000u), v[e]);
     }
   }
   const uint32_t code = max(m >> 23, 15u), half = 0x00010001u, spread = code | code << 15;

@@ -133,3 +133,19 @@ def test_scaled_neighbours_of_an_infinity_or_nan(value):
         assert (got[:, at] == value).all()
     else:
         assert np.isnan(got[:, at]).all()
+
+
+def test_scaled_numbers_next_to_the_largest_stay_finite():
+    t, e, k, hidden, inner = 200, 2, 2, 64, 64
+    x = torch.ones(t, hidden, dtype=torch.bfloat16)
+    w_up = torch.zeros(e, inner, hidden, dtype=torch.bfloat16)
+    w_up[:, 0, 0] = w_up[:, 1, 1] = 1.0
+    w_down = torch.zeros(e, hidden, inner, dtype=torch.bfloat16)
+    most = torch.tensor(float(2 ** 128 - 2 ** 120), dtype=torch.float64)
+    w_down[:, :, 0] = most.to(torch.bfloat16)
+    w_down[:, :, 1] = 0.998 * 2.0 ** 120              # z within 2^-17 of 2^128
+    w_down[:, 1::2] *= -1
+    idx = np.tile(np.array([[0, 1]], np.int32), (t, 1))
+    got = call(x, w_up, w_down, idx, np.full((t, k), 0.25, np.float32))
+    z = w_down[0, :, :2].double().sum(1).numpy()
+    assert np.isfinite(got).all() and (np.abs(got - 0.5 * z) <= 2.0 ** -8 * np.abs(z)).all()
