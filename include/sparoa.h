@@ -647,7 +647,7 @@ sparoa_status sparoa_expert_plan(int64_t tokens, int64_t top_k, int64_t experts,
  *   with many rows (more than 12) and top_k > 1, where it is rounded once to 9
  *   bits behind the point (8 channels share an exponent).  The weighted sum is fp32, in the
  *   order of j; y is rounded once.
- *   act: NONE, RELU, RELU6, SILU or GELU.
+ *   act: NONE, RELU, RELU6, SILU or GELU; each of a NaN is NaN.
  *   Kernels: few rows an expert stream its weights; many run tiles through
  *   LDS.  Only experts with a row are multiplied.
  *   Workspace: sparoa_expert_ffn_workspace_size bytes (u and the down
@@ -682,7 +682,7 @@ sparoa_status sparoa_expert_ffn(const sparoa_expert_ffn_desc *desc, sparoa_act a
  *   consecutive (they cost least when they are).  Adapters of smaller rank
  *   are padded with zero rows of lora_a.
  *   An infinity or NaN in a row of x or in an adapter stays with the rows it is
- *   of.
+ *   of; act (RELU and RELU6 too) of a NaN is NaN.
  *   a_a x accumulates in fp32, is scaled in fp32 and kept in fp32 where the
  *   weights are streamed, else rounded to dtype once for the second product.
  *   act: NONE, RELU or RELU6.

@@ -35,13 +35,19 @@ __device__ __forceinline__ f32x4 mma16(u32x4 w, u32x4 x, f32x4 acc) {
   }
 }
 
+// relu and relu6 of a NaN are NaN here (apply_act gives 0).
+__device__ __forceinline__ float row_act(float v, int act) {
+  const float u = apply_act(v, act);
+  return v == v ? u : v;
+}
+
 __device__ __forceinline__ float block_act(float v, int act) {
   // (reciprocal and power to one unit in the last place each: below a rounding
   // of u, in place of a division's dozen instructions in tiles' epilogues)
   if (act == SPAROA_ACT_SILU)
     return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -1.44269504088896341f));
   if (act == SPAROA_ACT_GELU) return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
-  return apply_act(v, act);
+  return row_act(v, act);
 }
 
 // V consecutive elements from an address aligned to them (V sizeof <= 16).

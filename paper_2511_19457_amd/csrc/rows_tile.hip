@@ -355,7 +355,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
         if (a.act != SPAROA_ACT_NONE)
 #pragma unroll
           for (int i = 0; i < NG * H * 8; ++i)
-            o[i / (8 * H)][i / 8 % H][i % 8] = apply_act(o[i / (8 * H)][i / 8 % H][i % 8], a.act);
+            o[i / (8 * H)][i / 8 % H][i % 8] = row_act(o[i / (8 * H)][i / 8 % H][i % 8], a.act);
       } else if constexpr (MODE <= kRowsUpGated) {
         // (a branch for all of the values, not one for each)
         auto all = [&](auto act) __attribute__((always_inline)) {
