@@ -41,11 +41,14 @@ __device__ __forceinline__ float row_act(float v, int act) {
   return v == v ? u : v;
 }
 
+template <int DT>
 __device__ __forceinline__ float block_act(float v, int act) {
-  // (reciprocal and power to one unit in the last place each: below a rounding
-  // of u, in place of a division's dozen instructions in tiles' epilogues)
-  if (act == SPAROA_ACT_SILU)
+  // (16-bit types: 2^x of a rounded product, off by |v| 2^-24, and a reciprocal are
+  // below a rounding of u, in place of expf's and a division's dozens of instructions)
+  if (act == SPAROA_ACT_SILU) {
+    if constexpr (DT == SPAROA_F32) return v / (1.f + expf(-v));
     return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -1.44269504088896341f));
+  }
   if (act == SPAROA_ACT_GELU) return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
   return row_act(v, act);
 }

@@ -257,7 +257,7 @@ __global__ __launch_bounds__(64 * NW, 2) void rows_split_kernel(RowsArgs a) {
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        g[e] = FC ? row_act(g[e], a.act) : block_act(g[e], a.act);
+        g[e] = FC ? row_act(g[e], a.act) : block_act<DT>(g[e], a.act);
         if constexpr (GATED) g[e] *= m[e];
         if constexpr (UP) g[e] = ch + e < a.n ? g[e] : 0.f;
       }

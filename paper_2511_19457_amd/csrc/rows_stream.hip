@@ -284,7 +284,7 @@ __global__ __launch_bounds__(kNT, 2) void rows_stream_kernel(RowsArgs a) {
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            o[e] = FC ? row_act(o[e], a.act) : block_act(o[e], a.act);
+            o[e] = FC ? row_act(o[e], a.act) : block_act<DT>(o[e], a.act);
             if (GATED) o[e] *= mul[e];
           }
           if (a.ldy % 4 == 0 && ch + 4 <= a.n) {

@@ -362,7 +362,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void rows_tile_kernel(RowsArgs a
 #pragma unroll
           for (int i = 0; i < NG * H * 8; ++i)
             o[i / (8 * H)][i / 8 % H][i % 8] =
-                block_act(o[i / (8 * H)][i / 8 % H][i % 8], decltype(act)::value);
+                block_act<DT>(o[i / (8 * H)][i / 8 % H][i % 8], decltype(act)::value);
         };
         switch (a.act) {
           case SPAROA_ACT_SILU: all(std::integral_constant<int, SPAROA_ACT_SILU>{}); break;

@@ -149,3 +149,29 @@ def test_scaled_numbers_next_to_the_largest_stay_finite():
     got = call(x, w_up, w_down, idx, np.full((t, k), 0.25, np.float32))
     z = w_down[0, :, :2].double().sum(1).numpy()
     assert np.isfinite(got).all() and (np.abs(got - 0.5 * z) <= 2.0 ** -8 * np.abs(z)).all()
+
+
+# ---------------------------------------------------------------- activations
+
+def _through(v, act, dt, hidden, rows):
+    """act(v): both matrices the identity, one expert of `rows` rows a token."""
+    t = -(-len(v) // hidden)
+    t = max(t, rows)
+    x = torch.zeros(t * hidden, dtype=DT[dt])
+    x[:len(v)] = v
+    eye = torch.eye(hidden, dtype=DT[dt])[None]
+    got = call(x.reshape(t, hidden), eye, eye, np.zeros((t, 1), np.int32),
+               np.ones((t, 1), np.float32), act=act)
+    return got.reshape(-1)[:len(v)]
+
+
+# (few rows and many; whole vectors, and rows that start off 16 bytes)
+@pytest.mark.parametrize("hidden,rows", [(64, 1), (64, 300), (61, 1), (61, 300)])
+def test_silu_fp32(hidden, rows):
+    """exp to one unit in the last place (two halves), the sum and the division to
+    half of one: 4 2^-24, and a second-order rest."""
+    v = torch.cat([torch.linspace(-60, 30, 3001), torch.linspace(-1e-3, 1e-3, 101)])
+    got, w = _through(v, "silu", "f32", hidden, rows), v.double().numpy()
+    want = w / (1.0 + np.exp(-w))
+    off = np.abs(got - want) / np.maximum(np.abs(want), 2.0 ** -126)
+    assert off.max() <= 4.5 * 2.0 ** -24, (off.max() * 2 ** 24, v[off.argmax()])
