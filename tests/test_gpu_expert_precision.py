@@ -77,6 +77,17 @@ def left_over(t, e, k, hidden, inner, dt, seed, scaled=False, channels=None):
     return got, want, err + U[dt] * (np.abs(want) + err) + TINY[dt], y
 
 
+# tokens, experts, choices, hidden, inner: few rows and many, whole vectors and not
+@pytest.mark.parametrize("dt,shape", [
+    ("bf16", (10, 8, 2, 128, 64)), ("bf16", (20, 8, 2, 131, 61)), ("f16", (10, 8, 2, 128, 64)),
+    ("f16", (600, 4, 2, 128, 64)), ("f16", (600, 4, 2, 131, 61)), ("bf16", (600, 4, 1, 128, 64)),
+    ("bf16", (600, 4, 1, 131, 61)), ("f32", (60, 4, 2, 128, 64)), ("f32", (600, 4, 2, 131, 61))])
+def test_down_products_stay_fp32(dt, shape):
+    got, want, bound, _ = left_over(*shape, dt, 1)
+    bad = ~(np.abs(got - want) <= bound)
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:3].tolist())
+
+
 SCALED = [(600, 4, 2, 128, 64), (600, 4, 2, 131, 61), (3000, 8, 8, 256, 64)]
 
 
