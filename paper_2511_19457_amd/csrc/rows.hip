@@ -255,8 +255,20 @@ sparoa_status launch_rows(RowsMode mode, const RowsArgs &a, sparoa_dtype dt, hip
       SPAROA_LAUNCH_CHECK("fc_adapted: first product of few rows");
       return SPAROA_OK;
     }
-    return a.h_f32 ? launch_rows_stream(mode, a, dt, stream)
-                   : launch_rows_split(mode, kTile16x64, a, dt, stream);
+    if (a.h_f32) return launch_rows_stream(mode, a, dt, stream);
+    // (a launch has fewer than 2^32 threads: rows in parts of whole tiles, up to 2^31
+    // threads each)
+    constexpr int64_t kPart = 1 << 24;
+    for (int64_t r0 = 0; r0 < a.rows; r0 += kPart) {
+      RowsArgs p = a;
+      p.rows = std::min(a.rows - r0, kPart);
+      p.x = reinterpret_cast<const char *>(a.x) + r0 * a.ldx * elem_size(dt);
+      p.ids = a.ids + r0;
+      p.y = reinterpret_cast<char *>(a.y) + r0 * a.ldy * elem_size(dt);
+      const sparoa_status st = launch_rows_split(mode, kTile16x64, p, dt, stream);
+      if (st != SPAROA_OK) return st;
+    }
+    return SPAROA_OK;
   }
   const RowsTile tile = rows_tile_for(mode, a, dt);
   if (mode == kRowsDownScaled && tile < kTile64x64)
@@ -268,9 +280,9 @@ sparoa_status launch_rows(RowsMode mode, const RowsArgs &a, sparoa_dtype dt, hip
 
 sparoa_status launch_pad_rows(const void *from, void *to, int64_t rows, int k, int pitch,
                               sparoa_dtype dt, hipStream_t stream) {
-  // (some 256 pieces a work-group, a row at least, and a grid that fits)
+  // (some 256 pieces a work-group, a row at least, and fewer than 2^32 threads)
   const int64_t per = std::max<int64_t>(std::max<int64_t>(1, 256 / (pitch / 8)),
-                                        cdiv(rows, 1 << 24));
+                                        cdiv(rows, 1 << 23));
   const unsigned grid = (unsigned)cdiv(rows, per);
   switch (elem_size(dt)) {
     case 4:

@@ -1,6 +1,7 @@
 """Kernels and tiles of the experts' products and adapted FCs, on the CPU: the
 library's launches are recorded instead of run (launch_recorder.c), in a process of
-its own.  The shapes of test_gpu_row_tiles.py run the tiles that they are there for."""
+its own.  The shapes of test_gpu_row_tiles.py run the tiles that they are there
+for, and no launch is larger than the runtime takes (2^32 threads a dimension)."""
 import json
 import os
 import re
@@ -83,3 +84,27 @@ def test_shapes_run_the_tiles_they_are_for(launches):
             [["adapted", CODE[dt], *s[:5]] for s, dt in cases])):
         want = "64x128" if dt == "f32" else s[5]
         assert st == 0 and tiles(got)[FC] == want, (s, dt, got)
+
+
+def threads(name):
+    m = re.search(r"rows_split_kernelILi\dELNS_8RowsModeE\dELi\d+ELi\d+ELi(\d+)E", name)
+    if m:
+        return 64 * int(m.group(1))
+    m = re.search(r"rows_tile_kernelILi\dELNS_8RowsModeE\dELi(\d+)ELi(\d+)E", name)
+    if m:
+        return 64 * int(m.group(1)) * int(m.group(2))
+    return 512 if "rows_stream" in name else 256
+
+
+# m, k, n, adapters, rank: very many short rows, aligned and padded
+HUGE = [(1 << 26, 8, 8, 2, 16), (1 << 27, 8, 8, 2, 16), ((1 << 27) + 5, 8, 8, 2, 16),
+        (1 << 28, 64, 64, 2, 64), (1 << 25, 8, 8, 2, 512), (1 << 29, 8, 8, 2, 8),
+        ((1 << 24) * 32, 57, 8, 2, 8), ((1 << 24) * 32 - 3, 57, 8, 2, 8), (1 << 29, 8, 8, 3, 512)]
+
+
+def test_launches_of_very_many_rows_fit(launches):
+    for dt in (0, 2):
+        for s, (st, got) in zip(HUGE, launches([["adapted", dt, *s] for s in HUGE])):
+            assert st == 0 and got, s
+            for name, x, y, z in got:
+                assert x * threads(name) < 1 << 32 and y < 1 << 16, (s, dt, name, x, y)
