@@ -644,16 +644,20 @@ sparoa_status sparoa_expert_plan(int64_t tokens, int64_t top_k, int64_t experts,
  *   token without experts gives residual, or 0.
  *   Products accumulate in fp32; u is rounded to dtype once (the second
  *   product's operand).  A slot's down product stays fp32, but for bf16 experts
- *   with many rows (more than 12) and top_k > 1, where it is rounded once to 9
- *   bits behind the point (8 channels share an exponent).  The weighted sum is fp32, in the
- *   order of j; y is rounded once.
+ *   with more than 12 rows each on average (32 where hidden or inner is no
+ *   multiple of 8) and top_k > 1, where it is rounded once to 9 bits behind the
+ *   point: 8 channels share an exponent, and one more than 2^28 below the
+ *   largest finite of them is off by up to 2^-38 of that one.  The weighted sum is
+ *   fp32, in the order of j; y is rounded once.  An infinity or NaN stays in the
+ *   channels and tokens that it is of.
  *   act: NONE, RELU, RELU6, SILU or GELU; each of a NaN is NaN.
  *   Kernels: few rows an expert stream its weights; many run tiles through
  *   LDS.  Only experts with a row are multiplied.
  *   Workspace: sparoa_expert_ffn_workspace_size bytes (u and the down
  *   products, tokens * top_k rows; where hidden or inner is no multiple of 16
- *   bytes and the experts have many rows also x and the matrices with rows
- *   that are); contents on entry do not matter.
+ *   bytes and the experts have many rows also x and the matrices, of unused
+ *   experts too, with rows that are, copied by every call); contents on entry do
+ *   not matter.
  * Errors: those of the plan's sizes; INVALID_ARG for hidden or inner <= 0, null
  * x/w_up/w_down/weights/plan/y, biases that do not match has_bias, an unknown
  * act; UNSUPPORTED for misaligned pointers, x or one expert's matrix of 2 GiB

@@ -324,9 +324,10 @@ sparoa_status sparoa_expert_ffn(const sparoa_expert_ffn_desc *d, sparoa_act act,
   // The down products of bf16 experts with many rows go to the weighted sum as 8
   // fp16 numbers that share an exponent (pack_scaled8), which halves their way
   // through memory: 4096 tokens, 64 experts, top 8, 2048 x 1024: the down product
-  // 213 -> 179 us, the weighted sum 55 -> 27.  9 bits behind the point add a fiftieth to the error that u's
-  // rounding gives; more where a single product is rounded again for y, and
-  // beside fp16's own 10 bits.
+  // 213 -> 179 us (least times), the weighted sum 55 -> 27.  9 bits behind the
+  // point, for channels down to 2^-28 of their largest neighbour, add a fiftieth to
+  // the error that u's rounding gives (root mean square, and no bias); more where a
+  // single product is rounded again for y, and beside fp16's own 10 bits.
   const bool scaled = d->dtype == SPAROA_BF16 && d->top_k > 1 &&
                       rows_tile_for(kRowsDown, a, d->dtype) >= kTile64x64;
   st = launch_rows(scaled ? kRowsDownScaled : kRowsDown, a, d->dtype, stream);

@@ -226,7 +226,9 @@ RowsTile rows_tile_for(RowsMode mode, const RowsArgs &a, sparoa_dtype dt) {
     return large_or_small(cdiv(a.rows, 128) * cdiv(wide, 256), cdiv(a.rows, 64) * cdiv(wide, 128),
                           chunks, 4);
   }
-  // Experts, by their average rows (us, 16-bit unless it says fp32).  Few: bound
+  // Experts, by their average rows: what the host knows.  (Slots without an expert
+  // count as rows, and a popular expert takes the others' tile; the figures are of
+  // even loads.)  In us, 16-bit unless it says fp32.  Few: bound
   // by the weights' stream (64 experts of 2048 x 1024 gated, 4 rows each: 142
   // against 156 in 64 x 64 tiles, 20 rows 204 / 177); fp32 products are slow
   // enough for 64 rows (16 experts of 1024 x 1024, 50 rows: 68 / 85, 125 rows

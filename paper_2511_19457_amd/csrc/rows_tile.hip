@@ -11,10 +11,11 @@
 // channels, so the product gate * up is a lane's own.
 // Low-rank adapters are chunks behind K's: for every adapter among the tile's
 // rows, its rows of h (the others' read as zeros) against its matrix b.
-// Bound by the matrix pipe and what feeds it: FC of 4096^3 bf16 128 us (1.07
-// PFLOP/s; 100 us with K's loads left out, 64 us at the pipe's rate), the MFMAs
-// busy half of the cycles; 4096 tokens over 64 experts (2048 x 1024 gated, top
-// 8) 295 us up, 179 us down.
+// Bound by the matrix pipe and what feeds it: FC of 4096^3 bf16 128 us at least
+// (1.07 PFLOP/s; 100 us with K's loads left out, 64 us at the pipe's rate), 143-157
+// us in the median of 30 passes (the first ones are the fastest), the MFMAs busy
+// half of the cycles; 4096 tokens over 64 experts (2048 x 1024 gated, top 8) at
+// least 303 us up and 182 down, in the median 331 and 200.
 // Work-groups are dealt round-robin to the 8 XCDs: XCD i takes the i-th run of
 // tiles, column tiles innermost, so the tiles of one expert share an L2.
 #include <algorithm>
