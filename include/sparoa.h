@@ -749,6 +749,129 @@ sparoa_status sparoa_block_norm(const sparoa_block_norm_desc *desc, const void *
                                 const void *r, const void *pre_w, const void *pre_b, void *r_out,
                                 void *n_out, hipStream_t stream);
 
+/* ------------------------------------------------------------------------
+ * Attention over a paged cache of keys and values: what lies between a block's
+ * projections and its output product while requests are served.
+ *
+ * The cache: k_cache and v_cache [pages][kv_heads][page_size][head_dim]
+ * (dtype).  Request r's key at position p lies in page page_table[r][p /
+ * page_size] (int32 [requests][table_pages]), row p % page_size.  Requests may
+ * share pages that no call writes.  A page number outside [0, pages) is no
+ * page: its keys are seen by no row, and nothing is written there.
+ *
+ * A call's rows: q (and k, v) hold `tokens` rows, request r's are q_start[r] ..
+ * q_start[r + 1] - 1 (int32 [requests + 1]); kv_len[r] keys (int32) are in the
+ * cache of r once the call's own are, so its row j has position kv_len[r] - n_r
+ * + j, n_r its rows.  Rows of no request (behind the last) are not looked at,
+ * and their outputs are left as they were.  These numbers lie on the device, so
+ * that a captured call serves other batches; `tokens`, `max_queries` (rows of a
+ * request) and `max_keys` (kv_len of a request) are what they may reach.  A
+ * request without rows, or whose numbers break these bounds (rows outside
+ * [0, tokens), n_r > max_queries, kv_len < n_r or > max_keys), is left out.
+ *
+ * Query head h reads the keys of head h / (heads / kv_heads).
+ * Errors of every call: INVALID_ARG for a null descriptor or required pointer,
+ * sizes <= 0, heads that kv_heads does not divide, max_keys > table_pages *
+ * page_size, an unknown dtype; UNSUPPORTED for head_dim > 256 or no multiple of
+ * 8, tokens * heads, max_keys, requests * table_pages or pages * kv_heads *
+ * page_size of 2^31 or more, a misaligned pointer.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  int64_t tokens, requests, heads, kv_heads, head_dim;
+  int64_t pages, page_size, table_pages, max_queries, max_keys;
+  sparoa_dtype dtype;
+} sparoa_kv_desc;
+
+/* Rotation by position, and the append to the cache: for every row t of a
+ * request, at position p = positions[t] (int32 [tokens]; NULL: its position in
+ * the cache), each head x of q and k becomes
+ *   (x_a, x_b) -> (x_a cos - x_b sin, x_a sin + x_b cos) of p freqs[i],
+ *   a = i, b = i + rot_dim / 2          (interleaved 0)
+ *   a = 2 i, b = 2 i + 1                (interleaved 1),     i < rot_dim / 2;
+ * dimensions from rot_dim on stay.  freqs: fp64 [rot_dim / 2], radians a
+ * position (NULL where rot_dim is 0).
+ *   q [tokens][heads * head_dim] -> q_out [tokens][heads][head_dim] (both NULL:
+ *   no queries; q_out may be q where q_stride = heads * head_dim);
+ *   k, v [tokens][kv_heads * head_dim] -> the cache, at the row's position in
+ *   it.  q_stride, k_stride, v_stride: elements from a row to the next (the rows
+ *   may be parts of one projection's).
+ *   Angles are reduced to a turn in fp64, the products fp32, rounded once.
+ * Errors: also INVALID_ARG for an odd rot_dim, one outside [0, head_dim], freqs
+ * that do not match it, q without q_out, strides below a row. */
+sparoa_status sparoa_kv_append(const sparoa_kv_desc *desc, int64_t rot_dim, int interleaved,
+                               const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                               const void *v, int64_t v_stride, const double *freqs,
+                               const int32_t *positions, const int32_t *q_start,
+                               const int32_t *kv_len, const int32_t *page_table, void *q_out,
+                               void *k_cache, void *v_cache, hipStream_t stream);
+
+/* Attention of every request's rows over its cache:
+ *   out = sum_k w_k v_k,  w = softmax over the seen keys k of
+ *   cap tanh(scale q.k / cap) - slopes[head] |p - k|
+ * (cap 0: scale q.k; slopes fp32 [heads], NULL: none).  The row at position p
+ * sees the keys lo <= k < hi:
+ *   hi = causal ? min(kv_len, max(p + 1, prefix_len[r])) : kv_len
+ *   lo = max(0, window ? p + 1 - window : 0, first_key[t])
+ * prefix_len int32 [requests] (NULL: 0; a prefix seen both ways), first_key
+ * int32 [tokens] (NULL: 0; where the row's document begins).  A row that sees
+ * no key gives 0.
+ *   q and out [tokens][heads][head_dim], no overlap.
+ *   Scores, softmax and sums are fp32; a weight is rounded once to dtype as an
+ *   operand of the second product, the output once.  An infinity or NaN in a
+ *   key or value stays with the rows that see it.
+ *   Equal inputs give equal bits.  Workspace: sparoa_attention_workspace_size
+ *   bytes, contents on entry do not matter; it may not be shared by calls that
+ *   overlap in time.
+ * Errors: also INVALID_ARG for null options, a scale or cap that is not finite,
+ * scale <= 0, cap < 0, window < 0; WORKSPACE. */
+typedef struct {
+  float scale, cap;
+  int64_t window;   /* keys a row sees up to its own, 0: all */
+  int causal;
+} sparoa_attention_opts;
+
+sparoa_status sparoa_attention_workspace_size(const sparoa_kv_desc *desc, size_t *bytes);
+sparoa_status sparoa_paged_attention(const sparoa_kv_desc *desc, const sparoa_attention_opts *opts,
+                                     const void *q, const void *k_cache, const void *v_cache,
+                                     const int32_t *q_start, const int32_t *kv_len,
+                                     const int32_t *page_table, const int32_t *prefix_len,
+                                     const int32_t *first_key, const float *slopes, void *out,
+                                     void *workspace, size_t ws_bytes, hipStream_t stream);
+
+/* Attention of drafted tokens that form a tree behind each request's context:
+ * the request's rows are the tree's nodes, their keys the last n_r of its cache
+ * (in the order of the rows).  Node j sees the context and the nodes i whose bit
+ * i % 64 of tree_mask[t][i / 64] is set, t its row (its ancestors; itself, if its
+ * own bit is set): uint64 [tokens][ceil(max_queries / 64)].
+ *   positions int32 [tokens]: the nodes' positions (context + depth); wanted
+ *   where there are slopes or a window, else nullable.  Distances are between
+ *   positions; a window hides what lies window or more positions back.
+ *   opts->causal is not looked at.  All else as for sparoa_paged_attention.
+ * Errors: also INVALID_ARG for a null tree_mask or positions that are wanted;
+ * UNSUPPORTED for max_queries > 256. */
+sparoa_status sparoa_tree_attention(const sparoa_kv_desc *desc, const sparoa_attention_opts *opts,
+                                    const void *q, const void *k_cache, const void *v_cache,
+                                    const int32_t *q_start, const int32_t *kv_len,
+                                    const int32_t *page_table, const uint64_t *tree_mask,
+                                    const int32_t *positions, const float *slopes, void *out,
+                                    void *workspace, size_t ws_bytes, hipStream_t stream);
+
+/* Accepted drafts into place: of request r's last n_r keys and values, node
+ * keep[r][j] moves to where node j was, for all j < kept[r] at once (read before
+ * any is written), in each of `layers` caches that lie one behind the other
+ * (k_cache, v_cache [layers][pages][kv_heads][page_size][head_dim]).  The context
+ * is then kv_len[r] - n_r + kept[r] keys long.
+ *   keep int32 [requests][most], kept int32 [requests].  An entry outside [0,
+ *   n_r) moves nothing; a request whose kept is above most or n_r is left out.
+ *   heads and tokens of the descriptor bound as above; pages that requests share
+ *   must not be among those written.
+ * Errors: also INVALID_ARG for layers or most <= 0; UNSUPPORTED for most > 256 or
+ * layers of 65536 or more. */
+sparoa_status sparoa_kv_keep(const sparoa_kv_desc *desc, int64_t layers, const int32_t *q_start,
+                             const int32_t *kv_len, const int32_t *page_table,
+                             const int32_t *keep, int64_t most, const int32_t *kept,
+                             void *k_cache, void *v_cache, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

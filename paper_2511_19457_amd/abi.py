@@ -41,7 +41,8 @@ EXPORTS = [
     "sparoa_block_norm", "sparoa_expert_plan_words", "sparoa_expert_route_workspace_size",
     "sparoa_expert_route", "sparoa_expert_plan_workspace_size", "sparoa_expert_plan",
     "sparoa_expert_ffn_workspace_size", "sparoa_expert_ffn", "sparoa_fc_adapted_workspace_size",
-    "sparoa_fc_adapted",
+    "sparoa_fc_adapted", "sparoa_kv_append", "sparoa_attention_workspace_size",
+    "sparoa_paged_attention", "sparoa_tree_attention", "sparoa_kv_keep",
 ]
 
 
@@ -118,6 +119,17 @@ class BlockNormDesc(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("gate_rows", ctypes.c_int64),
                 ("dtype", ctypes.c_int), ("post", ctypes.c_int), ("pre", ctypes.c_int),
                 ("eps", ctypes.c_float), ("residual_scale", ctypes.c_float)]
+
+
+class KvDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int64) for n in
+                ("tokens", "requests", "heads", "kv_heads", "head_dim", "pages", "page_size",
+                 "table_pages", "max_queries", "max_keys")] + [("dtype", ctypes.c_int)]
+
+
+class AttentionOpts(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("cap", ctypes.c_float), ("window", ctypes.c_int64),
+                ("causal", ctypes.c_int)]
 
 
 def _load():
@@ -200,6 +212,14 @@ def _load():
         "sparoa_fc_adapted": (ctypes.c_int, [P(FcAdaptedDesc), ctypes.c_int] + [vp] * 10 +
                               [sz, vp]),
         "sparoa_block_norm": (ctypes.c_int, [P(BlockNormDesc)] + [vp] * 10),
+        "sparoa_kv_append": (ctypes.c_int, [P(KvDesc), i64, ctypes.c_int] + [vp, i64] * 3 +
+                             [vp] * 9),
+        "sparoa_attention_workspace_size": (ctypes.c_int, [P(KvDesc), P(sz)]),
+        "sparoa_paged_attention": (ctypes.c_int, [P(KvDesc), P(AttentionOpts)] + [vp] * 11 +
+                                   [sz, vp]),
+        "sparoa_tree_attention": (ctypes.c_int, [P(KvDesc), P(AttentionOpts)] + [vp] * 11 +
+                                  [sz, vp]),
+        "sparoa_kv_keep": (ctypes.c_int, [P(KvDesc), i64] + [vp] * 4 + [i64] + [vp] * 4),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -709,3 +729,125 @@ def sparoa_block_norm(desc, y, post_w, post_b, gate, r, pre_w, pre_b, r_out, n_o
         _whole(post_b, dt, c, "post_b"), _whole(gate, dt, gates, "gate"), _whole(r, dt, n, "r"),
         _whole(pre_w, dt, c, "pre_w"), _whole(pre_b, dt, c, "pre_b"),
         _whole(r_out, dt, n, "r_out"), _whole(n_out, dt, n, "n_out"), _stream(stream)))
+
+# ------------------------------------ attention over a paged cache (see sparoa.h)
+
+def _here(*tensors):
+    """Refuses tensors of another device than the current one: the call's stream is its."""
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != torch.cuda.current_device():
+            raise SparoaError(1, f"a tensor on {t.device}, the current device is "
+                                 f"{torch.cuda.current_device()}")
+
+
+def _rows(t, dtype, rows, width, name):
+    """Pointer and row stride of a [rows, width] view whose rows are dense."""
+    if t.dim() != 2 or t.dtype is not dtype or tuple(t.shape) != (rows, width) or not t.is_cuda \
+            or (width > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < width):
+        raise SparoaError(1, f"{name}: a {dtype} device tensor [{rows}, {width}] with dense rows "
+                             f"is wanted, got {t.dtype} {tuple(t.shape)} with strides "
+                             f"{t.stride()} on {t.device}")
+    return t.data_ptr(), t.stride(0) if rows > 1 else width
+
+
+def kv_desc(tokens, requests, heads, kv_heads, head_dim, pages, page_size, table_pages, dtype=BF16,
+            max_queries=None, max_keys=None):
+    """max_queries: most rows of a request (default: tokens); max_keys: most keys of a
+    request (default: what its pages hold)."""
+    if isinstance(dtype, torch.dtype):
+        dtype = dtype_code(dtype)
+    return KvDesc(tokens, requests, heads, kv_heads, head_dim, pages, page_size, table_pages,
+                  tokens if max_queries is None else max_queries,
+                  table_pages * page_size if max_keys is None else max_keys, dtype)
+
+
+def attention_opts(scale, cap=0.0, window=0, causal=True):
+    return AttentionOpts(scale, cap, window, int(causal))
+
+
+def _batch(d, q_start, kv_len, page_table):
+    return (_whole(q_start, torch.int32, d.requests + 1, "q_start"),
+            _whole(kv_len, torch.int32, d.requests, "kv_len"),
+            _whole(page_table, torch.int32, d.requests * d.table_pages, "page_table"))
+
+
+def _cache(d, k_cache, v_cache, layers=1):
+    n, dt = layers * d.pages * d.kv_heads * d.page_size * d.head_dim, _DT_TORCH.get(d.dtype)
+    return _whole(k_cache, dt, n, "k_cache"), _whole(v_cache, dt, n, "v_cache")
+
+
+def sparoa_kv_append(desc, q, k, v, freqs, positions, q_start, kv_len, page_table, q_out, k_cache,
+                     v_cache, rot_dim=None, interleaved=False, stream=None):
+    """Rotates q and k by position (q to q_out) and puts k and v into the cache (see sparoa.h).
+    q [tokens, heads * head_dim], k and v [tokens, kv_heads * head_dim]: views with any row
+    stride; q and q_out None: no queries; rot_dim: default head_dim, or 0 without freqs."""
+    d, dt = desc, _DT_TORCH.get(desc.dtype)
+    if rot_dim is None:
+        rot_dim = 0 if freqs is None else d.head_dim
+    _here(q, k, v, freqs, positions, q_start, kv_len, page_table, q_out, k_cache, v_cache)
+    wide, narrow = d.heads * d.head_dim, d.kv_heads * d.head_dim
+    qp, qs = (None, wide) if q is None else _rows(q, dt, d.tokens, wide, "q")
+    kp, ks = _rows(k, dt, d.tokens, narrow, "k")
+    vp, vs = _rows(v, dt, d.tokens, narrow, "v")
+    batch, cache = _batch(d, q_start, kv_len, page_table), _cache(d, k_cache, v_cache)
+    _check(_L.sparoa_kv_append(
+        ctypes.byref(d), rot_dim, int(interleaved), qp, qs, kp, ks, vp, vs,
+        _whole(freqs, torch.float64, rot_dim // 2, "freqs"),
+        _whole(positions, torch.int32, d.tokens, "positions"), *batch,
+        _whole(q_out, dt, d.tokens * wide, "q_out"), *cache, _stream(stream)))
+
+
+def sparoa_attention_workspace_size(desc):
+    s = ctypes.c_size_t()
+    _check(_L.sparoa_attention_workspace_size(ctypes.byref(desc), ctypes.byref(s)))
+    return s.value
+
+
+def sparoa_paged_attention(desc, opts, q, k_cache, v_cache, q_start, kv_len, page_table,
+                           prefix_len, first_key, slopes, out, workspace, stream=None):
+    """Attention of every request's rows over its cache (see sparoa.h)."""
+    d, dt = desc, _DT_TORCH.get(desc.dtype)
+    _here(q, k_cache, v_cache, q_start, kv_len, page_table, prefix_len, first_key, slopes, out,
+          workspace)
+    n = d.tokens * d.heads * d.head_dim
+    ws, ws_bytes = _scratch(workspace)
+    _check(_L.sparoa_paged_attention(
+        ctypes.byref(d), ctypes.byref(opts), _whole(q, dt, n, "q"), *_cache(d, k_cache, v_cache),
+        *_batch(d, q_start, kv_len, page_table),
+        _whole(prefix_len, torch.int32, d.requests, "prefix_len"),
+        _whole(first_key, torch.int32, d.tokens, "first_key"),
+        _whole(slopes, torch.float32, d.heads, "slopes"), _whole(out, dt, n, "out"), ws, ws_bytes,
+        _stream(stream)))
+
+
+def sparoa_tree_attention(desc, opts, q, k_cache, v_cache, q_start, kv_len, page_table, tree_mask,
+                          positions, slopes, out, workspace, stream=None):
+    """Attention of drafted trees over their contexts (see sparoa.h); tree_mask: the bits in
+    int64 [tokens, ceil(max_queries / 64)]."""
+    d, dt = desc, _DT_TORCH.get(desc.dtype)
+    _here(q, k_cache, v_cache, q_start, kv_len, page_table, tree_mask, positions, slopes, out,
+          workspace)
+    n = d.tokens * d.heads * d.head_dim
+    ws, ws_bytes = _scratch(workspace)
+    _check(_L.sparoa_tree_attention(
+        ctypes.byref(d), ctypes.byref(opts), _whole(q, dt, n, "q"), *_cache(d, k_cache, v_cache),
+        *_batch(d, q_start, kv_len, page_table),
+        _whole(tree_mask, torch.int64, d.tokens * -(-d.max_queries // 64), "tree_mask"),
+        _whole(positions, torch.int32, d.tokens, "positions"),
+        _whole(slopes, torch.float32, d.heads, "slopes"), _whole(out, dt, n, "out"), ws, ws_bytes,
+        _stream(stream)))
+
+
+def sparoa_kv_keep(desc, layers, q_start, kv_len, page_table, keep, kept, k_cache, v_cache,
+                   stream=None):
+    """Accepted drafts' keys and values into place, in `layers` caches (see sparoa.h);
+    keep int32 [requests, most]."""
+    d = desc
+    _here(q_start, kv_len, page_table, keep, kept, k_cache, v_cache)
+    most = keep.shape[1] if keep.dim() == 2 else 0
+    batch = _batch(d, q_start, kv_len, page_table)
+    _check(_L.sparoa_kv_keep(
+        ctypes.byref(d), layers, *batch,
+        _whole(keep, torch.int32, d.requests * most, "keep"), most,
+        _whole(kept, torch.int32, d.requests, "kept"), *_cache(d, k_cache, v_cache, layers),
+        _stream(stream)))

@@ -11,7 +11,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libsparoa.so")
 SOURCES = ["abi.cpp", "measure.hip", "gemm.hip", "fc_bw.hip", "direct.hip", "noalloc.hip",
            "pointwise.hip", "block_abi.cpp", "norm.hip", "expert_route.hip", "rows.hip", "rows_stream.hip",
-           "rows_split.hip", "rows_tile.hip"]
+           "rows_split.hip", "rows_tile.hip", "cache_abi.cpp", "cache.hip", "attention.hip"]
 OBJDIR = os.path.join(PKG, "_build")
 
 FLAGS = [

@@ -1,0 +1,649 @@
+// Attention of rows over a paged cache.
+//
+// For the rows (token, head of the group) of one request and one kv head:
+//   S^T = K Q^T by MFMA, a lane holding 16 of every 32 keys' scores of one row;
+//   p = 2^(c s - m), m the row's maximum so far, l its sum, both in the lane;
+//   O^T += V^T P^T by MFMA: the lane's own p are this product's operand, since a
+//   product over keys asks for no order of them, and V^T comes out of LDS by the
+//   transposing read.  So no score leaves its lane and a row's factors meet its
+//   outputs there.
+// Keys and values go from memory to a ring of two stages in LDS by the loads
+// themselves.  Work is cut into items (row tile, range of key tiles) of like
+// size by every work-group from the lengths on the device; the ranges of a row
+// tile that has several are joined by a second kernel.
+#include <algorithm>
+
+#include "cache.h"
+#include "rows_ring.h"
+
+namespace sparoa {
+namespace {
+
+constexpr int kThreads = 256, kWaves = 4;
+constexpr int kWaveRows = 32, kTileRows = kWaves * kWaveRows;
+constexpr int kTarget = 512;       // items that the work is cut into (two a CU)
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kSlack = 8.f;      // a maximum may lag by 2^8 before sums are scaled
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
+// Bytes of zeros: what lanes past the head's last dimension read.
+__device__ const uint4 kZeros[1] = {};
+
+// Pieces of a head: D (head_dim padded to 64, 128 or 256), key tiles of KT rows.
+template <int DT, int D>
+struct Shape {
+  static constexpr int size = Elem<DT>::size, row = D * size, vectors = row / 16;
+  static constexpr int keys = row <= 256 ? 64 : 32;
+  static constexpr int tile = keys * row, stage = 2 * tile, lds = 2 * stage;
+  static constexpr int loads = keys * vectors / (64 * kWaves);   // a wave's, of K or V
+  static constexpr int groups = lds <= 64 * 1024 && D <= 128 ? 2 : 1;   // a CU's
+};
+inline int padded_dim(int64_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
+inline int tile_keys(int64_t dim, sparoa_dtype dt) {
+  return padded_dim(dim) * elem_size(dt) <= 256 ? 64 : 32;
+}
+
+// 16 elements of K (8 a lane) of a 32 x 32 block.
+template <int DT>
+struct Piece;
+template <>
+struct Piece<SPAROA_F32> {
+  u32x4 v[2];
+};
+template <>
+struct Piece<SPAROA_F16> {
+  u32x4 v[1];
+};
+template <>
+struct Piece<SPAROA_BF16> {
+  u32x4 v[1];
+};
+template <int DT>
+__device__ __forceinline__ f32x16 mma32(const Piece<DT> &a, const Piece<DT> &b, f32x16 acc) {
+  if constexpr (DT == SPAROA_BF16) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a.v[0]),
+                                                   __builtin_bit_cast(bf16x8, b.v[0]), acc, 0, 0, 0);
+  } else if constexpr (DT == SPAROA_F16) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a.v[0]),
+                                                  __builtin_bit_cast(f16x8, b.v[0]), acc, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.v[i / 4][i % 4]),
+                                                 __uint_as_float(b.v[i / 4][i % 4]), acc, 0, 0, 0);
+    return acc;
+  }
+}
+
+// A 16-byte load whose data goes to LDS (lane l's to lds + 16 l, lds uniform); in
+// assembly so that the compiler waits where the ring does (see ring_load).
+__device__ __forceinline__ void cache_load(const void *p, uint32_t lds) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "{m0}"(lds), "v"(p) : "memory");
+}
+
+__device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
+
+// ------------------------------------------------------------ split of the work
+
+struct Item {
+  int r, start, n, len;   // request (n 0: no item), its first row, rows, keys
+  int row0;               // first row (token, group head) of the tile
+  int t0, t1;             // key tiles
+  int slot, chunk, chunks;
+};
+
+// Row tiles, key tiles and their first of a request.
+struct Load {
+  int tiles, spans, first;
+};
+__device__ __forceinline__ Load load_of(const AttnArgs &a, const KvRequest &q, int keys) {
+  Load l{0, 0, 0};
+  if (!q.n) return l;
+  l.tiles = (q.n * a.kv.group + kTileRows - 1) / kTileRows;
+  // (a tree's rows reach back from where their positions say)
+  if (a.window && !a.mask) l.first = max(0, q.len - q.n + 1 - a.window) / keys;
+  l.spans = (q.len + keys - 1) / keys - l.first;
+  return l;
+}
+
+// Key tiles of an item: the whole work over the wanted items, a row tile's at most.
+__device__ __forceinline__ int chunk_tiles(const AttnArgs &a, int keys) {
+  const int lane = threadIdx.x & 63;
+  float work = 0.f;
+  for (int r0 = 0; r0 < a.kv.requests; r0 += 64) {
+    const KvRequest q = kv_request(a.kv, min(r0 + lane, a.kv.requests - 1));
+    const Load l = load_of(a, q, keys);
+    work += r0 + lane < a.kv.requests ? (float)l.tiles * (float)l.spans : 0.f;
+  }
+#pragma unroll
+  for (int m = 32; m; m >>= 1) work += __shfl_xor(work, m);
+  work = work * (float)a.kv.kv_heads / (float)a.target;
+  return work < 1e9f ? max(1, (int)ceilf(work)) : 1 << 30;
+}
+
+// Item (or with TILES row tile that is split) number `id` of a kv head.
+template <bool TILES>
+__device__ __forceinline__ Item find_item(const AttnArgs &a, int chunk, int id, int keys) {
+  const int lane = threadIdx.x & 63;
+  Item it{};
+  int before_slots = 0;
+  for (int r0 = 0; r0 < a.kv.requests; r0 += 64) {
+    KvRequest q = kv_request(a.kv, min(r0 + lane, a.kv.requests - 1));
+    if (r0 + lane >= a.kv.requests) q.n = 0;
+    const Load l = load_of(a, q, keys);
+    const int chunks = (l.spans + chunk - 1) / chunk, items = l.tiles * chunks;
+    const int slots = chunks > 1 ? items : 0;
+    const int counted = TILES ? (chunks > 1 ? l.tiles : 0) : items;
+    const int upto = wave_prefix(counted), slots_upto = wave_prefix(slots);
+    const uint64_t past = __ballot(upto > id);
+    if (past) {
+      const int w = __builtin_ctzll(past);
+      auto at = [&](int v) { return __builtin_amdgcn_readlane(v, w); };
+      const int local = id - at(upto - counted), tiles = at(l.tiles);
+      it.r = r0 + w, it.start = at(q.start), it.n = at(q.n), it.len = at(q.len);
+      it.chunks = at(chunks);
+      // (row tiles innermost, the last rows, which see most, first)
+      it.chunk = TILES ? 0 : local / tiles;
+      const int tile = local - it.chunk * tiles;
+      it.row0 = (tiles - 1 - tile) * kTileRows;
+      it.slot = before_slots + at(slots_upto - slots) + tile;   // chunk c: + c * tiles
+      const int first = at(l.first);
+      it.t0 = first + it.chunk * chunk;
+      it.t1 = min(it.t0 + chunk, first + at(l.spans));
+      if (!TILES) it.slot += it.chunk * tiles;
+      return it;
+    }
+    id -= __builtin_amdgcn_readlane(upto, 63);
+    before_slots += __builtin_amdgcn_readlane(slots_upto, 63);
+  }
+  return it;
+}
+
+// What row (token, group head) number `row` of a request sees, and where it lies.
+struct Row {
+  bool live;
+  int token, head, pos, lo, hi;
+};
+__device__ __forceinline__ Row row_of(const AttnArgs &a, const Item &it, int kv_head, int row) {
+  Row o;
+  o.live = row < it.n * a.kv.group;
+  const int j = kv_quotient(o.live ? row : 0, a.kv.by_group);
+  o.token = it.start + j;
+  o.head = kv_head * a.kv.group + (o.live ? row : 0) - j * a.kv.group;
+  o.pos = it.len - it.n + j;
+  o.lo = 0, o.hi = it.len;
+  if (a.mask) {
+    if (a.positions) o.pos = a.positions[o.token];
+  } else if (a.causal) {
+    o.hi = min(it.len, max(o.pos + 1, a.prefix ? a.prefix[it.r] : 0));
+  }
+  if (a.window) o.lo = max(0, o.pos - a.window + 1);
+  if (a.mask) o.lo = min(o.lo, it.len - it.n);   // (bounds the context; nodes go by bits)
+  if (a.first) o.lo = max(o.lo, a.first[o.token]);
+  return o;
+}
+
+// Whether a row sees key k, and how far it is (a tree's nodes: by their bits and
+// positions).
+__device__ __forceinline__ bool sees(const AttnArgs &a, const Item &it, const Row &row, int k) {
+  if (!a.mask) return k >= row.lo && k < row.hi;
+  const int node = k - (it.len - it.n);
+  if (node < 0) return k >= row.lo;
+  if (node >= it.n) return false;
+  if (!(a.mask[(int64_t)row.token * a.mask_words + (node >> 6)] >> (node & 63) & 1)) return false;
+  return !a.window || row.pos - a.positions[it.start + node] < a.window;
+}
+__device__ __forceinline__ float distance(const AttnArgs &a, const Item &it, const Row &row,
+                                          int k) {
+  const int node = k - (it.len - it.n);
+  const int at = a.mask && node >= 0 ? a.positions[it.start + min(node, it.n - 1)] : k;
+  return fabsf((float)(row.pos - at));
+}
+
+// The score's way to log2: cap tanh(s / cap), the bias by distance.
+template <int DT>
+__device__ __forceinline__ float shaped(const AttnArgs &a, float s) {
+  s *= a.scale;
+  if (a.cap > 0.f) {
+    const float x = s / a.cap;
+    // (16-bit types: 1 - 2 / (1 + e^2x), off by 2^-23 of the cap)
+    s = a.cap * (DT == SPAROA_F32
+                     ? tanhf(x)
+                     : 1.f - 2.f * __builtin_amdgcn_rcpf(
+                                       1.f + __builtin_amdgcn_exp2f(2.f * kLog2e * x)));
+  }
+  return s * kLog2e;
+}
+
+// Outputs of one row tile's wave: lane l has row l & 31; register 16 b + r has
+// dimension 32 b + 8 (r / 4) + 4 (l >> 5) + r % 4.
+template <int DT, int D>
+__device__ __forceinline__ void store_rows(const AttnArgs &a, const Row &row, int b,
+                                           const f32x16 &o, float by) {
+  const int half = (threadIdx.x & 63) >> 5;
+  const int64_t at = ((int64_t)row.token * a.kv.heads + row.head) * a.kv.dim;
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const int d = 32 * b + 8 * g + 4 * half;
+    if (!row.live || d >= a.kv.dim) continue;
+    const float v[4] = {o[4 * g] * by, o[4 * g + 1] * by, o[4 * g + 2] * by, o[4 * g + 3] * by};
+    store_elems<DT, 4>(a.out, at + d, v);
+  }
+}
+
+template <int DT, int D>
+__global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_kernel(AttnArgs a) {
+  using S = Shape<DT, D>;
+  using E = Elem<DT>;
+  constexpr int KT = S::keys, NB = KT / 32, DB = D / 32, NV = S::vectors;
+  __shared__ __attribute__((aligned(1024))) char smem[S::lds];
+  __shared__ int reach[kWaves][2];
+
+  const int lane = threadIdx.x & 63, rl = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kv_head = blockIdx.x % a.kv.kv_heads, id = blockIdx.x / a.kv.kv_heads;
+  const int chunk = chunk_tiles(a, KT);
+  Item it = find_item<false>(a, chunk, id, KT);
+  if (!it.n) return;
+  const int slot = it.slot * a.kv.kv_heads + kv_head;
+
+  const Row row = row_of(a, it, kv_head, it.row0 + wave * kWaveRows + rl);
+  // the wave's range of keys, and the part that all its rows see
+  int lo = row.live && row.lo < row.hi ? row.lo : INT32_MAX, hi = lo < INT32_MAX ? row.hi : 0;
+  int all_lo = row.live ? row.lo : 0;
+  int all_hi = row.live ? (a.mask ? it.len - it.n : row.hi) : INT32_MAX;
+#pragma unroll
+  for (int m = 32; m; m >>= 1) {
+    lo = min(lo, __shfl_xor(lo, m)), hi = max(hi, __shfl_xor(hi, m));
+    all_lo = max(all_lo, __shfl_xor(all_lo, m)), all_hi = min(all_hi, __shfl_xor(all_hi, m));
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo), hi = __builtin_amdgcn_readfirstlane(hi);
+  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+  all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+  if (lane == 0) reach[wave][0] = lo, reach[wave][1] = hi;
+  __syncthreads();
+  int tile_lo = INT32_MAX, tile_hi = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w)
+    tile_lo = min(tile_lo, reach[w][0]), tile_hi = max(tile_hi, reach[w][1]);
+  const int t0 = __builtin_amdgcn_readfirstlane(max(it.t0, tile_lo / KT));
+  const int t1 = __builtin_amdgcn_readfirstlane(min(it.t1, (tile_hi + KT - 1) / KT));
+
+  // ---- the ring: lane i of a wave knows the cache row of a tile's key i
+  const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+  const int vectors = a.kv.dim * S::size / 16;
+  const int64_t row_bytes = (int64_t)a.kv.dim * S::size;
+  auto place = [&](int t) __attribute__((always_inline)) {   // -1: no page
+    return kv_row(a.kv, it.r, kv_head, min(t * KT + (lane & (KT - 1)), it.len - 1));
+  };
+  auto load_tile = [&](int at, int stage) __attribute__((always_inline)) {
+    at = max(at, 0);
+#pragma unroll
+    for (int u = 0; u < S::loads; ++u) {
+      const int s = (u * kWaves + wave) * 64 + lane, r = s / NV, v = s % NV;
+      const int64_t from = (int64_t)__builtin_amdgcn_ds_bpermute(4 * r, at) * row_bytes;
+      const int kv = v ^ (r & 7), vv = S::size == 2 ? v ^ (2 * (r & 3)) : kv;
+      const uint32_t to = ring + stage * S::stage + (u * kWaves + wave) * 1024;
+      const char *zeros = reinterpret_cast<const char *>(kZeros);
+      cache_load(kv < vectors ? reinterpret_cast<const char *>(a.k) + from + 16 * kv : zeros, to);
+      cache_load(vv < vectors ? reinterpret_cast<const char *>(a.v) + from + 16 * vv : zeros,
+                 to + S::tile);
+    }
+  };
+
+  // ---- the rows' queries, 16 dimensions a step
+  constexpr int STEPS = D / 16, PV = S::size / 2;   // vectors of a lane's piece
+  Piece<DT> q[STEPS];
+  {
+    const char *from = reinterpret_cast<const char *>(a.q) +
+                       ((int64_t)row.token * a.kv.heads + row.head) * row_bytes;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+      for (int e = 0; e < PV; ++e) {
+        const int v = (2 * s + half) * PV + e;
+        q[s].v[e] = v < vectors ? reinterpret_cast<const u32x4 *>(from)[v] : u32x4{0, 0, 0, 0};
+      }
+  }
+  const bool bent = a.cap > 0.f || a.slopes;
+  const float c = bent ? 1.f : a.scale * kLog2e;   // scores to log2
+  const float slope = a.slopes ? a.slopes[row.head] * kLog2e : 0.f;
+
+  f32x16 acc[DB];
+#pragma unroll
+  for (int b = 0; b < DB; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
+  float m = -__builtin_inff(), l = 0.f;   // (l: the lane's own keys)
+  bool hidden = false;                     // a tile had keys that some row does not see
+
+  int here = 0, next = 0;
+  if (t0 < t1) {
+    here = place(t0);
+    load_tile(here, 0);
+    next = place(min(t0 + 1, t1 - 1));
+  }
+  for (int t = t0; t < t1; ++t) {
+    const int stage = (t - t0) & 1;
+    __builtin_amdgcn_s_waitcnt(vm_outstanding(0));
+    __syncthreads();   // the tile is there, and the other stage is read
+    const uint64_t pageless = __ballot(here < 0);
+    here = next;
+    if (t + 1 < t1) {
+      load_tile(next, stage ^ 1);
+      next = place(min(t + 2, t1 - 1));
+    }
+    const int k0 = t * KT;
+    if (k0 >= hi || k0 + KT <= lo) continue;   // none of this wave's rows
+
+    const char *keys = smem + stage * S::stage, *values = keys + S::tile;
+    f32x16 s[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
+#pragma unroll
+      for (int st = 0; st < STEPS; ++st) {
+        Piece<DT> k;
+#pragma unroll
+        for (int e = 0; e < PV; ++e)
+          k.v[e] = *reinterpret_cast<const u32x4 *>(
+              keys + (32 * n + rl) * S::row + 16 * (((2 * st + half) * PV + e) ^ (rl & 7)));
+        s[n] = mma32<DT>(k, q[st], s[n]);
+      }
+    }
+    if (bent) {
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[n][i] = shaped<DT>(a, s[n][i]);
+          if (a.slopes)
+            s[n][i] -= slope * distance(a, it, row, k0 + 32 * n + 8 * (i / 4) + 4 * half + i % 4);
+        }
+    }
+    if (k0 < all_lo || k0 + KT > all_hi || pageless) {
+      hidden = true;
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int k = 32 * n + 8 * (i / 4) + 4 * half + i % 4;
+          if (!sees(a, it, row, k0 + k) || (pageless >> k & 1)) s[n][i] = -__builtin_inff();
+        }
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
+    top = fmaxf(top, other_half(top));
+    if (__any(top * c > m * c + kSlack)) {
+      const float to = fmaxf(m, top);
+      const float by = to == m ? 1.f : __builtin_amdgcn_exp2f((m - to) * c);
+      m = to;
+      l *= by;
+#pragma unroll
+      for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[b][i] *= by;
+    }
+    const float base = m == -__builtin_inff() ? 0.f : m * c;
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -base));
+        l += s[n][i];
+      }
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {   // 16 keys
+        Piece<DT> p;
+        if constexpr (DT == SPAROA_F32) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) p.v[i / 4][i % 4] = __float_as_uint(s[n][8 * u + i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            p.v[0][i] = E::pack2(s[n][8 * u + 2 * i], s[n][8 * u + 2 * i + 1]);
+        }
+#pragma unroll
+        for (int b = 0; b < DB; ++b) {
+          Piece<DT> v;
+          if constexpr (DT == SPAROA_F32) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int r = 32 * n + 16 * u + 8 * (i / 4) + 4 * half + i % 4;
+              v.v[i / 4][i % 4] = *reinterpret_cast<const uint32_t *>(
+                  values + r * S::row + 16 * ((8 * b + rl / 4) ^ (r & 7)) + 4 * (rl & 3));
+            }
+          } else {
+            // 16 lanes read 4 keys of 16 dimensions; lane i of them receives dimension i
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const int r = 32 * n + 16 * u + 8 * x + 4 * half + ((lane & 15) >> 2);
+              const int vec = (4 * b + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (2 * (r & 3));
+              const char *from = values + r * S::row + 16 * vec + 8 * (lane & 1);
+              const i16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                  (__attribute__((address_space(3))) i16x4 *)from);
+              const uint2 w2 = __builtin_bit_cast(uint2, w);
+              v.v[0][2 * x] = w2.x, v.v[0][2 * x + 1] = w2.y;
+            }
+          }
+          acc[b] = mma32<DT>(v, p, acc[b]);
+        }
+      }
+  }
+
+  // A weight of 0 times a hidden key's infinity or NaN is NaN: such a wave's rows
+  // are added up again, by what each of them sees.
+  if (hidden) {
+    float bad = 0.f;
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) bad = fmaf(acc[b][i], 0.f, bad);
+    if (__any(row.live && bad != 0.f)) {
+#pragma unroll
+      for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
+      const float base = m == -__builtin_inff() ? 0.f : m * c;
+      const int from = max(t0 * KT, lo), to = min(t1 * KT, hi);
+#pragma nounroll
+      for (int k = from; k < to; ++k) {
+        const int at = kv_row(a.kv, it.r, kv_head, k);
+        if (at < 0 || !(row.live && sees(a, it, row, k))) continue;
+        float x = 0.f;
+        const int64_t q0 = ((int64_t)row.token * a.kv.heads + row.head) * a.kv.dim;
+        const int64_t k0 = (int64_t)at * a.kv.dim;
+#pragma nounroll
+        for (int d = 0; d < a.kv.dim; d += 4) {
+          float qv[4], kv[4];
+          load_elems<DT, 4>(a.q, q0 + d, qv);
+          load_elems<DT, 4>(a.k, k0 + d, kv);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x = fmaf(qv[e], kv[e], x);
+        }
+        if (bent) x = shaped<DT>(a, x) - (a.slopes ? slope * distance(a, it, row, k) : 0.f);
+        const float p = __builtin_amdgcn_exp2f(fmaf(x, c, -base));
+#pragma unroll
+        for (int b = 0; b < DB; ++b)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int d = 32 * b + 8 * g + 4 * half;
+            if (d >= a.kv.dim) continue;
+            float v[4];
+            load_elems<DT, 4>(a.v, k0 + d, v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[b][4 * g + e] = fmaf(p, v[e], acc[b][4 * g + e]);
+          }
+      }
+    }
+  }
+
+  l += other_half(l);
+  if (it.chunks == 1) {
+    const float by = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int b = 0; b < DB; ++b) store_rows<DT, D>(a, row, b, acc[b], by);
+    return;
+  }
+  if (slot >= a.slots || !row.live || wave >= a.slot_waves) return;
+  const int64_t part = (int64_t)slot * a.slot_waves + wave;
+  if (half == 0)
+    reinterpret_cast<float2 *>(a.ml)[part * kWaveRows + rl] = make_float2(m * c, l);
+  if (l == 0.f) return;
+  f32x4 *const o = reinterpret_cast<f32x4 *>(a.part) + part * (4 * DB) * 64 + lane;
+#pragma unroll
+  for (int b = 0; b < DB; ++b)
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      o[(4 * b + g) * 64] =
+          f32x4{acc[b][4 * g], acc[b][4 * g + 1], acc[b][4 * g + 2], acc[b][4 * g + 3]};
+}
+
+// Joins the ranges of a row tile: out = sum_c 2^(m_c - m) o_c / sum_c 2^(m_c - m) l_c.
+// A wave takes 32 dimensions of 32 rows.
+template <int DT, int D>
+__global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a) {
+  constexpr int KT = Shape<DT, D>::keys, DB = D / 32;
+  const int lane = threadIdx.x & 63, rl = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int chunk = chunk_tiles(a, KT);
+  const int per = a.kv.kv_heads * a.slot_waves;
+  for (int u = blockIdx.x;; u += gridDim.x) {
+    const int id = u / per, kv_head = u % per % a.kv.kv_heads, w = u % per / a.kv.kv_heads;
+    const Item it = find_item<true>(a, chunk, id, KT);
+    if (!it.n) return;
+    const int rows = it.n * a.kv.group, tiles = (rows + kTileRows - 1) / kTileRows;
+    if (it.row0 + w * kWaveRows >= rows) continue;
+    const Row row = row_of(a, it, kv_head, it.row0 + w * kWaveRows + rl);
+    auto part = [&](int ch) __attribute__((always_inline)) {
+      const int slot = (it.slot + ch * tiles) * a.kv.kv_heads + kv_head;
+      return slot < a.slots ? (int64_t)slot * a.slot_waves + w : (int64_t)-1;
+    };
+    const float2 *const ml = reinterpret_cast<const float2 *>(a.ml);
+    float m = -__builtin_inff();
+    for (int ch = 0; ch < it.chunks; ++ch) {
+      const int64_t p = part(ch);
+      if (p < 0 || !row.live) continue;
+      const float2 v = ml[p * kWaveRows + rl];
+      if (v.y != 0.f) m = fmaxf(m, v.x);
+    }
+    float l = 0.f;
+    f32x16 acc[(DB + kWaves - 1) / kWaves];
+#pragma unroll
+    for (int i = 0; i < (DB + kWaves - 1) / kWaves; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
+    for (int ch = 0; ch < it.chunks; ++ch) {
+      const int64_t p = part(ch);
+      if (p < 0 || !row.live) continue;
+      const float2 v = ml[p * kWaveRows + rl];
+      if (v.y == 0.f) continue;   // (the range held nothing for this row)
+      const float by = v.x == m ? 1.f : __builtin_amdgcn_exp2f(v.x - m);
+      l = fmaf(by, v.y, l);
+      const f32x4 *const o = reinterpret_cast<const f32x4 *>(a.part) + p * (4 * DB) * 64 + lane;
+#pragma unroll
+      for (int i = 0; i < (DB + kWaves - 1) / kWaves; ++i) {
+        const int b = wave + i * kWaves;
+        if (b >= DB) break;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 x = o[(4 * b + g) * 64];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][4 * g + e] = fmaf(by, x[e], acc[i][4 * g + e]);
+        }
+      }
+    }
+    const float by = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int i = 0; i < (DB + kWaves - 1) / kWaves; ++i)
+      if (wave + i * kWaves < DB) store_rows<DT, D>(a, row, wave + i * kWaves, acc[i], by);
+  }
+}
+
+// Row tiles that the descriptor allows.
+int64_t most_tiles(const sparoa_kv_desc &d) {
+  const int64_t group = d.heads / d.kv_heads;
+  const int64_t queries = std::min(d.max_queries, d.tokens);
+  return std::min(d.requests * cdiv(queries * group, kTileRows),
+                  d.tokens * group / kTileRows + d.requests);
+}
+
+struct Split {
+  int target, slots, slot_waves;
+};
+Split attention_split(const sparoa_kv_desc &d) {
+  const int64_t group = d.heads / d.kv_heads;
+  Split s;
+  s.target = kTarget;
+  s.slot_waves = (int)std::min<int64_t>(
+      kWaves, cdiv(std::min(d.max_queries, d.tokens) * group, kWaveRows));
+  // A request's row tiles that are split have ceil(spans / chunk) < 2 spans / chunk
+  // ranges each, and all spans are at most `target` chunks.  (+ kv_heads: the work's
+  // sum is rounded.)
+  const int64_t chunks = cdiv(d.max_keys, tile_keys(d.head_dim, d.dtype));
+  const int64_t most = most_tiles(d);
+  const int64_t cap = 2 * s.target + 2 * d.kv_heads;
+  s.slots = (int)(chunks <= 1 ? 0
+                  : chunks < cap && most < cap && most * chunks < cap / d.kv_heads
+                      ? most * chunks * d.kv_heads : cap);
+  return s;
+}
+size_t ml_bytes(const Split &s) {
+  return (size_t)((int64_t)s.slots * s.slot_waves * kWaveRows * 8 + 255) / 256 * 256;
+}
+
+template <int DT, int D>
+sparoa_status launch(const AttnArgs &a, int64_t tiles, hipStream_t stream) {
+  const int64_t items = (tiles + cdiv(a.target, a.kv.kv_heads) + 1) * a.kv.kv_heads;
+  if (items > 1 << 23)
+    return fail(SPAROA_ERR_UNSUPPORTED, "attention: more than 2^23 row tiles");
+  attention_kernel<DT, D><<<(unsigned)items, kThreads, 0, stream>>>(a);
+  SPAROA_LAUNCH_CHECK("attention");
+  if (a.slots) {
+    const unsigned grid = (unsigned)std::min<int64_t>(
+        std::min<int64_t>(tiles, a.slots) * a.kv.kv_heads * a.slot_waves, 1024);
+    join_kernel<DT, D><<<grid, kThreads, 0, stream>>>(a);
+    SPAROA_LAUNCH_CHECK("attention: join");
+  }
+  return SPAROA_OK;
+}
+template <int DT>
+sparoa_status launch_dim(const AttnArgs &a, int64_t tiles, hipStream_t stream) {
+  switch (padded_dim(a.kv.dim)) {
+    case 64: return launch<DT, 64>(a, tiles, stream);
+    case 128: return launch<DT, 128>(a, tiles, stream);
+    default: return launch<DT, 256>(a, tiles, stream);
+  }
+}
+
+}  // namespace
+
+size_t attention_workspace(const sparoa_kv_desc &d) {
+  const Split s = attention_split(d);
+  return ml_bytes(s) + (size_t)((int64_t)s.slots * s.slot_waves * kWaveRows *
+                                padded_dim(d.head_dim) * 4) + 256;
+}
+
+sparoa_status launch_attention(AttnArgs a, const sparoa_kv_desc &d, void *workspace,
+                               hipStream_t stream) {
+  const Split s = attention_split(d);
+  a.target = s.target, a.slots = s.slots, a.slot_waves = s.slot_waves;
+  a.ml = workspace;
+  a.part = reinterpret_cast<char *>(workspace) + ml_bytes(s);
+  const int64_t tiles = most_tiles(d);
+  switch (d.dtype) {
+    case SPAROA_F32: return launch_dim<SPAROA_F32>(a, tiles, stream);
+    case SPAROA_F16: return launch_dim<SPAROA_F16>(a, tiles, stream);
+    default: return launch_dim<SPAROA_BF16>(a, tiles, stream);
+  }
+}
+
+}  // namespace sparoa
