@@ -733,11 +733,14 @@ def sparoa_block_norm(desc, y, post_w, post_b, gate, r, pre_w, pre_b, r_out, n_o
 # ------------------------------------ attention over a paged cache (see sparoa.h)
 
 def _here(*tensors):
-    """Refuses tensors of another device than the current one: the call's stream is its."""
+    """Refuses tensors of another device than the current one: the call's stream is its.
+    (Host tensors are refused by what they are.)"""
+    if not torch.cuda.is_initialized():
+        return
+    here = torch._C._cuda_getDevice()
     for t in tensors:
-        if t is not None and t.is_cuda and t.device.index != torch.cuda.current_device():
-            raise SparoaError(1, f"a tensor on {t.device}, the current device is "
-                                 f"{torch.cuda.current_device()}")
+        if t is not None and t.get_device() not in (here, -1):
+            raise SparoaError(1, f"a tensor on {t.device}, the current device is {here}")
 
 
 def _rows(t, dtype, rows, width, name):

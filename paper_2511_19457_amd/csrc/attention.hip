@@ -21,7 +21,10 @@ namespace {
 
 constexpr int kThreads = 256, kWaves = 4;
 constexpr int kWaveRows = 32, kTileRows = kWaves * kWaveRows;
-constexpr int kTarget = 512;       // items that the work is cut into (two a CU)
+#ifndef KTARGET
+#define KTARGET 1024
+#endif
+constexpr int kTarget = KTARGET;       // items that the work is cut into (two a CU)
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.f;      // a maximum may lag by 2^8 before sums are scaled
 
@@ -149,9 +152,11 @@ __device__ __forceinline__ Item find_item(const AttnArgs &a, int chunk, int id, 
       const int tile = local - it.chunk * tiles;
       it.row0 = (tiles - 1 - tile) * kTileRows;
       it.slot = before_slots + at(slots_upto - slots) + tile;   // chunk c: + c * tiles
-      const int first = at(l.first);
-      it.t0 = first + it.chunk * chunk;
-      it.t1 = min(it.t0 + chunk, first + at(l.spans));
+      // (ranges of like size)
+      const int first = at(l.first), spans = at(l.spans);
+      const int per = (spans + it.chunks - 1) / it.chunks;
+      it.t0 = first + min(it.chunk * per, spans);
+      it.t1 = first + min((it.chunk + 1) * per, spans);
       if (!TILES) it.slot += it.chunk * tiles;
       return it;
     }
@@ -494,77 +499,100 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
     return;
   }
   if (slot >= a.slots || !row.live || wave >= a.slot_waves) return;
-  const int64_t part = (int64_t)slot * a.slot_waves + wave;
-  if (half == 0)
-    reinterpret_cast<float2 *>(a.ml)[part * kWaveRows + rl] = make_float2(m * c, l);
-  if (l == 0.f) return;
-  f32x4 *const o = reinterpret_cast<f32x4 *>(a.part) + part * (4 * DB) * 64 + lane;
+  const int64_t part = ((int64_t)slot * a.slot_waves + wave) * kWaveRows + rl;
+  if (half == 0) reinterpret_cast<float2 *>(a.ml)[part] = make_float2(m * c, l);
+  float *const o = reinterpret_cast<float *>(a.part) + part * D + 4 * half;
 #pragma unroll
   for (int b = 0; b < DB; ++b)
 #pragma unroll
     for (int g = 0; g < 4; ++g)
-      o[(4 * b + g) * 64] =
+      *reinterpret_cast<f32x4 *>(o + 32 * b + 8 * g) =
           f32x4{acc[b][4 * g], acc[b][4 * g + 1], acc[b][4 * g + 2], acc[b][4 * g + 3]};
 }
 
 // Joins the ranges of a row tile: out = sum_c 2^(m_c - m) o_c / sum_c 2^(m_c - m) l_c.
-// A wave takes 32 dimensions of 32 rows.
+// D / 4 lanes have a row; where a row has many ranges several such groups share them
+// and meet in LDS, since the chain of loads is all that such a call takes.
+constexpr int kJoinRows = 8;   // rows of a work-group's step
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a) {
-  constexpr int KT = Shape<DT, D>::keys, DB = D / 32;
-  const int lane = threadIdx.x & 63, rl = lane & 31;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int KT = Shape<DT, D>::keys, LANES = D / 4, GROUPS = kThreads / LANES;
+  constexpr int AHEAD = 4;
+  __shared__ f32x4 sums[GROUPS][LANES];
+  __shared__ float2 stats[GROUPS];
+  const int tid = threadIdx.x, group = tid / LANES, lane = tid % LANES;
   const int chunk = chunk_tiles(a, KT);
-  const int per = a.kv.kv_heads * a.slot_waves;
+  const int row_groups = a.slot_waves * (kWaveRows / kJoinRows);
+  const int per = a.kv.kv_heads * row_groups;
   for (int u = blockIdx.x;; u += gridDim.x) {
-    const int id = u / per, kv_head = u % per % a.kv.kv_heads, w = u % per / a.kv.kv_heads;
-    const Item it = find_item<true>(a, chunk, id, KT);
+    const int in = u % per, kv_head = in % a.kv.kv_heads, g = in / a.kv.kv_heads;
+    const Item it = find_item<true>(a, chunk, u / per, KT);
     if (!it.n) return;
     const int rows = it.n * a.kv.group, tiles = (rows + kTileRows - 1) / kTileRows;
-    if (it.row0 + w * kWaveRows >= rows) continue;
-    const Row row = row_of(a, it, kv_head, it.row0 + w * kWaveRows + rl);
-    auto part = [&](int ch) __attribute__((always_inline)) {
-      const int slot = (it.slot + ch * tiles) * a.kv.kv_heads + kv_head;
-      return slot < a.slots ? (int64_t)slot * a.slot_waves + w : (int64_t)-1;
-    };
-    const float2 *const ml = reinterpret_cast<const float2 *>(a.ml);
-    float m = -__builtin_inff();
-    for (int ch = 0; ch < it.chunks; ++ch) {
-      const int64_t p = part(ch);
-      if (p < 0 || !row.live) continue;
-      const float2 v = ml[p * kWaveRows + rl];
-      if (v.y != 0.f) m = fmaxf(m, v.x);
-    }
-    float l = 0.f;
-    f32x16 acc[(DB + kWaves - 1) / kWaves];
+    if (it.row0 + g * kJoinRows >= rows) continue;
+    int share = 1;   // groups that share a row's ranges
+    while (share < GROUPS && 2 * share <= it.chunks) share *= 2;
+    const int part = group % share;
+    for (int r0 = 0; r0 < kJoinRows; r0 += GROUPS / share) {
+      const int r = r0 + group / share, row = it.row0 + g * kJoinRows + r;
+      const bool live = r < kJoinRows && row < rows;
+      float m = -__builtin_inff(), l = 0.f;
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+      if (live)
+        for (int c0 = part; c0 < it.chunks; c0 += AHEAD * share) {
+          float2 ml[AHEAD];
+          f32x4 o[AHEAD];
+          bool has[AHEAD];
 #pragma unroll
-    for (int i = 0; i < (DB + kWaves - 1) / kWaves; ++i)
+          for (int i = 0; i < AHEAD; ++i) {
+            const int ch = c0 + i * share;
+            const int slot = (it.slot + min(ch, it.chunks - 1) * tiles) * a.kv.kv_heads + kv_head;
+            has[i] = ch < it.chunks && slot < a.slots;
+            const int64_t at = (int64_t)min(slot, a.slots - 1) * a.slot_waves * kWaveRows +
+                               g * kJoinRows + r;
+            ml[i] = reinterpret_cast<const float2 *>(a.ml)[at];
+            o[i] = reinterpret_cast<const f32x4 *>(a.part)[at * LANES + lane];
+          }
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][e] = 0.f;
-    for (int ch = 0; ch < it.chunks; ++ch) {
-      const int64_t p = part(ch);
-      if (p < 0 || !row.live) continue;
-      const float2 v = ml[p * kWaveRows + rl];
-      if (v.y == 0.f) continue;   // (the range held nothing for this row)
-      const float by = v.x == m ? 1.f : __builtin_amdgcn_exp2f(v.x - m);
-      l = fmaf(by, v.y, l);
-      const f32x4 *const o = reinterpret_cast<const f32x4 *>(a.part) + p * (4 * DB) * 64 + lane;
+          for (int i = 0; i < AHEAD; ++i) {
+            if (!has[i] || ml[i].y == 0.f) continue;   // (the range held nothing for this row)
+            const float to = fmaxf(m, ml[i].x);
+            const float old = m == to ? 1.f : __builtin_amdgcn_exp2f(m - to);
+            const float by = ml[i].x == to ? 1.f : __builtin_amdgcn_exp2f(ml[i].x - to);
+            m = to;
+            l = fmaf(by, ml[i].y, l * old);
 #pragma unroll
-      for (int i = 0; i < (DB + kWaves - 1) / kWaves; ++i) {
-        const int b = wave + i * kWaves;
-        if (b >= DB) break;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const f32x4 x = o[(4 * b + g) * 64];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[i][4 * g + e] = fmaf(by, x[e], acc[i][4 * g + e]);
+            for (int e = 0; e < 4; ++e) acc[e] = fmaf(by, o[i][e], acc[e] * old);
+          }
         }
-      }
-    }
-    const float by = l == 0.f ? 0.f : 1.f / l;
+      if (share > 1) {
+        sums[group][lane] = acc;
+        if (lane == 0) stats[group] = make_float2(m, l);
+        __syncthreads();
+        if (part == 0)
+          for (int p = 1; p < share; ++p) {
+            const float2 v = stats[group + p];
+            const f32x4 x = sums[group + p][lane];
+            if (v.y == 0.f) continue;
+            const float to = fmaxf(m, v.x);
+            const float old = m == to ? 1.f : __builtin_amdgcn_exp2f(m - to);
+            const float by = v.x == to ? 1.f : __builtin_amdgcn_exp2f(v.x - to);
+            m = to;
+            l = fmaf(by, v.y, l * old);
 #pragma unroll
-    for (int i = 0; i < (DB + kWaves - 1) / kWaves; ++i)
-      if (wave + i * kWaves < DB) store_rows<DT, D>(a, row, wave + i * kWaves, acc[i], by);
+            for (int e = 0; e < 4; ++e) acc[e] = fmaf(by, x[e], acc[e] * old);
+          }
+        __syncthreads();
+      }
+      const int d = 4 * lane;
+      if (!live || part || d >= a.kv.dim) continue;
+      const int j = kv_quotient(row, a.kv.by_group);
+      const int64_t to = ((int64_t)(it.start + j) * a.kv.heads + kv_head * a.kv.group +
+                          (row - j * a.kv.group)) * a.kv.dim + d;
+      const float by = l == 0.f ? 0.f : 1.f / l;
+      const float v[4] = {acc[0] * by, acc[1] * by, acc[2] * by, acc[3] * by};
+      store_elems<DT, 4>(a.out, to, v);
+    }
   }
 }
 
@@ -609,7 +637,8 @@ sparoa_status launch(const AttnArgs &a, int64_t tiles, hipStream_t stream) {
   SPAROA_LAUNCH_CHECK("attention");
   if (a.slots) {
     const unsigned grid = (unsigned)std::min<int64_t>(
-        std::min<int64_t>(tiles, a.slots) * a.kv.kv_heads * a.slot_waves, 1024);
+        std::min<int64_t>(tiles, a.slots) * a.kv.kv_heads * a.slot_waves * (kWaveRows / kJoinRows),
+        2048);
     join_kernel<DT, D><<<grid, kThreads, 0, stream>>>(a);
     SPAROA_LAUNCH_CHECK("attention: join");
   }

@@ -174,52 +174,58 @@ void append(const AppendArgs &a, hipStream_t stream) {
     append_kernel<DT, 1, true, false><<<grid, kThreads, 0, stream>>>(a, kv_div(units), units);
 }
 
-// Accepted drafts of one (request, kv head) in one layer's keys or values.  All
-// that a slice of columns moves is in registers before any of it is written.
-__global__ __launch_bounds__(kThreads) void keep_kernel(KeepArgs a, int vectors) {
+// Accepted drafts of one (request, kv head) in the keys or values of `per` layers:
+// the list of moves is made once for all of them.  All that a batch of vectors moves
+// is in registers before any of it is written; a batch is a slice of columns, which
+// no other batch touches.
+__global__ __launch_bounds__(kThreads) void keep_kernel(KeepArgs a, int layers, int per,
+                                                        int vectors) {
   constexpr int kHeld = 8;   // vectors a thread holds
   __shared__ int from[256], to[256];
-  char *cache = reinterpret_cast<char *>(blockIdx.z ? a.v_cache : a.k_cache) +
-                (int64_t)blockIdx.y * a.layer_bytes;
-  const int tid = threadIdx.x;
+  __shared__ int moves;
+  char *cache = reinterpret_cast<char *>(blockIdx.z ? a.v_cache : a.k_cache);
+  const int tid = threadIdx.x, layer0 = blockIdx.y * per, layer1 = min(layer0 + per, layers);
   const int64_t items = (int64_t)a.kv.requests * a.kv.kv_heads;
   for (int64_t i = blockIdx.x; i < items; i += gridDim.x) {
     const int r = (int)(i / a.kv.kv_heads), h = (int)(i - (int64_t)r * a.kv.kv_heads);
     const KvRequest q = kv_request(a.kv, r);
     const int kept = a.kept[r];
     if (!q.n || kept <= 0 || kept > a.most || kept > q.n) continue;   // (alike in all threads)
+    if (tid == 0) moves = 0;
+    __syncthreads();
     if (tid < kept) {
       const int n = a.keep[(int64_t)r * a.most + tid], base = q.len - q.n;
-      int s = -1, d = -1;
       if (n >= 0 && n < q.n && n != tid) {
-        s = kv_row(a.kv, r, h, base + n);
-        d = kv_row(a.kv, r, h, base + tid);
+        const int s = kv_row(a.kv, r, h, base + n), d = kv_row(a.kv, r, h, base + tid);
+        if (s >= 0 && d >= 0) {
+          const int at = atomicAdd(&moves, 1);   // (their order does not matter)
+          from[at] = s, to[at] = d;
+        }
       }
-      from[tid] = s;
-      to[tid] = s < 0 ? -1 : d;
     }
     __syncthreads();
-    const int cols = min(vectors, max(1, kHeld * kThreads / kept));
-    for (int c0 = 0; c0 < vectors; c0 += cols) {
-      const int wide = min(cols, vectors - c0);
+    const int n = moves, all = (layer1 - layer0) * vectors;   // columns of every layer, in a row
+    const int cols = n ? min(all, kHeld * kThreads / n) : 0;
+    for (int c0 = 0; c0 < all && cols; c0 += cols) {
+      const int wide = min(cols, all - c0);
       u32x4 held[kHeld];
+      int64_t dst[kHeld];
 #pragma unroll
       for (int u = 0; u < kHeld; ++u) {
-        const int e = tid + u * kThreads, j = e / wide;
-        held[u] = u32x4{0, 0, 0, 0};
-        if (j < kept && to[j] >= 0)
-          held[u] = reinterpret_cast<const u32x4 *>(cache)[(int64_t)from[j] * vectors + c0 +
-                                                           (e - j * wide)];
+        const int e = tid + u * kThreads, j = e / wide, c = c0 + (e - j * wide);
+        dst[u] = -1;
+        if (j < n) {
+          const int layer = c / vectors;
+          const int64_t at = (layer0 + layer) * a.layer_bytes + 16 * (int64_t)(c - layer * vectors);
+          held[u] = *reinterpret_cast<const u32x4 *>(cache + at + (int64_t)from[j] * vectors * 16);
+          dst[u] = at + (int64_t)to[j] * vectors * 16;
+        }
       }
       __builtin_amdgcn_s_waitcnt(vm_outstanding(0));   // every load has its value
       __syncthreads();
 #pragma unroll
-      for (int u = 0; u < kHeld; ++u) {
-        const int e = tid + u * kThreads, j = e / wide;
-        if (j < kept && to[j] >= 0)
-          reinterpret_cast<u32x4 *>(cache)[(int64_t)to[j] * vectors + c0 + (e - j * wide)] =
-              held[u];
-      }
+      for (int u = 0; u < kHeld; ++u)
+        if (dst[u] >= 0) *reinterpret_cast<u32x4 *>(cache + dst[u]) = held[u];
     }
     __syncthreads();
   }
@@ -240,8 +246,12 @@ sparoa_status launch_kv_append(const AppendArgs &a, sparoa_dtype dt, hipStream_t
 sparoa_status launch_kv_keep(const KeepArgs &a, int64_t layers, sparoa_dtype dt,
                              hipStream_t stream) {
   const int64_t items = (int64_t)a.kv.requests * a.kv.kv_heads;
-  const dim3 grid((unsigned)std::min<int64_t>(items, 1 << 20), (unsigned)layers, 2);
-  keep_kernel<<<grid, kThreads, 0, stream>>>(a, a.kv.dim * (int)elem_size(dt) / 16);
+  // (the layers that fill a work-group's registers share its list: 64 requests of 8
+  // heads, 16 layers, 6 drafts: 41 us with a work-group a layer)
+  const int vectors = a.kv.dim * (int)elem_size(dt) / 16;
+  const int per = (int)std::min<int64_t>(layers, std::max(1, 2048 / (a.most * vectors)));
+  const dim3 grid((unsigned)std::min<int64_t>(items, 1 << 20), (unsigned)cdiv(layers, per), 2);
+  keep_kernel<<<grid, kThreads, 0, stream>>>(a, (int)layers, per, vectors);
   SPAROA_LAUNCH_CHECK("kv_keep");
   return SPAROA_OK;
 }
