@@ -19,7 +19,10 @@
 namespace sparoa {
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4;
+#ifndef NW
+#define NW 4
+#endif
+constexpr int kThreads = 64 * NW, kWaves = NW;
 constexpr int kWaveRows = 32, kTileRows = kWaves * kWaveRows;
 #ifndef KTARGET
 #define KTARGET 1024
@@ -41,7 +44,7 @@ struct Shape {
   static constexpr int keys = row <= 256 ? 64 : 32;
   static constexpr int tile = keys * row, stage = 2 * tile, lds = 2 * stage;
   static constexpr int loads = keys * vectors / (64 * kWaves);   // a wave's, of K or V
-  static constexpr int groups = lds <= 64 * 1024 && D <= 128 ? 2 : 1;   // a CU's
+  static constexpr int groups = lds <= 64 * 1024 && D <= 128 && NW == 4 ? 2 : 1;   // a CU's
 };
 inline int padded_dim(int64_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 inline int tile_keys(int64_t dim, sparoa_dtype dt) {
@@ -190,36 +193,48 @@ __device__ __forceinline__ Row row_of(const AttnArgs &a, const Item &it, int kv_
   return o;
 }
 
-// Whether a row sees key k, and how far it is (a tree's nodes: by their bits and
-// positions).
-__device__ __forceinline__ bool sees(const AttnArgs &a, const Item &it, const Row &row, int k) {
-  if (!a.mask) return k >= row.lo && k < row.hi;
-  const int node = k - (it.len - it.n);
-  if (node < 0) return k >= row.lo;
-  if (node >= it.n) return false;
-  if (!(a.mask[(int64_t)row.token * a.mask_words + (node >> 6)] >> (node & 63) & 1)) return false;
-  return !a.window || row.pos - a.positions[it.start + node] < a.window;
+// Which of the 64 keys from k0 on a row sees, a bit a key.
+__device__ __forceinline__ uint64_t low_bits(int n) {   // the n lowest, n of any size
+  return n <= 0 ? 0 : n >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << n) - 1;
 }
+__device__ __forceinline__ uint64_t seen_keys(const AttnArgs &a, const Item &it, const Row &row,
+                                              int k0) {
+  if (!a.mask) return low_bits(row.hi - k0) & ~low_bits(row.lo - k0);
+  const int context = it.len - it.n, first = k0 - context;   // the node at k0, or below 0
+  uint64_t seen = low_bits(context - k0) & ~low_bits(row.lo - k0);
+  if (first + 64 <= 0) return seen;
+  const uint64_t *words = a.mask + (int64_t)row.token * a.mask_words;
+  const int w = first >> 6, shift = first & 63;   // (w may be -1)
+  uint64_t nodes = 0;
+  if (w >= 0 && w < a.mask_words) nodes = words[w] >> shift;
+  if (shift && w + 1 < a.mask_words) nodes |= words[w + 1] << (64 - shift);
+  nodes &= low_bits(it.n - first) & ~low_bits(-first);
+  if (a.window)   // nodes that lie too far back
+#pragma nounroll
+    for (int i = max(0, -first); i < min(64, it.n - first); ++i)
+      if (row.pos - a.positions[it.start + first + i] >= a.window) nodes &= ~((uint64_t)1 << i);
+  return seen | nodes;
+}
+
+// How far a row is from key k (a tree's nodes: by their positions).
 __device__ __forceinline__ float distance(const AttnArgs &a, const Item &it, const Row &row,
                                           int k) {
-  const int node = k - (it.len - it.n);
-  const int at = a.mask && node >= 0 ? a.positions[it.start + min(node, it.n - 1)] : k;
+  int at = k;
+  if (a.mask) {
+    const int node = k - (it.len - it.n);
+    const int there = a.positions[it.start + min(max(node, 0), it.n - 1)];
+    at = node < 0 ? k : there;
+  }
   return fabsf((float)(row.pos - at));
 }
 
-// The score's way to log2: cap tanh(s / cap), the bias by distance.
+// cap tanh(s / cap)
 template <int DT>
-__device__ __forceinline__ float shaped(const AttnArgs &a, float s) {
-  s *= a.scale;
-  if (a.cap > 0.f) {
-    const float x = s / a.cap;
-    // (16-bit types: 1 - 2 / (1 + e^2x), off by 2^-23 of the cap)
-    s = a.cap * (DT == SPAROA_F32
-                     ? tanhf(x)
-                     : 1.f - 2.f * __builtin_amdgcn_rcpf(
-                                       1.f + __builtin_amdgcn_exp2f(2.f * kLog2e * x)));
-  }
-  return s * kLog2e;
+__device__ __forceinline__ float capped(float s, float cap, float by) {
+  // (16-bit types: 1 - 2 / (1 + e^2x), off by 2^-23 of the cap)
+  if constexpr (DT == SPAROA_F32) return cap * tanhf(s * by);
+  return cap - 2.f * cap * __builtin_amdgcn_rcpf(
+                               1.f + __builtin_amdgcn_exp2f(2.f * kLog2e * by * s));
 }
 
 // Outputs of one row tile's wave: lane l has row l & 31; register 16 b + r has
@@ -239,7 +254,7 @@ __device__ __forceinline__ void store_rows(const AttnArgs &a, const Row &row, in
 }
 
 template <int DT, int D>
-__global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kThreads, (NW / 4 * Shape<DT, D>::groups)) void attention_kernel(AttnArgs a) {
   using S = Shape<DT, D>;
   using E = Elem<DT>;
   constexpr int KT = S::keys, NB = KT / 32, DB = D / 32, NV = S::vectors;
@@ -279,16 +294,28 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
   // ---- the ring: lane i of a wave knows the cache row of a tile's key i
   const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
   const int vectors = a.kv.dim * S::size / 16;
-  const int64_t row_bytes = (int64_t)a.kv.dim * S::size;
-  auto place = [&](int t) __attribute__((always_inline)) {   // -1: no page
-    return kv_row(a.kv, it.r, kv_head, min(t * KT + (lane & (KT - 1)), it.len - 1));
+  const uint32_t row_bytes = (uint32_t)a.kv.dim * S::size;
+  // (the page's number is only asked for; made use of a tile later, since its wait
+  // would be one for the tile that was sent for before it, too)
+  auto key_of = [&](int t) __attribute__((always_inline)) {
+    return min(t * KT + (lane & (KT - 1)), it.len - 1);
+  };
+  const int32_t *const pages = a.kv.table + (int64_t)it.r * a.kv.table_pages;
+  auto ask = [&](int t) __attribute__((always_inline)) {
+    return pages[kv_quotient(key_of(t), a.kv.by_page)];
+  };
+  auto place = [&](int t, int page) __attribute__((always_inline)) {   // -1: no page
+    const int k = key_of(t), in = kv_quotient(k, a.kv.by_page);
+    const uint32_t at = ((uint32_t)page * a.kv.kv_heads + kv_head) * a.kv.page_size +
+                        (k - in * a.kv.page_size);
+    return (uint32_t)page < (uint32_t)a.kv.pages ? (int)at : -1;
   };
   auto load_tile = [&](int at, int stage) __attribute__((always_inline)) {
     at = max(at, 0);
 #pragma unroll
     for (int u = 0; u < S::loads; ++u) {
       const int s = (u * kWaves + wave) * 64 + lane, r = s / NV, v = s % NV;
-      const int64_t from = (int64_t)__builtin_amdgcn_ds_bpermute(4 * r, at) * row_bytes;
+      const uint64_t from = (uint64_t)(uint32_t)__builtin_amdgcn_ds_bpermute(4 * r, at) * row_bytes;
       const int kv = v ^ (r & 7), vv = S::size == 2 ? v ^ (2 * (r & 3)) : kv;
       const uint32_t to = ring + stage * S::stage + (u * kWaves + wave) * 1024;
       const char *zeros = reinterpret_cast<const char *>(kZeros);
@@ -312,9 +339,11 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
         q[s].v[e] = v < vectors ? reinterpret_cast<const u32x4 *>(from)[v] : u32x4{0, 0, 0, 0};
       }
   }
-  const bool bent = a.cap > 0.f || a.slopes;
-  const float c = bent ? 1.f : a.scale * kLog2e;   // scores to log2
-  const float slope = a.slopes ? a.slopes[row.head] * kLog2e : 0.f;
+  // scores to log2: 2^(c s), s the product, or cap tanh(scale product / cap); the bias
+  // by distance in units of 1 / c
+  const float c = a.cap > 0.f ? kLog2e : a.scale * kLog2e;
+  const float cap_by = a.cap > 0.f ? a.scale / a.cap : 0.f;
+  const float slope = a.slopes ? a.slopes[row.head] / (a.cap > 0.f ? 1.f : a.scale) : 0.f;
 
   f32x16 acc[DB];
 #pragma unroll
@@ -324,21 +353,21 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
   float m = -__builtin_inff(), l = 0.f;   // (l: the lane's own keys)
   bool hidden = false;                     // a tile had keys that some row does not see
 
-  int here = 0, next = 0;
+  int here = 0, page = 0;
   if (t0 < t1) {
-    here = place(t0);
+    here = place(t0, ask(t0));
     load_tile(here, 0);
-    next = place(min(t0 + 1, t1 - 1));
+    page = ask(min(t0 + 1, t1 - 1));
   }
   for (int t = t0; t < t1; ++t) {
     const int stage = (t - t0) & 1;
     __builtin_amdgcn_s_waitcnt(vm_outstanding(0));
     __syncthreads();   // the tile is there, and the other stage is read
     const uint64_t pageless = __ballot(here < 0);
-    here = next;
     if (t + 1 < t1) {
-      load_tile(next, stage ^ 1);
-      next = place(min(t + 2, t1 - 1));
+      here = place(t + 1, page);
+      load_tile(here, stage ^ 1);
+      page = ask(min(t + 2, t1 - 1));
     }
     const int k0 = t * KT;
     if (k0 >= hi || k0 + KT <= lo) continue;   // none of this wave's rows
@@ -359,25 +388,42 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
         s[n] = mma32<DT>(k, q[st], s[n]);
       }
     }
-    if (bent) {
+    if (a.cap > 0.f) {
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[n][i] = shaped<DT>(a, s[n][i]);
-          if (a.slopes)
-            s[n][i] -= slope * distance(a, it, row, k0 + 32 * n + 8 * (i / 4) + 4 * half + i % 4);
-        }
+        for (int i = 0; i < 16; ++i) s[n][i] = capped<DT>(s[n][i], a.cap, cap_by);
+    }
+    if (a.slopes) {   // (scores are in units of 1 / c here)
+      if (!a.mask || k0 + KT <= it.len - it.n) {
+        const int from = row.pos - k0 - 4 * half;
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            s[n][i] = fmaf(-slope, fabsf((float)(from - (32 * n + 8 * (i / 4) + i % 4))), s[n][i]);
+      } else {
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            s[n][i] = fmaf(-slope,
+                           distance(a, it, row, k0 + 32 * n + 8 * (i / 4) + 4 * half + i % 4),
+                           s[n][i]);
+      }
     }
     if (k0 < all_lo || k0 + KT > all_hi || pageless) {
       hidden = true;
+      const uint64_t seen = (seen_keys(a, it, row, k0) & ~pageless) >> (4 * half);
 #pragma unroll
-      for (int n = 0; n < NB; ++n)
+      for (int n = 0; n < NB; ++n) {
+        const int bits = (int)(uint32_t)(seen >> (32 * n));
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int k = 32 * n + 8 * (i / 4) + 4 * half + i % 4;
-          if (!sees(a, it, row, k0 + k) || (pageless >> k & 1)) s[n][i] = -__builtin_inff();
+        for (int i = 0; i < 16; ++i) {   // the bit as a mask: the score, or -infinity
+          const int b = 8 * (i / 4) + i % 4, keep = (int)((uint32_t)bits << (31 - b)) >> 31;
+          s[n][i] = __int_as_float((__float_as_int(s[n][i]) & keep) | (~keep & (int)0xFF800000));
         }
+      }
     }
     float top = s[0][0];
 #pragma unroll
@@ -462,7 +508,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
 #pragma nounroll
       for (int k = from; k < to; ++k) {
         const int at = kv_row(a.kv, it.r, kv_head, k);
-        if (at < 0 || !(row.live && sees(a, it, row, k))) continue;
+        if (at < 0 || !(row.live && (seen_keys(a, it, row, k) & 1))) continue;
         float x = 0.f;
         const int64_t q0 = ((int64_t)row.token * a.kv.heads + row.head) * a.kv.dim;
         const int64_t k0 = (int64_t)at * a.kv.dim;
@@ -474,7 +520,8 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
 #pragma unroll
           for (int e = 0; e < 4; ++e) x = fmaf(qv[e], kv[e], x);
         }
-        if (bent) x = shaped<DT>(a, x) - (a.slopes ? slope * distance(a, it, row, k) : 0.f);
+        if (a.cap > 0.f) x = capped<DT>(x, a.cap, cap_by);
+        if (a.slopes) x = fmaf(-slope, distance(a, it, row, k), x);
         const float p = __builtin_amdgcn_exp2f(fmaf(x, c, -base));
 #pragma unroll
         for (int b = 0; b < DB; ++b)
