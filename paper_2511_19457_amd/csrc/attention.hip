@@ -44,6 +44,14 @@ struct Shape {
   static constexpr int keys = row <= 256 ? 64 : 32;
   static constexpr int tile = keys * row, stage = 2 * tile, lds = 2 * stage;
   static constexpr int loads = keys * vectors / (64 * kWaves);   // a wave's, of K or V
+  // Vector v of a tile's row r lies at vector v ^ (swizzle of r): LDS has 64 banks of 4
+  // bytes, and the lanes that are served together (16 of 16 bytes: 16 rows of K; 32 of
+  // 8: 4 rows of 64 bytes of V; 64 of 4: 2 rows of 128) shall meet all of them.
+  __device__ static constexpr int swizzle_k(int r) { return vectors % 16 ? r >> 1 & 7 : r & 15; }
+  __device__ static constexpr int swizzle_v(int r) {
+    if (size == 4) return vectors % 16 ? 0 : 8 * (r >> 2 & 1);
+    return vectors % 16 ? 4 * (r >> 1 & 1) : 4 * (r & 3);
+  }
   static constexpr int groups = lds <= 64 * 1024 && D <= 128 && NW == 4 ? 2 : 1;   // a CU's
 };
 inline int padded_dim(int64_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
@@ -316,7 +324,7 @@ __global__ __launch_bounds__(kThreads, (NW / 4 * Shape<DT, D>::groups)) void att
     for (int u = 0; u < S::loads; ++u) {
       const int s = (u * kWaves + wave) * 64 + lane, r = s / NV, v = s % NV;
       const uint64_t from = (uint64_t)(uint32_t)__builtin_amdgcn_ds_bpermute(4 * r, at) * row_bytes;
-      const int kv = v ^ (r & 7), vv = S::size == 2 ? v ^ (2 * (r & 3)) : kv;
+      const int kv = v ^ S::swizzle_k(r), vv = v ^ S::swizzle_v(r);
       const uint32_t to = ring + stage * S::stage + (u * kWaves + wave) * 1024;
       const char *zeros = reinterpret_cast<const char *>(kZeros);
       cache_load(kv < vectors ? reinterpret_cast<const char *>(a.k) + from + 16 * kv : zeros, to);
@@ -384,7 +392,8 @@ __global__ __launch_bounds__(kThreads, (NW / 4 * Shape<DT, D>::groups)) void att
 #pragma unroll
         for (int e = 0; e < PV; ++e)
           k.v[e] = *reinterpret_cast<const u32x4 *>(
-              keys + (32 * n + rl) * S::row + 16 * (((2 * st + half) * PV + e) ^ (rl & 7)));
+              keys + (32 * n + rl) * S::row +
+              16 * (((2 * st + half) * PV + e) ^ S::swizzle_k(rl)));
         s[n] = mma32<DT>(k, q[st], s[n]);
       }
     }
@@ -470,14 +479,14 @@ __global__ __launch_bounds__(kThreads, (NW / 4 * Shape<DT, D>::groups)) void att
             for (int i = 0; i < 8; ++i) {
               const int r = 32 * n + 16 * u + 8 * (i / 4) + 4 * half + i % 4;
               v.v[i / 4][i % 4] = *reinterpret_cast<const uint32_t *>(
-                  values + r * S::row + 16 * ((8 * b + rl / 4) ^ (r & 7)) + 4 * (rl & 3));
+                  values + r * S::row + 16 * ((8 * b + rl / 4) ^ S::swizzle_v(r)) + 4 * (rl & 3));
             }
           } else {
             // 16 lanes read 4 keys of 16 dimensions; lane i of them receives dimension i
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
               const int r = 32 * n + 16 * u + 8 * x + 4 * half + ((lane & 15) >> 2);
-              const int vec = (4 * b + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (2 * (r & 3));
+              const int vec = (4 * b + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ S::swizzle_v(r);
               const char *from = values + r * S::row + 16 * vec + 8 * (lane & 1);
               const i16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                   (__attribute__((address_space(3))) i16x4 *)from);
