@@ -19,15 +19,15 @@
 namespace sparoa {
 namespace {
 
-#ifndef NW
-#define NW 4
-#endif
-constexpr int kThreads = 64 * NW, kWaves = NW;
+constexpr int kThreads = 256, kWaves = 4;
 constexpr int kWaveRows = 32, kTileRows = kWaves * kWaveRows;
-#ifndef KTARGET
-#define KTARGET 1024
-#endif
-constexpr int kTarget = KTARGET;       // items that the work is cut into (two a CU)
+constexpr int kMaxRanges = 64;     // of a row: a step of the join
+// Items that the work is cut into.  Few rows: small ranges even the load out and cost
+// little; many: a range's outputs pass through memory, so a row tile is cut only where
+// it is longer than what 320 of the 512 resident work-groups would have each (64
+// decoding requests: 512 237 us, 768 217, 1024 222, 2048 223; 12 chunks of prompts: 256
+// 65, 320 65, 512 81; 32 trees: 169, 150, 166).
+constexpr int kTargetFew = 1024, kTargetMany = 320;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.f;      // a maximum may lag by 2^8 before sums are scaled
 
@@ -52,7 +52,7 @@ struct Shape {
     if (size == 4) return vectors % 16 ? 0 : 8 * (r >> 2 & 1);
     return vectors % 16 ? 4 * (r >> 1 & 1) : 4 * (r & 3);
   }
-  static constexpr int groups = lds <= 64 * 1024 && D <= 128 && NW == 4 ? 2 : 1;   // a CU's
+  static constexpr int groups = lds <= 64 * 1024 && D <= 128 ? 2 : 1;   // a CU's
 };
 inline int padded_dim(int64_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 inline int tile_keys(int64_t dim, sparoa_dtype dt) {
@@ -137,6 +137,16 @@ __device__ __forceinline__ int chunk_tiles(const AttnArgs &a, int keys) {
   return work < 1e9f ? max(1, (int)ceilf(work)) : 1 << 30;
 }
 
+// Ranges of a request's row tiles.  A range's outputs pass through memory twice (4
+// bytes each), which shall not be more than its keys and values do.
+__device__ __forceinline__ int ranges_of(const AttnArgs &a, const KvRequest &q, const Load &l,
+                                         int chunk, int keys) {
+  const int rows = min(q.n * a.kv.group, kTileRows);
+  const int least = (rows * 4 + keys * a.elem - 1) / (keys * a.elem);
+  const int size = max(max(chunk, least), (l.spans + kMaxRanges - 1) / kMaxRanges);
+  return (l.spans + size - 1) / size;
+}
+
 // Item (or with TILES row tile that is split) number `id` of a kv head.
 template <bool TILES>
 __device__ __forceinline__ Item find_item(const AttnArgs &a, int chunk, int id, int keys) {
@@ -147,7 +157,7 @@ __device__ __forceinline__ Item find_item(const AttnArgs &a, int chunk, int id, 
     KvRequest q = kv_request(a.kv, min(r0 + lane, a.kv.requests - 1));
     if (r0 + lane >= a.kv.requests) q.n = 0;
     const Load l = load_of(a, q, keys);
-    const int chunks = (l.spans + chunk - 1) / chunk, items = l.tiles * chunks;
+    const int chunks = ranges_of(a, q, l, chunk, keys), items = l.tiles * chunks;
     const int slots = chunks > 1 ? items : 0;
     const int counted = TILES ? (chunks > 1 ? l.tiles : 0) : items;
     const int upto = wave_prefix(counted), slots_upto = wave_prefix(slots);
@@ -262,7 +272,7 @@ __device__ __forceinline__ void store_rows(const AttnArgs &a, const Row &row, in
 }
 
 template <int DT, int D>
-__global__ __launch_bounds__(kThreads, (NW / 4 * Shape<DT, D>::groups)) void attention_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_kernel(AttnArgs a) {
   using S = Shape<DT, D>;
   using E = Elem<DT>;
   constexpr int KT = S::keys, NB = KT / 32, DB = D / 32, NV = S::vectors;
@@ -569,29 +579,28 @@ __global__ __launch_bounds__(kThreads, (NW / 4 * Shape<DT, D>::groups)) void att
 // Joins the ranges of a row tile: out = sum_c 2^(m_c - m) o_c / sum_c 2^(m_c - m) l_c.
 // D / 4 lanes have a row; where a row has many ranges several such groups share them
 // and meet in LDS, since the chain of loads is all that such a call takes.
-constexpr int kJoinRows = 8;   // rows of a work-group's step
 template <int DT, int D>
-__global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a, int step) {
   constexpr int KT = Shape<DT, D>::keys, LANES = D / 4, GROUPS = kThreads / LANES;
-  constexpr int AHEAD = 4;
+  constexpr int AHEAD = 8;
   __shared__ f32x4 sums[GROUPS][LANES];
   __shared__ float2 stats[GROUPS];
   const int tid = threadIdx.x, group = tid / LANES, lane = tid % LANES;
   const int chunk = chunk_tiles(a, KT);
-  const int row_groups = a.slot_waves * (kWaveRows / kJoinRows);
+  const int row_groups = (a.tile_rows + step - 1) / step;
   const int per = a.kv.kv_heads * row_groups;
   for (int u = blockIdx.x;; u += gridDim.x) {
     const int in = u % per, kv_head = in % a.kv.kv_heads, g = in / a.kv.kv_heads;
     const Item it = find_item<true>(a, chunk, u / per, KT);
     if (!it.n) return;
     const int rows = it.n * a.kv.group, tiles = (rows + kTileRows - 1) / kTileRows;
-    if (it.row0 + g * kJoinRows >= rows) continue;
+    if (it.row0 + g * step >= rows) continue;
     int share = 1;   // groups that share a row's ranges
-    while (share < GROUPS && 2 * share <= it.chunks) share *= 2;
+    while (share * step < GROUPS && 2 * share <= it.chunks) share *= 2;
     const int part = group % share;
-    for (int r0 = 0; r0 < kJoinRows; r0 += GROUPS / share) {
-      const int r = r0 + group / share, row = it.row0 + g * kJoinRows + r;
-      const bool live = r < kJoinRows && row < rows;
+    for (int r0 = 0; r0 < step; r0 += GROUPS / share) {
+      const int r = r0 + group / share, row = it.row0 + g * step + r;
+      const bool live = r < step && row < rows;
       float m = -__builtin_inff(), l = 0.f;
       f32x4 acc = {0.f, 0.f, 0.f, 0.f};
       if (live)
@@ -605,7 +614,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a) {
             const int slot = (it.slot + min(ch, it.chunks - 1) * tiles) * a.kv.kv_heads + kv_head;
             has[i] = ch < it.chunks && slot < a.slots;
             const int64_t at = (int64_t)min(slot, a.slots - 1) * a.slot_waves * kWaveRows +
-                               g * kJoinRows + r;
+                               g * step + r;
             ml[i] = reinterpret_cast<const float2 *>(a.ml)[at];
             o[i] = reinterpret_cast<const f32x4 *>(a.part)[at * LANES + lane];
           }
@@ -666,9 +675,9 @@ struct Split {
 Split attention_split(const sparoa_kv_desc &d) {
   const int64_t group = d.heads / d.kv_heads;
   Split s;
-  s.target = kTarget;
   s.slot_waves = (int)std::min<int64_t>(
       kWaves, cdiv(std::min(d.max_queries, d.tokens) * group, kWaveRows));
+  s.target = s.slot_waves == 1 ? kTargetFew : kTargetMany;
   // A request's row tiles that are split have ceil(spans / chunk) < 2 spans / chunk
   // ranges each, and all spans are at most `target` chunks.  (+ kv_heads: the work's
   // sum is rounded.)
@@ -692,10 +701,12 @@ sparoa_status launch(const AttnArgs &a, int64_t tiles, hipStream_t stream) {
   attention_kernel<DT, D><<<(unsigned)items, kThreads, 0, stream>>>(a);
   SPAROA_LAUNCH_CHECK("attention");
   if (a.slots) {
+    // (few rows: a work-group a row; many: the lookups are made for 8)
+    const int step = a.slot_waves == 1 ? 1 : a.slot_waves == 2 ? 4 : 8;
     const unsigned grid = (unsigned)std::min<int64_t>(
-        std::min<int64_t>(tiles, a.slots) * a.kv.kv_heads * a.slot_waves * (kWaveRows / kJoinRows),
+        std::min<int64_t>(tiles, a.slots) * a.kv.kv_heads * cdiv(a.tile_rows, step),
         2048);
-    join_kernel<DT, D><<<grid, kThreads, 0, stream>>>(a);
+    join_kernel<DT, D><<<grid, kThreads, 0, stream>>>(a, step);
     SPAROA_LAUNCH_CHECK("attention: join");
   }
   return SPAROA_OK;
@@ -721,6 +732,8 @@ sparoa_status launch_attention(AttnArgs a, const sparoa_kv_desc &d, void *worksp
                                hipStream_t stream) {
   const Split s = attention_split(d);
   a.target = s.target, a.slots = s.slots, a.slot_waves = s.slot_waves;
+  a.elem = (int)elem_size(d.dtype);
+  a.tile_rows = (int)std::min<int64_t>(kTileRows, (int64_t)a.kv.max_queries * a.kv.group);
   a.ml = workspace;
   a.part = reinterpret_cast<char *>(workspace) + ml_bytes(s);
   const int64_t tiles = most_tiles(d);

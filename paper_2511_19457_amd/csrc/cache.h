@@ -84,6 +84,8 @@ struct AttnArgs {
   int window, causal;
   // how the work is split (attention_split)
   int target, slots, slot_waves;
+  int elem;                // bytes of an element
+  int tile_rows;           // rows of a tile at most
   void *ml, *part;         // workspace: (maximum, sum) of rows, unscaled outputs
 };
 size_t attention_workspace(const sparoa_kv_desc &d);
