@@ -94,7 +94,7 @@ __device__ __forceinline__ f32x16 mma32(const Piece<DT> &a, const Piece<DT> &b, 
 // A 16-byte load whose data goes to LDS (lane l's to lds + 16 l, lds uniform); in
 // assembly so that the compiler waits where the ring does (see ring_load).
 __device__ __forceinline__ void cache_load(const void *p, uint32_t lds) {
-  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "{m0}"(lds), "v"(p) : "memory");
+  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %1, off" : : "{m0}"(lds), "v"(p) : "memory");
 }
 
 __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32); }
@@ -328,19 +328,24 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
                         (k - in * a.kv.page_size);
     return (uint32_t)page < (uint32_t)a.kv.pages ? (int)at : -1;
   };
-  auto load_tile = [&](int at, int stage) __attribute__((always_inline)) {
-    at = max(at, 0);
+  auto load_rows = [&](const void *cache, int swizzle(int), const int (&at)[S::loads], uint32_t to)
+                       __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < S::loads; ++u) {
-      const int s = (u * kWaves + wave) * 64 + lane, r = s / NV, v = s % NV;
-      const uint64_t from = (uint64_t)(uint32_t)__builtin_amdgcn_ds_bpermute(4 * r, at) * row_bytes;
-      const int kv = v ^ S::swizzle_k(r), vv = v ^ S::swizzle_v(r);
-      const uint32_t to = ring + stage * S::stage + (u * kWaves + wave) * 1024;
-      const char *zeros = reinterpret_cast<const char *>(kZeros);
-      cache_load(kv < vectors ? reinterpret_cast<const char *>(a.k) + from + 16 * kv : zeros, to);
-      cache_load(vv < vectors ? reinterpret_cast<const char *>(a.v) + from + 16 * vv : zeros,
-                 to + S::tile);
+      const int s = (u * kWaves + wave) * 64 + lane, r = s / NV, v = (s % NV) ^ swizzle(r);
+      const char *const first = v < vectors ? reinterpret_cast<const char *>(cache) + 16 * v
+                                            : reinterpret_cast<const char *>(kZeros);
+      cache_load(first + (uint64_t)(uint32_t)at[u] * (v < vectors ? row_bytes : 0),
+                 to + (u * kWaves + wave) * 1024);
     }
+  };
+  auto load_tile = [&](int at, int stage) __attribute__((always_inline)) {
+    int row[S::loads];
+#pragma unroll
+    for (int u = 0; u < S::loads; ++u)
+      row[u] = __builtin_amdgcn_ds_bpermute(4 * (((u * kWaves + wave) * 64 + lane) / NV), max(at, 0));
+    load_rows(a.k, [](int r) { return S::swizzle_k(r); }, row, ring + stage * S::stage);
+    load_rows(a.v, [](int r) { return S::swizzle_v(r); }, row, ring + stage * S::stage + S::tile);
   };
 
   // ---- the rows' queries, 16 dimensions a step
@@ -391,20 +396,26 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
     if (k0 >= hi || k0 + KT <= lo) continue;   // none of this wave's rows
 
     const char *keys = smem + stage * S::stage, *values = keys + S::tile;
+    constexpr int KA = 2, VA = 2;   // pieces that are read before their product
     f32x16 s[NB];
+    {
+      Piece<DT> k[KA + 1];
 #pragma unroll
-    for (int n = 0; n < NB; ++n) {
+      for (int i = 0; i < NB * STEPS + KA; ++i) {   // (NB sums in turn: no product waits for one)
+        if (i < NB * STEPS) {
+          const int n = i % NB, st = i / NB;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
+          for (int e = 0; e < PV; ++e)
+            k[i % (KA + 1)].v[e] = *reinterpret_cast<const u32x4 *>(
+                keys + (32 * n + rl) * S::row +
+                16 * (((2 * st + half) * PV + e) ^ S::swizzle_k(rl)));
+        }
+        if (i < KA) continue;
+        const int n = (i - KA) % NB, st = (i - KA) / NB;
+        if (st == 0)
 #pragma unroll
-      for (int st = 0; st < STEPS; ++st) {
-        Piece<DT> k;
-#pragma unroll
-        for (int e = 0; e < PV; ++e)
-          k.v[e] = *reinterpret_cast<const u32x4 *>(
-              keys + (32 * n + rl) * S::row +
-              16 * (((2 * st + half) * PV + e) ^ S::swizzle_k(rl)));
-        s[n] = mma32<DT>(k, q[st], s[n]);
+          for (int e = 0; e < 16; ++e) s[n][e] = 0.f;
+        s[n] = mma32<DT>(k[(i - KA) % (KA + 1)], q[st], s[n]);
       }
     }
     if (a.cap > 0.f) {
@@ -468,45 +479,47 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
         s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -base));
         l += s[n][i];
       }
+    Piece<DT> v[VA + 1], p;
 #pragma unroll
-    for (int n = 0; n < NB; ++n)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {   // 16 keys
-        Piece<DT> p;
+    for (int i = 0; i < 2 * NB * DB + VA; ++i) {   // 16 keys of 32 dimensions
+      if (i < 2 * NB * DB) {
+        const int k0 = 16 * (i / DB), b = i % DB;
         if constexpr (DT == SPAROA_F32) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) p.v[i / 4][i % 4] = __float_as_uint(s[n][8 * u + i]);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            p.v[0][i] = E::pack2(s[n][8 * u + 2 * i], s[n][8 * u + 2 * i + 1]);
-        }
-#pragma unroll
-        for (int b = 0; b < DB; ++b) {
-          Piece<DT> v;
-          if constexpr (DT == SPAROA_F32) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int r = 32 * n + 16 * u + 8 * (i / 4) + 4 * half + i % 4;
-              v.v[i / 4][i % 4] = *reinterpret_cast<const uint32_t *>(
-                  values + r * S::row + 16 * ((8 * b + rl / 4) ^ S::swizzle_v(r)) + 4 * (rl & 3));
-            }
-          } else {
-            // 16 lanes read 4 keys of 16 dimensions; lane i of them receives dimension i
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              const int r = 32 * n + 16 * u + 8 * x + 4 * half + ((lane & 15) >> 2);
-              const int vec = (4 * b + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ S::swizzle_v(r);
-              const char *from = values + r * S::row + 16 * vec + 8 * (lane & 1);
-              const i16x4 w = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                  (__attribute__((address_space(3))) i16x4 *)from);
-              const uint2 w2 = __builtin_bit_cast(uint2, w);
-              v.v[0][2 * x] = w2.x, v.v[0][2 * x + 1] = w2.y;
-            }
+          for (int e = 0; e < 8; ++e) {
+            const int r = k0 + 8 * (e / 4) + 4 * half + e % 4;
+            v[i % (VA + 1)].v[e / 4][e % 4] = *reinterpret_cast<const uint32_t *>(
+                values + r * S::row + 16 * ((8 * b + rl / 4) ^ S::swizzle_v(r)) + 4 * (rl & 3));
           }
-          acc[b] = mma32<DT>(v, p, acc[b]);
+        } else {
+          // 16 lanes read 4 keys of 16 dimensions; lane i of them receives dimension i
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const int r = k0 + 8 * x + 4 * half + ((lane & 15) >> 2);
+            const int vec = (4 * b + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ S::swizzle_v(r);
+            const char *from = values + r * S::row + 16 * vec + 8 * (lane & 1);
+            const uint2 w = __builtin_bit_cast(
+                uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                           (__attribute__((address_space(3))) i16x4 *)from));
+            v[i % (VA + 1)].v[0][2 * x] = w.x, v[i % (VA + 1)].v[0][2 * x + 1] = w.y;
+          }
         }
       }
+      if (i < VA) continue;
+      const int j = i - VA, u = j / DB, b = j % DB;
+      if (b == 0) {   // the lane's weights of these keys
+        if constexpr (DT == SPAROA_F32) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            p.v[e / 4][e % 4] = __float_as_uint(s[u / 2][8 * (u & 1) + e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            p.v[0][e] = E::pack2(s[u / 2][8 * (u & 1) + 2 * e], s[u / 2][8 * (u & 1) + 2 * e + 1]);
+        }
+      }
+      acc[b] = mma32<DT>(v[j % (VA + 1)], p, acc[b]);
+    }
   }
 
   // A weight of 0 times a hidden key's infinity or NaN is NaN: such a wave's rows
