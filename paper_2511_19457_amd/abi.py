@@ -732,24 +732,30 @@ def sparoa_block_norm(desc, y, post_w, post_b, gate, r, pre_w, pre_b, r_out, n_o
 
 # ------------------------------------ attention over a paged cache (see sparoa.h)
 
-def _here(*tensors):
-    """Refuses tensors of another device than the current one: the call's stream is its.
-    (Host tensors are refused by what they are.)"""
-    if not torch.cuda.is_initialized():
-        return
-    here = torch._C._cuda_getDevice()
-    for t in tensors:
-        if t is not None and t.get_device() not in (here, -1):
-            raise SparoaError(1, f"a tensor on {t.device}, the current device is {here}")
+def _device():
+    """Index of the current device, whose stream a call is enqueued on (-2: no device yet)."""
+    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
 
 
-def _rows(t, dtype, rows, width, name):
+def _on(t, dtype, numel, name, here):
+    """As _whole, of the current device `here`."""
+    if t is None:
+        return None
+    if t.get_device() != here or t.dtype is not dtype or t.numel() != numel \
+            or not t.is_contiguous():
+        _whole(t, dtype, numel, name)
+        raise SparoaError(1, f"{name}: a tensor on {t.device}, the current device is {here}")
+    return t.data_ptr()
+
+
+def _rows(t, dtype, rows, width, name, here):
     """Pointer and row stride of a [rows, width] view whose rows are dense."""
-    if t.dim() != 2 or t.dtype is not dtype or tuple(t.shape) != (rows, width) or not t.is_cuda \
+    if t.get_device() != here or t.dtype is not dtype or t.dim() != 2 \
+            or t.shape[0] != rows or t.shape[1] != width or here < 0 \
             or (width > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < width):
-        raise SparoaError(1, f"{name}: a {dtype} device tensor [{rows}, {width}] with dense rows "
-                             f"is wanted, got {t.dtype} {tuple(t.shape)} with strides "
-                             f"{t.stride()} on {t.device}")
+        raise SparoaError(1, f"{name}: a {dtype} tensor [{rows}, {width}] with dense rows on the "
+                             f"current device is wanted, got {t.dtype} {tuple(t.shape)} with "
+                             f"strides {t.stride()} on {t.device}")
     return t.data_ptr(), t.stride(0) if rows > 1 else width
 
 
@@ -768,15 +774,23 @@ def attention_opts(scale, cap=0.0, window=0, causal=True):
     return AttentionOpts(scale, cap, window, int(causal))
 
 
-def _batch(d, q_start, kv_len, page_table):
-    return (_whole(q_start, torch.int32, d.requests + 1, "q_start"),
-            _whole(kv_len, torch.int32, d.requests, "kv_len"),
-            _whole(page_table, torch.int32, d.requests * d.table_pages, "page_table"))
+def _batch(d, q_start, kv_len, page_table, here):
+    return (_on(q_start, torch.int32, d.requests + 1, "q_start", here),
+            _on(kv_len, torch.int32, d.requests, "kv_len", here),
+            _on(page_table, torch.int32, d.requests * d.table_pages, "page_table", here))
 
 
-def _cache(d, k_cache, v_cache, layers=1):
-    n, dt = layers * d.pages * d.kv_heads * d.page_size * d.head_dim, _DT_TORCH.get(d.dtype)
-    return _whole(k_cache, dt, n, "k_cache"), _whole(v_cache, dt, n, "v_cache")
+def _cache(d, dt, k_cache, v_cache, here, layers=1):
+    n = layers * d.pages * d.kv_heads * d.page_size * d.head_dim
+    return _on(k_cache, dt, n, "k_cache", here), _on(v_cache, dt, n, "v_cache", here)
+
+
+def _room(t, here):
+    """Pointer and bytes of a workspace tensor (or None) of the current device."""
+    if t is None:
+        return None, 0
+    n = t.numel()
+    return _on(t, t.dtype, n, "workspace", here), n * t.element_size()
 
 
 def sparoa_kv_append(desc, q, k, v, freqs, positions, q_start, kv_len, page_table, q_out, k_cache,
@@ -784,20 +798,21 @@ def sparoa_kv_append(desc, q, k, v, freqs, positions, q_start, kv_len, page_tabl
     """Rotates q and k by position (q to q_out) and puts k and v into the cache (see sparoa.h).
     q [tokens, heads * head_dim], k and v [tokens, kv_heads * head_dim]: views with any row
     stride; q and q_out None: no queries; rot_dim: default head_dim, or 0 without freqs."""
-    d, dt = desc, _DT_TORCH.get(desc.dtype)
+    d, dt, here = desc, _DT_TORCH.get(desc.dtype), _device()
+    tokens, dim = d.tokens, d.head_dim
     if rot_dim is None:
-        rot_dim = 0 if freqs is None else d.head_dim
-    _here(q, k, v, freqs, positions, q_start, kv_len, page_table, q_out, k_cache, v_cache)
-    wide, narrow = d.heads * d.head_dim, d.kv_heads * d.head_dim
-    qp, qs = (None, wide) if q is None else _rows(q, dt, d.tokens, wide, "q")
-    kp, ks = _rows(k, dt, d.tokens, narrow, "k")
-    vp, vs = _rows(v, dt, d.tokens, narrow, "v")
-    batch, cache = _batch(d, q_start, kv_len, page_table), _cache(d, k_cache, v_cache)
+        rot_dim = 0 if freqs is None else dim
+    wide, narrow = d.heads * dim, d.kv_heads * dim
+    qp, qs = (None, wide) if q is None else _rows(q, dt, tokens, wide, "q", here)
+    kp, ks = _rows(k, dt, tokens, narrow, "k", here)
+    vp, vs = _rows(v, dt, tokens, narrow, "v", here)
     _check(_L.sparoa_kv_append(
-        ctypes.byref(d), rot_dim, int(interleaved), qp, qs, kp, ks, vp, vs,
-        _whole(freqs, torch.float64, rot_dim // 2, "freqs"),
-        _whole(positions, torch.int32, d.tokens, "positions"), *batch,
-        _whole(q_out, dt, d.tokens * wide, "q_out"), *cache, _stream(stream)))
+        ctypes.byref(d), rot_dim, interleaved, qp, qs, kp, ks, vp, vs,
+        _on(freqs, torch.float64, rot_dim // 2, "freqs", here),
+        _on(positions, torch.int32, tokens, "positions", here),
+        *_batch(d, q_start, kv_len, page_table, here),
+        _on(q_out, dt, tokens * wide, "q_out", here), *_cache(d, dt, k_cache, v_cache, here),
+        _stream(stream)))
 
 
 def sparoa_attention_workspace_size(desc):
@@ -809,48 +824,40 @@ def sparoa_attention_workspace_size(desc):
 def sparoa_paged_attention(desc, opts, q, k_cache, v_cache, q_start, kv_len, page_table,
                            prefix_len, first_key, slopes, out, workspace, stream=None):
     """Attention of every request's rows over its cache (see sparoa.h)."""
-    d, dt = desc, _DT_TORCH.get(desc.dtype)
-    _here(q, k_cache, v_cache, q_start, kv_len, page_table, prefix_len, first_key, slopes, out,
-          workspace)
+    d, dt, here = desc, _DT_TORCH.get(desc.dtype), _device()
     n = d.tokens * d.heads * d.head_dim
-    ws, ws_bytes = _scratch(workspace)
     _check(_L.sparoa_paged_attention(
-        ctypes.byref(d), ctypes.byref(opts), _whole(q, dt, n, "q"), *_cache(d, k_cache, v_cache),
-        *_batch(d, q_start, kv_len, page_table),
-        _whole(prefix_len, torch.int32, d.requests, "prefix_len"),
-        _whole(first_key, torch.int32, d.tokens, "first_key"),
-        _whole(slopes, torch.float32, d.heads, "slopes"), _whole(out, dt, n, "out"), ws, ws_bytes,
-        _stream(stream)))
+        ctypes.byref(d), ctypes.byref(opts), _on(q, dt, n, "q", here),
+        *_cache(d, dt, k_cache, v_cache, here), *_batch(d, q_start, kv_len, page_table, here),
+        _on(prefix_len, torch.int32, d.requests, "prefix_len", here),
+        _on(first_key, torch.int32, d.tokens, "first_key", here),
+        _on(slopes, torch.float32, d.heads, "slopes", here), _on(out, dt, n, "out", here),
+        *_room(workspace, here), _stream(stream)))
 
 
 def sparoa_tree_attention(desc, opts, q, k_cache, v_cache, q_start, kv_len, page_table, tree_mask,
                           positions, slopes, out, workspace, stream=None):
     """Attention of drafted trees over their contexts (see sparoa.h); tree_mask: the bits in
     int64 [tokens, ceil(max_queries / 64)]."""
-    d, dt = desc, _DT_TORCH.get(desc.dtype)
-    _here(q, k_cache, v_cache, q_start, kv_len, page_table, tree_mask, positions, slopes, out,
-          workspace)
+    d, dt, here = desc, _DT_TORCH.get(desc.dtype), _device()
     n = d.tokens * d.heads * d.head_dim
-    ws, ws_bytes = _scratch(workspace)
     _check(_L.sparoa_tree_attention(
-        ctypes.byref(d), ctypes.byref(opts), _whole(q, dt, n, "q"), *_cache(d, k_cache, v_cache),
-        *_batch(d, q_start, kv_len, page_table),
-        _whole(tree_mask, torch.int64, d.tokens * -(-d.max_queries // 64), "tree_mask"),
-        _whole(positions, torch.int32, d.tokens, "positions"),
-        _whole(slopes, torch.float32, d.heads, "slopes"), _whole(out, dt, n, "out"), ws, ws_bytes,
-        _stream(stream)))
+        ctypes.byref(d), ctypes.byref(opts), _on(q, dt, n, "q", here),
+        *_cache(d, dt, k_cache, v_cache, here), *_batch(d, q_start, kv_len, page_table, here),
+        _on(tree_mask, torch.int64, d.tokens * -(-d.max_queries // 64), "tree_mask", here),
+        _on(positions, torch.int32, d.tokens, "positions", here),
+        _on(slopes, torch.float32, d.heads, "slopes", here), _on(out, dt, n, "out", here),
+        *_room(workspace, here), _stream(stream)))
 
 
 def sparoa_kv_keep(desc, layers, q_start, kv_len, page_table, keep, kept, k_cache, v_cache,
                    stream=None):
     """Accepted drafts' keys and values into place, in `layers` caches (see sparoa.h);
     keep int32 [requests, most]."""
-    d = desc
-    _here(q_start, kv_len, page_table, keep, kept, k_cache, v_cache)
+    d, here = desc, _device()
     most = keep.shape[1] if keep.dim() == 2 else 0
-    batch = _batch(d, q_start, kv_len, page_table)
     _check(_L.sparoa_kv_keep(
-        ctypes.byref(d), layers, *batch,
-        _whole(keep, torch.int32, d.requests * most, "keep"), most,
-        _whole(kept, torch.int32, d.requests, "kept"), *_cache(d, k_cache, v_cache, layers),
-        _stream(stream)))
+        ctypes.byref(d), layers, *_batch(d, q_start, kv_len, page_table, here),
+        _on(keep, torch.int32, d.requests * most, "keep", here), most,
+        _on(kept, torch.int32, d.requests, "kept", here),
+        *_cache(d, _DT_TORCH.get(d.dtype), k_cache, v_cache, here, layers), _stream(stream)))

@@ -37,10 +37,13 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 // Bytes of zeros: what lanes past the head's last dimension read.
 __device__ const uint4 kZeros[1] = {};
 
-// Pieces of a head: D (head_dim padded to 64, 128 or 256), key tiles of KT rows.
+// Pieces of a head: D (head_dim padded to 64, 96, 128, 192 or 256) in rows of 128 bytes'
+// multiples, key tiles of KT rows.
 template <int DT, int D>
 struct Shape {
-  static constexpr int size = Elem<DT>::size, row = D * size, vectors = row / 16;
+  static constexpr int size = Elem<DT>::size, row = (D * size + 127) / 128 * 128;
+  static constexpr int vectors = row / 16;
+  static constexpr int pitch = D <= 64 ? 64 : D <= 128 ? 128 : 256;   // of a range's outputs
   static constexpr int keys = row <= 256 ? 64 : 32;
   static constexpr int tile = keys * row, stage = 2 * tile, lds = 2 * stage;
   static constexpr int loads = keys * vectors / (64 * kWaves);   // a wave's, of K or V
@@ -54,9 +57,12 @@ struct Shape {
   }
   static constexpr int groups = lds <= 64 * 1024 && D <= 128 ? 2 : 1;   // a CU's
 };
-inline int padded_dim(int64_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
+inline int padded_dim(int64_t dim) {
+  return dim <= 64 ? 64 : dim <= 96 ? 96 : dim <= 128 ? 128 : dim <= 192 ? 192 : 256;
+}
+inline int output_pitch(int64_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 inline int tile_keys(int64_t dim, sparoa_dtype dt) {
-  return padded_dim(dim) * elem_size(dt) <= 256 ? 64 : 32;
+  return (padded_dim(dim) * elem_size(dt) + 127) / 128 * 128 <= 256 ? 64 : 32;
 }
 
 // 16 elements of K (8 a lane) of a 32 x 32 block.
@@ -580,7 +586,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
   if (slot >= a.slots || !row.live || wave >= a.slot_waves) return;
   const int64_t part = ((int64_t)slot * a.slot_waves + wave) * kWaveRows + rl;
   if (half == 0) reinterpret_cast<float2 *>(a.ml)[part] = make_float2(m * c, l);
-  float *const o = reinterpret_cast<float *>(a.part) + part * D + 4 * half;
+  float *const o = reinterpret_cast<float *>(a.part) + part * S::pitch + 4 * half;
 #pragma unroll
   for (int b = 0; b < DB; ++b)
 #pragma unroll
@@ -594,7 +600,8 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
 // and meet in LDS, since the chain of loads is all that such a call takes.
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a, int step) {
-  constexpr int KT = Shape<DT, D>::keys, LANES = D / 4, GROUPS = kThreads / LANES;
+  constexpr int KT = Shape<DT, D>::keys, LANES = Shape<DT, D>::pitch / 4;
+  constexpr int GROUPS = kThreads / LANES;
   constexpr int AHEAD = 8;
   __shared__ f32x4 sums[GROUPS][LANES];
   __shared__ float2 stats[GROUPS];
@@ -728,7 +735,9 @@ template <int DT>
 sparoa_status launch_dim(const AttnArgs &a, int64_t tiles, hipStream_t stream) {
   switch (padded_dim(a.kv.dim)) {
     case 64: return launch<DT, 64>(a, tiles, stream);
+    case 96: return launch<DT, 96>(a, tiles, stream);
     case 128: return launch<DT, 128>(a, tiles, stream);
+    case 192: return launch<DT, 192>(a, tiles, stream);
     default: return launch<DT, 256>(a, tiles, stream);
   }
 }
@@ -738,7 +747,7 @@ sparoa_status launch_dim(const AttnArgs &a, int64_t tiles, hipStream_t stream) {
 size_t attention_workspace(const sparoa_kv_desc &d) {
   const Split s = attention_split(d);
   return ml_bytes(s) + (size_t)((int64_t)s.slots * s.slot_waves * kWaveRows *
-                                padded_dim(d.head_dim) * 4) + 256;
+                                output_pitch(d.head_dim) * 4) + 256;
 }
 
 sparoa_status launch_attention(AttnArgs a, const sparoa_kv_desc &d, void *workspace,

@@ -144,13 +144,11 @@ def test_null_descriptors_and_results():
 @pytest.mark.parametrize("kw", [{}, dict(max_queries=1), dict(tokens=100000, requests=300),
                                 dict(table_pages=100000, max_keys=1600000, pages=200000),
                                 dict(head_dim=256, dtype=abi.F32)])
-def test_workspace_covers_the_bounds(kw):
-    """Wider bounds never ask for less, and what is asked for is accepted by size alone."""
-    small = abi.sparoa_attention_workspace_size(_desc(**kw))
-    assert small > 0
-    assert _attend(ws=small - 1, **kw) == WORKSPACE
-    for more in (dict(max_queries=8), dict(heads=16)):
-        assert abi.sparoa_attention_workspace_size(_desc(**{**kw, **more})) >= small
+def test_workspace(kw):
+    """A byte less than what is asked for is refused, for trees, too."""
+    size = abi.sparoa_attention_workspace_size(_desc(**kw))
+    assert size > 0
+    assert _attend(ws=size - 1, **kw) == WORKSPACE and _tree(ws=size - 1, **kw) == WORKSPACE
 
 
 def test_the_binding_refuses_other_tensors():
@@ -171,4 +169,4 @@ def test_the_binding_refuses_other_tensors():
         abi.sparoa_kv_keep(d, 1, i32(2), i32(1), i32(2), i32(4), i32(1), cache, cache)
     for bad in (q.float(), q[:3], q.t(), q[:, ::2], torch.zeros(128).bfloat16()):
         with pytest.raises(abi.SparoaError):
-            abi._rows(bad, torch.bfloat16, 4, 128, "q")
+            abi._rows(bad, torch.bfloat16, 4, 128, "q", 0)
