@@ -110,21 +110,27 @@ __device__ __forceinline__ float other_half(float v) { return __shfl_xor(v, 32);
 struct Item {
   int r, start, n, len;   // request (n 0: no item), its first row, rows, keys
   int row0;               // first row (token, group head) of the tile
-  int t0, t1;             // key tiles
-  int slot, chunk, chunks;
+  int slot, chunk, chunks;   // number `chunk` of the row tile's ranges of keys
 };
 
-// Row tiles, key tiles and their first of a request.
+// Row tiles of a request, key tiles that one of them reaches at most, and on average
+// (as far as lengths tell; not below half of the most).
 struct Load {
-  int tiles, spans, first;
+  int tiles, spans;
+  float mean;
 };
 __device__ __forceinline__ Load load_of(const AttnArgs &a, const KvRequest &q, int keys) {
-  Load l{0, 0, 0};
+  Load l{0, 0, 0.f};
   if (!q.n) return l;
   l.tiles = (q.n * a.kv.group + kTileRows - 1) / kTileRows;
-  // (a tree's rows reach back from where their positions say)
-  if (a.window && !a.mask) l.first = max(0, q.len - q.n + 1 - a.window) / keys;
-  l.spans = (q.len + keys - 1) / keys - l.first;
+  int reach = q.len;
+  float mean = (float)q.len;
+  if (a.causal && !a.mask) {
+    if (a.window) reach = min(q.len, a.window + kTileRows / a.kv.group + 1);
+    mean = fminf((float)q.len - 0.5f * (float)q.n, (float)reach);
+  }
+  l.spans = (reach - 1) / keys + 1 + (reach < q.len);   // (a window begins within a tile)
+  l.mean = fmaxf(mean / (float)keys, 0.5f * (float)l.spans);
   return l;
 }
 
@@ -135,7 +141,7 @@ __device__ __forceinline__ int chunk_tiles(const AttnArgs &a, int keys) {
   for (int r0 = 0; r0 < a.kv.requests; r0 += 64) {
     const KvRequest q = kv_request(a.kv, min(r0 + lane, a.kv.requests - 1));
     const Load l = load_of(a, q, keys);
-    work += r0 + lane < a.kv.requests ? (float)l.tiles * (float)l.spans : 0.f;
+    work += r0 + lane < a.kv.requests ? (float)l.tiles * l.mean : 0.f;
   }
 #pragma unroll
   for (int m = 32; m; m >>= 1) work += __shfl_xor(work, m);
@@ -144,11 +150,11 @@ __device__ __forceinline__ int chunk_tiles(const AttnArgs &a, int keys) {
 }
 
 // Ranges of a request's row tiles.  A range's outputs pass through memory twice (4
-// bytes each), which shall not be more than its keys and values do.
+// bytes each), which shall not be more than twice what its keys and values do.
 __device__ __forceinline__ int ranges_of(const AttnArgs &a, const KvRequest &q, const Load &l,
                                          int chunk, int keys) {
   const int rows = min(q.n * a.kv.group, kTileRows);
-  const int least = (rows * 4 + keys * a.elem - 1) / (keys * a.elem);
+  const int least = (rows * 2 + keys * a.elem - 1) / (keys * a.elem);
   const int size = max(max(chunk, least), (l.spans + kMaxRanges - 1) / kMaxRanges);
   return (l.spans + size - 1) / size;
 }
@@ -179,11 +185,6 @@ __device__ __forceinline__ Item find_item(const AttnArgs &a, int chunk, int id, 
       const int tile = local - it.chunk * tiles;
       it.row0 = (tiles - 1 - tile) * kTileRows;
       it.slot = before_slots + at(slots_upto - slots) + tile;   // chunk c: + c * tiles
-      // (ranges of like size)
-      const int first = at(l.first), spans = at(l.spans);
-      const int per = (spans + it.chunks - 1) / it.chunks;
-      it.t0 = first + min(it.chunk * per, spans);
-      it.t1 = first + min((it.chunk + 1) * per, spans);
       if (!TILES) it.slot += it.chunk * tiles;
       return it;
     }
@@ -312,8 +313,11 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
 #pragma unroll
   for (int w = 0; w < kWaves; ++w)
     tile_lo = min(tile_lo, reach[w][0]), tile_hi = max(tile_hi, reach[w][1]);
-  const int t0 = __builtin_amdgcn_readfirstlane(max(it.t0, tile_lo / KT));
-  const int t1 = __builtin_amdgcn_readfirstlane(min(it.t1, (tile_hi + KT - 1) / KT));
+  // this range of the key tiles that the rows reach
+  const int begin = tile_lo / KT, reached = max(0, (tile_hi + KT - 1) / KT - begin);
+  const int per = (reached + it.chunks - 1) / it.chunks;
+  const int t0 = __builtin_amdgcn_readfirstlane(begin + min(it.chunk * per, reached));
+  const int t1 = __builtin_amdgcn_readfirstlane(begin + min((it.chunk + 1) * per, reached));
 
   // ---- the ring: lane i of a wave knows the cache row of a tile's key i
   const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
@@ -699,11 +703,11 @@ Split attention_split(const sparoa_kv_desc &d) {
       kWaves, cdiv(std::min(d.max_queries, d.tokens) * group, kWaveRows));
   s.target = s.slot_waves == 1 ? kTargetFew : kTargetMany;
   // A request's row tiles that are split have ceil(spans / chunk) < 2 spans / chunk
-  // ranges each, and all spans are at most `target` chunks.  (+ kv_heads: the work's
-  // sum is rounded.)
+  // ranges each, spans are at most twice their mean, and all means at most `target`
+  // chunks.  (+ kv_heads: the work's sum is rounded.)
   const int64_t chunks = cdiv(d.max_keys, tile_keys(d.head_dim, d.dtype));
   const int64_t most = most_tiles(d);
-  const int64_t cap = 2 * s.target + 2 * d.kv_heads;
+  const int64_t cap = 4 * s.target + 4 * d.kv_heads;
   s.slots = (int)(chunks <= 1 ? 0
                   : chunks < cap && most < cap && most * chunks < cap / d.kv_heads
                       ? most * chunks * d.kv_heads : cap);
@@ -715,7 +719,10 @@ size_t ml_bytes(const Split &s) {
 
 template <int DT, int D>
 sparoa_status launch(const AttnArgs &a, int64_t tiles, hipStream_t stream) {
-  const int64_t items = (tiles + cdiv(a.target, a.kv.kv_heads) + 1) * a.kv.kv_heads;
+  // (by the work that they share, or by the ranges that a row tile can have)
+  const int64_t ranges = std::min<int64_t>(kMaxRanges, cdiv(a.kv.max_keys, Shape<DT, D>::keys) + 1);
+  const int64_t items = std::min(tiles + cdiv(2 * a.target, a.kv.kv_heads) + 2, tiles * ranges) *
+                        a.kv.kv_heads;
   if (items > 1 << 23)
     return fail(SPAROA_ERR_UNSUPPORTED, "attention: more than 2^23 row tiles");
   attention_kernel<DT, D><<<(unsigned)items, kThreads, 0, stream>>>(a);
