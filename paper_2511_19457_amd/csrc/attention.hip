@@ -134,17 +134,8 @@ __device__ __forceinline__ Load load_of(const AttnArgs &a, const KvRequest &q, i
   return l;
 }
 
-// Key tiles of an item: the whole work over the wanted items, a row tile's at most.
-__device__ __forceinline__ int chunk_tiles(const AttnArgs &a, int keys) {
-  const int lane = threadIdx.x & 63;
-  float work = 0.f;
-  for (int r0 = 0; r0 < a.kv.requests; r0 += 64) {
-    const KvRequest q = kv_request(a.kv, min(r0 + lane, a.kv.requests - 1));
-    const Load l = load_of(a, q, keys);
-    work += r0 + lane < a.kv.requests ? (float)l.tiles * l.mean : 0.f;
-  }
-#pragma unroll
-  for (int m = 32; m; m >>= 1) work += __shfl_xor(work, m);
+// Key tiles of an item: the whole work over the wanted items.
+__device__ __forceinline__ int chunk_of(const AttnArgs &a, float work) {
   work = work * (float)a.kv.kv_heads / (float)a.target;
   return work < 1e9f ? max(1, (int)ceilf(work)) : 1 << 30;
 }
@@ -159,38 +150,121 @@ __device__ __forceinline__ int ranges_of(const AttnArgs &a, const KvRequest &q, 
   return (l.spans + size - 1) / size;
 }
 
-// Item (or with TILES row tile that is split) number `id` of a kv head.
+// A request's share of the work: its items (row tiles times ranges), those whose outputs
+// are joined, and the row tiles that are.
+struct Share {
+  int items, slots, splits;
+};
+__device__ __forceinline__ Share share_of(const Load &l, int chunks) {
+  const int items = l.tiles * chunks;
+  return Share{items, chunks > 1 ? items : 0, chunks > 1 ? l.tiles : 0};
+}
+
+// Up to 64 requests every wave works the split out by itself, a lane a request.  More
+// are planned by a kernel in front: plan[0] is the chunk, then, for every request and
+// behind the last, the items, slots and split row tiles before it (arrays of
+// requests + 1).
+constexpr int kLaneRequests = 64;
+constexpr int kPlanThreads = 1024;
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttnArgs a, int keys) {
+  __shared__ float work_of[kPlanThreads / 64];
+  __shared__ int before[kPlanThreads / 64][3];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = a.kv.requests;
+  float work = 0.f;
+  for (int r = tid; r < n; r += kPlanThreads) {
+    const Load l = load_of(a, kv_request(a.kv, r), keys);
+    work += (float)l.tiles * l.mean;
+  }
+#pragma unroll
+  for (int m = 32; m; m >>= 1) work += __shfl_xor(work, m);
+  if (lane == 0) work_of[wave] = work;
+  __syncthreads();
+  work = 0.f;
+  for (int w = 0; w < kPlanThreads / 64; ++w) work += work_of[w];
+  const int chunk = chunk_of(a, work);
+  int32_t *const items = a.plan + 1, *const slots = items + n + 1, *const splits = slots + n + 1;
+  int sum[3] = {0, 0, 0};
+  for (int r0 = 0; r0 < n; r0 += kPlanThreads) {
+    const int r = r0 + tid;
+    KvRequest q = kv_request(a.kv, min(r, n - 1));
+    if (r >= n) q.n = 0;
+    const Load l = load_of(a, q, keys);
+    const Share s = share_of(l, ranges_of(a, q, l, chunk, keys));
+    const int mine[3] = {s.items, s.slots, s.splits};
+    int upto[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      upto[i] = wave_prefix(mine[i]);
+      if (lane == 63) before[wave][i] = upto[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      int at = sum[i] + upto[i] - mine[i];
+      for (int w = 0; w < kPlanThreads / 64; ++w) {
+        if (w < wave) at += before[w][i];
+        sum[i] += before[w][i];
+      }
+      if (r < n) (i == 0 ? items : i == 1 ? slots : splits)[r] = at;
+    }
+    __syncthreads();
+  }
+  if (tid == 0) a.plan[0] = chunk, items[n] = sum[0], slots[n] = sum[1], splits[n] = sum[2];
+}
+
+// Item (or with TILES row tile that is split) number `id` of a kv head; the whole wave.
 template <bool TILES>
-__device__ __forceinline__ Item find_item(const AttnArgs &a, int chunk, int id, int keys) {
+__device__ __forceinline__ Item find_item(const AttnArgs &a, int id, int keys) {
   const int lane = threadIdx.x & 63;
   Item it{};
-  int before_slots = 0;
-  for (int r0 = 0; r0 < a.kv.requests; r0 += 64) {
-    KvRequest q = kv_request(a.kv, min(r0 + lane, a.kv.requests - 1));
-    if (r0 + lane >= a.kv.requests) q.n = 0;
-    const Load l = load_of(a, q, keys);
-    const int chunks = ranges_of(a, q, l, chunk, keys), items = l.tiles * chunks;
-    const int slots = chunks > 1 ? items : 0;
-    const int counted = TILES ? (chunks > 1 ? l.tiles : 0) : items;
-    const int upto = wave_prefix(counted), slots_upto = wave_prefix(slots);
+  int chunk, local, slot0;
+  Load l;
+  if (!a.plan) {
+    KvRequest q = kv_request(a.kv, min(lane, a.kv.requests - 1));
+    if (lane >= a.kv.requests) q.n = 0;
+    l = load_of(a, q, keys);
+    float work = (float)l.tiles * l.mean;
+#pragma unroll
+    for (int m = 32; m; m >>= 1) work += __shfl_xor(work, m);
+    chunk = chunk_of(a, work);
+    const int chunks = ranges_of(a, q, l, chunk, keys);
+    const Share s = share_of(l, chunks);
+    const int counted = TILES ? s.splits : s.items;
+    const int upto = wave_prefix(counted), slots_upto = wave_prefix(s.slots);
     const uint64_t past = __ballot(upto > id);
-    if (past) {
-      const int w = __builtin_ctzll(past);
-      auto at = [&](int v) { return __builtin_amdgcn_readlane(v, w); };
-      const int local = id - at(upto - counted), tiles = at(l.tiles);
-      it.r = r0 + w, it.start = at(q.start), it.n = at(q.n), it.len = at(q.len);
-      it.chunks = at(chunks);
-      // (row tiles innermost, the last rows, which see most, first)
-      it.chunk = TILES ? 0 : local / tiles;
-      const int tile = local - it.chunk * tiles;
-      it.row0 = (tiles - 1 - tile) * kTileRows;
-      it.slot = before_slots + at(slots_upto - slots) + tile;   // chunk c: + c * tiles
-      if (!TILES) it.slot += it.chunk * tiles;
-      return it;
+    if (!past) return it;
+    const int w = __builtin_ctzll(past);
+    auto at = [&](int v) { return __builtin_amdgcn_readlane(v, w); };
+    it.r = w, it.start = at(q.start), it.n = at(q.n), it.len = at(q.len);
+    it.chunks = at(chunks), l.tiles = at(l.tiles);
+    local = id - at(upto - counted), slot0 = at(slots_upto - s.slots);
+  } else {
+    const int n = a.kv.requests;
+    const int32_t *const items = a.plan + 1, *const slots = items + n + 1;
+    const int32_t *const counted = TILES ? slots + n + 1 : items;
+    if (id >= counted[n]) return it;
+    // the last request that begins at id or before (64 ways a step)
+    int at = 0, left = n;
+    while (left > 1) {
+      const int step = (left + 63) / 64, probe = at + lane * step;
+      const uint64_t below = __ballot(lane * step < left && counted[min(probe, n)] <= id);
+      const int last = below ? 63 - __builtin_clzll(below) : 0;
+      at += last * step;
+      left = min(step, left - last * step);
     }
-    id -= __builtin_amdgcn_readlane(upto, 63);
-    before_slots += __builtin_amdgcn_readlane(slots_upto, 63);
+    it.r = __builtin_amdgcn_readfirstlane(at);
+    const KvRequest q = kv_request(a.kv, it.r);
+    l = load_of(a, q, keys);
+    it.start = q.start, it.n = q.n, it.len = q.len;
+    it.chunks = ranges_of(a, q, l, a.plan[0], keys);
+    local = id - counted[it.r], slot0 = slots[it.r];
+    if (!it.n) return it;
   }
+  // (row tiles innermost, the last rows, which see most, first)
+  it.chunk = TILES ? 0 : local / l.tiles;
+  const int tile = local - it.chunk * l.tiles;
+  it.row0 = (l.tiles - 1 - tile) * kTileRows;
+  it.slot = slot0 + tile + it.chunk * l.tiles;   // (TILES: range c has slot + c tiles)
   return it;
 }
 
@@ -278,6 +352,61 @@ __device__ __forceinline__ void store_rows(const AttnArgs &a, const Row &row, in
   }
 }
 
+// Whether a tile in LDS holds an infinity or NaN (an exponent of ones); the whole wave.
+template <int DT>
+__device__ __forceinline__ bool holds_bad(const char *tile, int bytes) {
+  constexpr uint32_t kExp = DT == SPAROA_F32 ? 0x7F800000u : DT == SPAROA_F16 ? 0x7C007C00u
+                                                                             : 0x7F807F80u;
+  constexpr uint32_t kOne = DT == SPAROA_F32 ? 0x00800000u : DT == SPAROA_F16 ? 0x04000400u
+                                                                             : 0x00800080u;
+  uint32_t top = 0;   // (ones plus one carry to the sign's place)
+#pragma unroll 4
+  for (int i = 16 * (threadIdx.x & 63); i < bytes; i += 1024) {
+    const u32x4 w = *reinterpret_cast<const u32x4 *>(tile + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top |= (w[e] & kExp) + kOne;
+  }
+  return __any((top & (DT == SPAROA_F32 ? 0x80000000u : 0x80008000u)) != 0);
+}
+
+// acc += weights x values over the keys from .. to that each row sees, one by one.
+template <int DT, int D>
+__device__ __forceinline__ void add_seen(const AttnArgs &a, const Item &it, const Row &row,
+                                         int kv_head, int from, int to, float c, float cap_by,
+                                         float slope, float base, f32x16 (&acc)[D / 32]) {
+  const int half = (threadIdx.x & 63) >> 5;
+  const int64_t q0 = ((int64_t)row.token * a.kv.heads + row.head) * a.kv.dim;
+#pragma nounroll
+  for (int k = from; k < min(to, it.len); ++k) {
+    const int at = kv_row(a.kv, it.r, kv_head, k);
+    if (at < 0 || !(row.live && (seen_keys(a, it, row, k) & 1))) continue;
+    float x = 0.f;
+    const int64_t k0 = (int64_t)at * a.kv.dim;
+#pragma nounroll
+    for (int d = 0; d < a.kv.dim; d += 4) {
+      float qv[4], kv[4];
+      load_elems<DT, 4>(a.q, q0 + d, qv);
+      load_elems<DT, 4>(a.k, k0 + d, kv);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x = fmaf(qv[e], kv[e], x);
+    }
+    if (a.cap > 0.f) x = capped<DT>(x, a.cap, cap_by);
+    if (a.slopes) x = fmaf(-slope, distance(a, it, row, k), x);
+    const float p = __builtin_amdgcn_exp2f(fmaf(x, c, -base));
+#pragma unroll
+    for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int d = 32 * b + 8 * g + 4 * half;
+        if (d >= a.kv.dim) continue;
+        float v[4];
+        load_elems<DT, 4>(a.v, k0 + d, v);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[b][4 * g + e] = fmaf(p, v[e], acc[b][4 * g + e]);
+      }
+  }
+}
+
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_kernel(AttnArgs a) {
   using S = Shape<DT, D>;
@@ -289,8 +418,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
   const int lane = threadIdx.x & 63, rl = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kv_head = blockIdx.x % a.kv.kv_heads, id = blockIdx.x / a.kv.kv_heads;
-  const int chunk = chunk_tiles(a, KT);
-  Item it = find_item<false>(a, chunk, id, KT);
+  const Item it = find_item<false>(a, id, KT);
   if (!it.n) return;
   const int slot = it.slot * a.kv.kv_heads + kv_head;
 
@@ -384,7 +512,10 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
   float m = -__builtin_inff(), l = 0.f;   // (l: the lane's own keys)
-  bool hidden = false;                     // a tile had keys that some row does not see
+  // Tiles that hold an infinity or NaN beside keys that some row does not see are left to
+  // the end (behind the 64th with all that follow): their values are added key by key.
+  uint64_t put_off = 0;
+  int put_off_from = INT32_MAX;
 
   int here = 0, page = 0;
   if (t0 < t1) {
@@ -452,8 +583,8 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
                            s[n][i]);
       }
     }
-    if (k0 < all_lo || k0 + KT > all_hi || pageless) {
-      hidden = true;
+    const bool hidden = k0 < all_lo || k0 + KT > all_hi || pageless;   // from some row
+    if (hidden) {
       const uint64_t seen = (seen_keys(a, it, row, k0) & ~pageless) >> (4 * half);
 #pragma unroll
       for (int n = 0; n < NB; ++n) {
@@ -489,6 +620,15 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
         s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -base));
         l += s[n][i];
       }
+    // (a weight of 0 times a hidden key's infinity or NaN is NaN)
+    if (t >= put_off_from) continue;
+    if (hidden && holds_bad<DT>(values, S::tile)) {
+      if (t - t0 < 64)
+        put_off |= (uint64_t)1 << (t - t0);
+      else
+        put_off_from = t;
+      continue;
+    }
     Piece<DT> v[VA + 1], p;
 #pragma unroll
     for (int i = 0; i < 2 * NB * DB + VA; ++i) {   // 16 keys of 32 dimensions
@@ -532,52 +672,11 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
     }
   }
 
-  // A weight of 0 times a hidden key's infinity or NaN is NaN: such a wave's rows
-  // are added up again, by what each of them sees.
-  if (hidden) {
-    float bad = 0.f;
-#pragma unroll
-    for (int b = 0; b < DB; ++b)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) bad = fmaf(acc[b][i], 0.f, bad);
-    if (__any(row.live && bad != 0.f)) {
-#pragma unroll
-      for (int b = 0; b < DB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
-      const float base = m == -__builtin_inff() ? 0.f : m * c;
-      const int from = max(t0 * KT, lo), to = min(t1 * KT, hi);
-#pragma nounroll
-      for (int k = from; k < to; ++k) {
-        const int at = kv_row(a.kv, it.r, kv_head, k);
-        if (at < 0 || !(row.live && (seen_keys(a, it, row, k) & 1))) continue;
-        float x = 0.f;
-        const int64_t q0 = ((int64_t)row.token * a.kv.heads + row.head) * a.kv.dim;
-        const int64_t k0 = (int64_t)at * a.kv.dim;
-#pragma nounroll
-        for (int d = 0; d < a.kv.dim; d += 4) {
-          float qv[4], kv[4];
-          load_elems<DT, 4>(a.q, q0 + d, qv);
-          load_elems<DT, 4>(a.k, k0 + d, kv);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x = fmaf(qv[e], kv[e], x);
-        }
-        if (a.cap > 0.f) x = capped<DT>(x, a.cap, cap_by);
-        if (a.slopes) x = fmaf(-slope, distance(a, it, row, k), x);
-        const float p = __builtin_amdgcn_exp2f(fmaf(x, c, -base));
-#pragma unroll
-        for (int b = 0; b < DB; ++b)
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const int d = 32 * b + 8 * g + 4 * half;
-            if (d >= a.kv.dim) continue;
-            float v[4];
-            load_elems<DT, 4>(a.v, k0 + d, v);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[b][4 * g + e] = fmaf(p, v[e], acc[b][4 * g + e]);
-          }
-      }
-    }
+  if (put_off || put_off_from < t1) {
+    const float base = m == -__builtin_inff() ? 0.f : m * c;
+    for (int t = t0; t < t1; ++t)
+      if (t >= put_off_from || (t - t0 < 64 && put_off >> (t - t0) & 1))
+        add_seen<DT, D>(a, it, row, kv_head, t * KT, t * KT + KT, c, cap_by, slope, base, acc);
   }
 
   l += other_half(l);
@@ -610,12 +709,11 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a, int step) {
   __shared__ f32x4 sums[GROUPS][LANES];
   __shared__ float2 stats[GROUPS];
   const int tid = threadIdx.x, group = tid / LANES, lane = tid % LANES;
-  const int chunk = chunk_tiles(a, KT);
   const int row_groups = (a.tile_rows + step - 1) / step;
   const int per = a.kv.kv_heads * row_groups;
   for (int u = blockIdx.x;; u += gridDim.x) {
     const int in = u % per, kv_head = in % a.kv.kv_heads, g = in / a.kv.kv_heads;
-    const Item it = find_item<true>(a, chunk, u / per, KT);
+    const Item it = find_item<true>(a, u / per, KT);
     if (!it.n) return;
     const int rows = it.n * a.kv.group, tiles = (rows + kTileRows - 1) / kTileRows;
     if (it.row0 + g * step >= rows) continue;
@@ -717,6 +815,10 @@ size_t ml_bytes(const Split &s) {
   return (size_t)((int64_t)s.slots * s.slot_waves * kWaveRows * 8 + 255) / 256 * 256;
 }
 
+size_t plan_bytes(const sparoa_kv_desc &d) {
+  return d.requests <= kLaneRequests ? 0 : (size_t)(12 * (d.requests + 1) + 4 + 255) / 256 * 256;
+}
+
 template <int DT, int D>
 sparoa_status launch(const AttnArgs &a, int64_t tiles, hipStream_t stream) {
   // (by the work that they share, or by the ranges that a row tile can have)
@@ -724,7 +826,11 @@ sparoa_status launch(const AttnArgs &a, int64_t tiles, hipStream_t stream) {
   const int64_t items = std::min(tiles + cdiv(2 * a.target, a.kv.kv_heads) + 2, tiles * ranges) *
                         a.kv.kv_heads;
   if (items > 1 << 23)
-    return fail(SPAROA_ERR_UNSUPPORTED, "attention: more than 2^23 row tiles");
+    return fail(SPAROA_ERR_UNSUPPORTED, "attention: 2^30 or more rows (token, head)");
+  if (a.plan) {
+    plan_kernel<<<1, kPlanThreads, 0, stream>>>(a, Shape<DT, D>::keys);
+    SPAROA_LAUNCH_CHECK("attention: plan");
+  }
   attention_kernel<DT, D><<<(unsigned)items, kThreads, 0, stream>>>(a);
   SPAROA_LAUNCH_CHECK("attention");
   if (a.slots) {
@@ -753,7 +859,7 @@ sparoa_status launch_dim(const AttnArgs &a, int64_t tiles, hipStream_t stream) {
 
 size_t attention_workspace(const sparoa_kv_desc &d) {
   const Split s = attention_split(d);
-  return ml_bytes(s) + (size_t)((int64_t)s.slots * s.slot_waves * kWaveRows *
+  return plan_bytes(d) + ml_bytes(s) + (size_t)((int64_t)s.slots * s.slot_waves * kWaveRows *
                                 output_pitch(d.head_dim) * 4) + 256;
 }
 
@@ -763,8 +869,10 @@ sparoa_status launch_attention(AttnArgs a, const sparoa_kv_desc &d, void *worksp
   a.target = s.target, a.slots = s.slots, a.slot_waves = s.slot_waves;
   a.elem = (int)elem_size(d.dtype);
   a.tile_rows = (int)std::min<int64_t>(kTileRows, (int64_t)a.kv.max_queries * a.kv.group);
-  a.ml = workspace;
-  a.part = reinterpret_cast<char *>(workspace) + ml_bytes(s);
+  char *const ws = reinterpret_cast<char *>(workspace);
+  a.plan = d.requests <= kLaneRequests ? nullptr : reinterpret_cast<int32_t *>(ws);
+  a.ml = ws + plan_bytes(d);
+  a.part = ws + plan_bytes(d) + ml_bytes(s);
   const int64_t tiles = most_tiles(d);
   switch (d.dtype) {
     case SPAROA_F32: return launch_dim<SPAROA_F32>(a, tiles, stream);

@@ -86,6 +86,7 @@ struct AttnArgs {
   int target, slots, slot_waves;
   int elem;                // bytes of an element
   int tile_rows;           // rows of a tile at most
+  int32_t *plan;           // workspace: the split of many requests, or null
   void *ml, *part;         // workspace: (maximum, sum) of rows, unscaled outputs
 };
 size_t attention_workspace(const sparoa_kv_desc &d);

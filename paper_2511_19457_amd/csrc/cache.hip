@@ -80,7 +80,8 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, KvDiv by
   const int heads = a.q ? a.kv.heads : 0;
   const int rotated = (heads + a.kv.kv_heads) * units;
   const int total = rotated + a.kv.kv_heads * (dim / V);
-  for (int t = blockIdx.x; t < a.kv.tokens; t += gridDim.x) {
+  for (int64_t at_row = blockIdx.x; at_row < a.kv.tokens; at_row += gridDim.x) {
+    const int t = (int)at_row;
     const RowOf row = request_of(a.kv, t);
     if (!row.q.n) continue;   // (alike in every wave)
     const int at = row.q.len - row.q.n + (t - row.q.start);

@@ -75,7 +75,8 @@ sparoa_status attend(const sparoa_kv_desc *d, const sparoa_attention_opts *o, At
   if (!workspace || ws_bytes < attention_workspace(*d))
     return fail(SPAROA_ERR_WORKSPACE, "attention: workspace too small");
   a.scale = o->scale, a.cap = o->cap;
-  a.window = (int)(o->window < kMax31 ? o->window : 0);   // (longer than any cache)
+  // (longer than any distance there is: none; a tree's positions may be any)
+  a.window = (int)(o->window < (a.mask ? kMax31 : d->max_keys) ? o->window : 0);
   a.causal = o->causal != 0;
   return launch_attention(a, *d, workspace, stream);
 }

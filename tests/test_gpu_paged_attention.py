@@ -95,7 +95,9 @@ def test_causal(rows, keys, heads, kv, dim, page, dt):
 @pytest.mark.parametrize("dt", TYPES)
 @pytest.mark.parametrize("opts", [dict(causal=False), dict(window=1), dict(window=64),
                                   dict(window=100, causal=False), dict(cap=5.0),
-                                  dict(cap=30.0, window=37), dict(scale=0.5)])
+                                  dict(cap=30.0, window=37), dict(scale=0.5),
+                                  dict(window=410), dict(window=411), dict(window=2 ** 31 - 2),
+                                  dict(window=2 ** 40)])
 def test_options(opts, dt):
     compare(Batch([70, 1, 150], [70, 300, 411], 4, 2, 64, 20, dt, seed=5), opts)
 
@@ -142,6 +144,30 @@ def test_hidden_infinities(bad, dim, dt):
     others = [d for d in range(dim) if d != 3]
     assert torch.isfinite(got[31:, 2:, others]).all()
     check(got[31:, 2:, others], ref[31:, 2:, others], err[31:, 2:, others], bad)
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_hidden_infinities_in_every_tile(dt):
+    """A document that begins late, behind bad values in tiles of the other row's: few
+    ranges (many heads), so that one work-group meets more than 64 such tiles."""
+    b = Batch([2], [6000], 1024, 1024, 8, 16, dt, seed=18)
+    for at in range(3, 5400, 40):
+        page, off = b.where(0, [at])
+        b.v[page, :, off, 1] = math.nan if at % 3 else math.inf
+    first = [0, 5450]
+    got = run(b, first=first).double().cpu()
+    sees, u = visible(b, 0, first=first)[1:], {"bf16": 2.0 ** -8, "f16": 2.0 ** -11, "f32": 0.0}[dt]
+    assert torch.isfinite(got[1]).all()
+    for h in (0, 1, 500, 1023):
+        k, v = b.get(b.k, 0)[:, h].double(), b.get(b.v, 0)[:, h].double()
+        k, v = k[sees[0]], v[sees[0]]
+        x = (b.q[1:, h].double() @ k.t()) * 8 ** -0.5
+        w = torch.softmax(x, 1)
+        # weights and the output are rounded (u each), scores off by 24 roundings of 2^-24
+        size = w @ v.abs()
+        off = torch.expm1(2 * 24 * 2.0 ** -24 * (b.q[1:, h].double().abs() @ k.abs().t()).max() +
+                          2.0 ** -19 * x.abs().max())
+        assert ((got[1, h] - w @ v).abs() <= (2 * u + off + 700 * 2.0 ** -24) * size + 1e-4 * u).all()
 
 
 @pytest.mark.parametrize("dt", TYPES)
@@ -208,7 +234,7 @@ def test_requests_out_of_bounds_are_left_out(dt):
         check(out[keep], ref[keep], err[keep], starts)
 
 
-@pytest.mark.parametrize("requests", [63, 64, 65, 200])
+@pytest.mark.parametrize("requests", [63, 64, 65, 200, 1500])
 def test_many_requests(requests):
     g = torch.Generator().manual_seed(requests)
     rows = torch.randint(0, 3, (requests,), generator=g).tolist()
