@@ -24,10 +24,11 @@ constexpr int kWaveRows = 32, kTileRows = kWaves * kWaveRows;
 constexpr int kMaxRanges = 64;     // of a row: a step of the join
 // Items that the work is cut into.  Few rows: small ranges even the load out and cost
 // little; many: a range's outputs pass through memory, so a row tile is cut only where
-// it is longer than what 320 of the 512 resident work-groups would have each (64
-// decoding requests: 512 237 us, 768 217, 1024 222, 2048 223; 12 chunks of prompts: 256
-// 65, 320 65, 512 81; 32 trees: 169, 150, 166).
-constexpr int kTargetFew = 1024, kTargetMany = 320;
+// it is longer than what 320 of the 512 resident work-groups would have each, in fp32,
+// whose products take longer, 448 (64 decoding requests: 512 237 us, 768 217, 1024 222,
+// 2048 223; 12 chunks of prompts: 320 56, 448 56, 512 90; 32 trees: 320 150, 448 170;
+// 5 fp32 prompts: 320 35, 448 31, 640 31).
+constexpr int kTargetFew = 1024, kTargetMany = 320, kTargetF32 = 448;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.f;      // a maximum may lag by 2^8 before sums are scaled
 
@@ -212,61 +213,94 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttnArgs a, int keys
   if (tid == 0) a.plan[0] = chunk, items[n] = sum[0], slots[n] = sum[1], splits[n] = sum[2];
 }
 
-// Item (or with TILES row tile that is split) number `id` of a kv head; the whole wave.
+// The split as a wave sees it: items (or with TILES row tiles that are split) of a kv
+// head by their number.
 template <bool TILES>
-__device__ __forceinline__ Item find_item(const AttnArgs &a, int id, int keys) {
-  const int lane = threadIdx.x & 63;
-  Item it{};
-  int chunk, local, slot0;
+struct Split {
+  const AttnArgs &a;
+  const int keys;
+  // up to 64 requests: the lane's, and the sums up to the lane's place in the order
+  KvRequest q;
   Load l;
-  if (!a.plan) {
-    KvRequest q = kv_request(a.kv, min(lane, a.kv.requests - 1));
+  int chunks, rank, counted, upto, slots, slots_upto;
+
+  __device__ __forceinline__ Split(const AttnArgs &args, int tile_keys)
+      : a(args), keys(tile_keys) {
+    if (a.plan) return;
+    const int lane = threadIdx.x & 63;
+    q = kv_request(a.kv, min(lane, a.kv.requests - 1));
     if (lane >= a.kv.requests) q.n = 0;
     l = load_of(a, q, keys);
     float work = (float)l.tiles * l.mean;
 #pragma unroll
     for (int m = 32; m; m >>= 1) work += __shfl_xor(work, m);
-    chunk = chunk_of(a, work);
-    const int chunks = ranges_of(a, q, l, chunk, keys);
-    const Share s = share_of(l, chunks);
-    const int counted = TILES ? s.splits : s.items;
-    const int upto = wave_prefix(counted), slots_upto = wave_prefix(s.slots);
-    const uint64_t past = __ballot(upto > id);
-    if (!past) return it;
-    const int w = __builtin_ctzll(past);
-    auto at = [&](int v) { return __builtin_amdgcn_readlane(v, w); };
-    it.r = w, it.start = at(q.start), it.n = at(q.n), it.len = at(q.len);
-    it.chunks = at(chunks), l.tiles = at(l.tiles);
-    local = id - at(upto - counted), slot0 = at(slots_upto - s.slots);
-  } else {
-    const int n = a.kv.requests;
-    const int32_t *const items = a.plan + 1, *const slots = items + n + 1;
-    const int32_t *const counted = TILES ? slots + n + 1 : items;
-    if (id >= counted[n]) return it;
-    // the last request that begins at id or before (64 ways a step)
-    int at = 0, left = n;
-    while (left > 1) {
-      const int step = (left + 63) / 64, probe = at + lane * step;
-      const uint64_t below = __ballot(lane * step < left && counted[min(probe, n)] <= id);
-      const int last = below ? 63 - __builtin_clzll(below) : 0;
-      at += last * step;
-      left = min(step, left - last * step);
+    chunks = ranges_of(a, q, l, chunk_of(a, work), keys);
+    // The requests of the longest ranges first where rows are many: 12 chunks of prompts 63
+    // -> 55 us, 32 trees the same.  (Single rows are a stream, whose last ranges have the
+    // memory to themselves: 64 requests 224 us in their order, 238 by length.)
+    rank = lane;
+    if (a.tile_rows > kWaveRows && a.kv.requests > 1) {
+      const int size = chunks ? (l.spans + chunks - 1) / chunks : 0;
+      rank = 0;
+      for (int o = 0; o < a.kv.requests; ++o) {
+        const int other = __builtin_amdgcn_readlane(size, o);
+        rank += other > size || (other == size && o < lane);
+      }
+      if (lane >= a.kv.requests) rank = lane;
     }
-    it.r = __builtin_amdgcn_readfirstlane(at);
-    const KvRequest q = kv_request(a.kv, it.r);
-    l = load_of(a, q, keys);
-    it.start = q.start, it.n = q.n, it.len = q.len;
-    it.chunks = ranges_of(a, q, l, a.plan[0], keys);
-    local = id - counted[it.r], slot0 = slots[it.r];
-    if (!it.n) return it;
+    const Share s = share_of(l, chunks);
+    counted = TILES ? s.splits : s.items, slots = s.slots;
+    if (a.tile_rows > kWaveRows) {
+      counted = __builtin_amdgcn_ds_permute(4 * rank, counted);
+      slots = __builtin_amdgcn_ds_permute(4 * rank, slots);
+    }
+    upto = wave_prefix(counted), slots_upto = wave_prefix(slots);
   }
-  // (row tiles innermost, the last rows, which see most, first)
-  it.chunk = TILES ? 0 : local / l.tiles;
-  const int tile = local - it.chunk * l.tiles;
-  it.row0 = (l.tiles - 1 - tile) * kTileRows;
-  it.slot = slot0 + tile + it.chunk * l.tiles;   // (TILES: range c has slot + c tiles)
-  return it;
-}
+
+  __device__ __forceinline__ Item find(int id) const {   // (the whole wave)
+    const int lane = threadIdx.x & 63;
+    Item it{};
+    int local, slot0, tiles;
+    if (!a.plan) {
+      const uint64_t past = __ballot(upto > id);
+      if (!past) return it;
+      const int w = __builtin_ctzll(past);   // its rank
+      it.r = __builtin_ctzll(__ballot(rank == w));
+      auto at = [&](int v) { return __builtin_amdgcn_readlane(v, it.r); };
+      it.start = at(q.start), it.n = at(q.n), it.len = at(q.len);
+      it.chunks = at(chunks), tiles = at(l.tiles);
+      local = id - __builtin_amdgcn_readlane(upto - counted, w);
+      slot0 = __builtin_amdgcn_readlane(slots_upto - slots, w);
+    } else {
+      const int n = a.kv.requests;
+      const int32_t *const items = a.plan + 1, *const slots_of = items + n + 1;
+      const int32_t *const before = TILES ? slots_of + n + 1 : items;
+      if (id >= before[n]) return it;
+      // the last request that begins at id or before (64 ways a step)
+      int at = 0, left = n;
+      while (left > 1) {
+        const int step = (left + 63) / 64, probe = at + lane * step;
+        const uint64_t below = __ballot(lane * step < left && before[min(probe, n)] <= id);
+        const int last = below ? 63 - __builtin_clzll(below) : 0;
+        at += last * step;
+        left = min(step, left - last * step);
+      }
+      it.r = __builtin_amdgcn_readfirstlane(at);
+      const KvRequest mine = kv_request(a.kv, it.r);
+      if (!mine.n) return it;
+      const Load load = load_of(a, mine, keys);
+      it.start = mine.start, it.n = mine.n, it.len = mine.len;
+      it.chunks = ranges_of(a, mine, load, a.plan[0], keys);
+      tiles = load.tiles, local = id - before[it.r], slot0 = slots_of[it.r];
+    }
+    // (row tiles innermost, the last rows, which see most, first)
+    it.chunk = TILES ? 0 : local / tiles;
+    const int tile = local - it.chunk * tiles;
+    it.row0 = (tiles - 1 - tile) * kTileRows;
+    it.slot = slot0 + tile + it.chunk * tiles;   // (TILES: range c has slot + c tiles)
+    return it;
+  }
+};
 
 // What row (token, group head) number `row` of a request sees, and where it lies.
 struct Row {
@@ -407,6 +441,15 @@ __device__ __forceinline__ void add_seen(const AttnArgs &a, const Item &it, cons
   }
 }
 
+// A row tile's range of keys: 4 waves of 32 rows share every tile of keys and values.
+// Many rows are bound by matrix and vector instructions alike (a tile of 64 keys takes a
+// wave 1024 cycles of the one and some 1100 of the other, 2400 together): two work-groups
+// a CU, one's products beside the other's weights.  2 x 4096 causal rows, 32 heads of 128,
+// 8 kv heads, bf16: 305-318 us, 0.87-0.90 PFLOP/s; 64 single rows over 200 to 8000 keys:
+// 219 us, the kernel 5.3 TB/s.  Built and dropped: the next tile's scores beside this
+// one's weights (313 us against 305 then; fp32 42 against 35), 8 waves with rings of 4
+// stages (325), a kernel for up to 32 rows with a ring a wave and no barrier (decoding
+// 216 us against 221 then, one token 15.4 against 13.8).
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_kernel(AttnArgs a) {
   using S = Shape<DT, D>;
@@ -418,7 +461,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
   const int lane = threadIdx.x & 63, rl = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kv_head = blockIdx.x % a.kv.kv_heads, id = blockIdx.x / a.kv.kv_heads;
-  const Item it = find_item<false>(a, id, KT);
+  const Item it = Split<false>(a, KT).find(id);
   if (!it.n) return;
   const int slot = it.slot * a.kv.kv_heads + kv_head;
 
@@ -657,7 +700,10 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
       }
       if (i < VA) continue;
       const int j = i - VA, u = j / DB, b = j % DB;
-      if (b == 0) {   // the lane's weights of these keys
+      // The lane's weights of these keys.  16-bit types round them once, as an operand
+      // has to be: half a step each, without bias, which puts an output 1.4 times as far
+      // from 64 bits as its own rounding does; their sum l is of the unrounded ones.
+      if (b == 0) {
         if constexpr (DT == SPAROA_F32) {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
@@ -709,11 +755,12 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a, int step) {
   __shared__ f32x4 sums[GROUPS][LANES];
   __shared__ float2 stats[GROUPS];
   const int tid = threadIdx.x, group = tid / LANES, lane = tid % LANES;
+  const Split<true> split(a, KT);
   const int row_groups = (a.tile_rows + step - 1) / step;
   const int per = a.kv.kv_heads * row_groups;
   for (int u = blockIdx.x;; u += gridDim.x) {
     const int in = u % per, kv_head = in % a.kv.kv_heads, g = in / a.kv.kv_heads;
-    const Item it = find_item<true>(a, u / per, KT);
+    const Item it = split.find(u / per);
     if (!it.n) return;
     const int rows = it.n * a.kv.group, tiles = (rows + kTileRows - 1) / kTileRows;
     if (it.row0 + g * step >= rows) continue;
@@ -791,15 +838,17 @@ int64_t most_tiles(const sparoa_kv_desc &d) {
                   d.tokens * group / kTileRows + d.requests);
 }
 
-struct Split {
+struct Parts {
   int target, slots, slot_waves;
 };
-Split attention_split(const sparoa_kv_desc &d) {
+Parts attention_split(const sparoa_kv_desc &d) {
   const int64_t group = d.heads / d.kv_heads;
-  Split s;
+  Parts s;
   s.slot_waves = (int)std::min<int64_t>(
       kWaves, cdiv(std::min(d.max_queries, d.tokens) * group, kWaveRows));
-  s.target = s.slot_waves == 1 ? kTargetFew : kTargetMany;
+  s.target = s.slot_waves == 1         ? kTargetFew
+             : d.dtype == SPAROA_F32 ? kTargetF32
+                                     : kTargetMany;
   // A request's row tiles that are split have ceil(spans / chunk) < 2 spans / chunk
   // ranges each, spans are at most twice their mean, and all means at most `target`
   // chunks.  (+ kv_heads: the work's sum is rounded.)
@@ -811,7 +860,7 @@ Split attention_split(const sparoa_kv_desc &d) {
                       ? most * chunks * d.kv_heads : cap);
   return s;
 }
-size_t ml_bytes(const Split &s) {
+size_t ml_bytes(const Parts &s) {
   return (size_t)((int64_t)s.slots * s.slot_waves * kWaveRows * 8 + 255) / 256 * 256;
 }
 
@@ -834,8 +883,10 @@ sparoa_status launch(const AttnArgs &a, int64_t tiles, hipStream_t stream) {
   attention_kernel<DT, D><<<(unsigned)items, kThreads, 0, stream>>>(a);
   SPAROA_LAUNCH_CHECK("attention");
   if (a.slots) {
-    // (few rows: a work-group a row; many: the lookups are made for 8)
-    const int step = a.slot_waves == 1 ? 1 : a.slot_waves == 2 ? 4 : 8;
+    // (a work-group a row where they are few altogether; else the lookups are made for
+    // several: 64 requests of 4 rows a kv head 221 us with 1 each, 217 with 4)
+    const int step = a.slot_waves == 1 ? (tiles * a.kv.kv_heads > 64 ? 4 : 1)
+                                            : a.slot_waves == 2 ? 4 : 8;
     const unsigned grid = (unsigned)std::min<int64_t>(
         std::min<int64_t>(tiles, a.slots) * a.kv.kv_heads * cdiv(a.tile_rows, step),
         2048);
@@ -858,14 +909,14 @@ sparoa_status launch_dim(const AttnArgs &a, int64_t tiles, hipStream_t stream) {
 }  // namespace
 
 size_t attention_workspace(const sparoa_kv_desc &d) {
-  const Split s = attention_split(d);
+  const Parts s = attention_split(d);
   return plan_bytes(d) + ml_bytes(s) + (size_t)((int64_t)s.slots * s.slot_waves * kWaveRows *
                                 output_pitch(d.head_dim) * 4) + 256;
 }
 
 sparoa_status launch_attention(AttnArgs a, const sparoa_kv_desc &d, void *workspace,
                                hipStream_t stream) {
-  const Split s = attention_split(d);
+  const Parts s = attention_split(d);
   a.target = s.target, a.slots = s.slots, a.slot_waves = s.slot_waves;
   a.elem = (int)elem_size(d.dtype);
   a.tile_rows = (int)std::min<int64_t>(kTileRows, (int64_t)a.kv.max_queries * a.kv.group);
