@@ -126,6 +126,23 @@ class KvDesc(ctypes.Structure):
                 ("tokens", "requests", "heads", "kv_heads", "head_dim", "pages", "page_size",
                  "table_pages", "max_queries", "max_keys")] + [("dtype", ctypes.c_int)]
 
+    def __setattr__(self, name, value):
+        super().__setattr__(name, value)
+        self.__dict__.pop("_of", None)
+
+    def of(self):
+        """The tensors' sizes that follow from the fields (a field costs 70 ns to read, as
+        much as a question to a tensor; kept until a field is set)."""
+        got = self.__dict__.get("_of")
+        if got is None:
+            got = self.__dict__["_of"] = (
+                _DT_TORCH.get(self.dtype), self.tokens, self.heads * self.head_dim,
+                self.kv_heads * self.head_dim,
+                self.pages * self.kv_heads * self.page_size * self.head_dim, self.requests,
+                self.requests * self.table_pages, -(-self.max_queries // 64), self.heads,
+                self.head_dim)
+        return got
+
 
 class AttentionOpts(ctypes.Structure):
     _fields_ = [("scale", ctypes.c_float), ("cap", ctypes.c_float), ("window", ctypes.c_int64),
@@ -732,31 +749,38 @@ def sparoa_block_norm(desc, y, post_w, post_b, gate, r, pre_w, pre_b, r_out, n_o
 
 # ------------------------------------ attention over a paged cache (see sparoa.h)
 
-def _device():
-    """Index of the current device, whose stream a call is enqueued on (-2: no device yet)."""
-    return torch._C._cuda_getDevice() if torch.cuda.is_initialized() else -2
+def _now(stream):
+    """(current device, the stream's handle); device -2: none yet."""
+    if not torch.cuda.is_initialized():
+        return -2, _stream(stream)
+    here = torch._C._cuda_getDevice()
+    if stream is None:
+        return here, torch._C._cuda_getCurrentRawStream(here)
+    return here, _stream(stream)
 
 
 def _on(t, dtype, numel, name, here):
     """As _whole, of the current device `here`."""
     if t is None:
         return None
-    if t.get_device() != here or t.dtype is not dtype or t.numel() != numel \
-            or not t.is_contiguous():
-        _whole(t, dtype, numel, name)
-        raise SparoaError(1, f"{name}: a tensor on {t.device}, the current device is {here}")
-    return t.data_ptr()
+    if t.numel() == numel and t.dtype is dtype and t.get_device() == here and t.is_contiguous():
+        return t.data_ptr()
+    _whole(t, dtype, numel, name)
+    raise SparoaError(1, f"{name}: a tensor on {t.device}, the current device is {here}")
 
 
 def _rows(t, dtype, rows, width, name, here):
     """Pointer and row stride of a [rows, width] view whose rows are dense."""
-    if t.get_device() != here or t.dtype is not dtype or t.dim() != 2 \
-            or t.shape[0] != rows or t.shape[1] != width or here < 0 \
-            or (width > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < width):
-        raise SparoaError(1, f"{name}: a {dtype} tensor [{rows}, {width}] with dense rows on the "
-                             f"current device is wanted, got {t.dtype} {tuple(t.shape)} with "
-                             f"strides {t.stride()} on {t.device}")
-    return t.data_ptr(), t.stride(0) if rows > 1 else width
+    if t.dim() == 2 and t.dtype is dtype and t.get_device() == here >= 0 \
+            and t.shape == (rows, width):
+        row, one = t.stride()
+        if rows == 1:
+            row = width
+        if row >= width and (one == 1 or width == 1):
+            return t.data_ptr(), row
+    raise SparoaError(1, f"{name}: a {dtype} tensor [{rows}, {width}] with dense rows on the "
+                         f"current device is wanted, got {t.dtype} {tuple(t.shape)} with "
+                         f"strides {t.stride()} on {t.device}")
 
 
 def kv_desc(tokens, requests, heads, kv_heads, head_dim, pages, page_size, table_pages, dtype=BF16,
@@ -774,17 +798,6 @@ def attention_opts(scale, cap=0.0, window=0, causal=True):
     return AttentionOpts(scale, cap, window, int(causal))
 
 
-def _batch(d, q_start, kv_len, page_table, here):
-    return (_on(q_start, torch.int32, d.requests + 1, "q_start", here),
-            _on(kv_len, torch.int32, d.requests, "kv_len", here),
-            _on(page_table, torch.int32, d.requests * d.table_pages, "page_table", here))
-
-
-def _cache(d, dt, k_cache, v_cache, here, layers=1):
-    n = layers * d.pages * d.kv_heads * d.page_size * d.head_dim
-    return _on(k_cache, dt, n, "k_cache", here), _on(v_cache, dt, n, "v_cache", here)
-
-
 def _room(t, here):
     """Pointer and bytes of a workspace tensor (or None) of the current device."""
     if t is None:
@@ -798,21 +811,22 @@ def sparoa_kv_append(desc, q, k, v, freqs, positions, q_start, kv_len, page_tabl
     """Rotates q and k by position (q to q_out) and puts k and v into the cache (see sparoa.h).
     q [tokens, heads * head_dim], k and v [tokens, kv_heads * head_dim]: views with any row
     stride; q and q_out None: no queries; rot_dim: default head_dim, or 0 without freqs."""
-    d, dt, here = desc, _DT_TORCH.get(desc.dtype), _device()
-    tokens, dim = d.tokens, d.head_dim
+    dt, tokens, wide, narrow, cache, requests, table, _, _, dim = desc.of()
+    here, handle = _now(stream)
     if rot_dim is None:
         rot_dim = 0 if freqs is None else dim
-    wide, narrow = d.heads * dim, d.kv_heads * dim
     qp, qs = (None, wide) if q is None else _rows(q, dt, tokens, wide, "q", here)
     kp, ks = _rows(k, dt, tokens, narrow, "k", here)
     vp, vs = _rows(v, dt, tokens, narrow, "v", here)
+    i32 = torch.int32
     _check(_L.sparoa_kv_append(
-        ctypes.byref(d), rot_dim, interleaved, qp, qs, kp, ks, vp, vs,
+        ctypes.byref(desc), rot_dim, interleaved, qp, qs, kp, ks, vp, vs,
         _on(freqs, torch.float64, rot_dim // 2, "freqs", here),
-        _on(positions, torch.int32, tokens, "positions", here),
-        *_batch(d, q_start, kv_len, page_table, here),
-        _on(q_out, dt, tokens * wide, "q_out", here), *_cache(d, dt, k_cache, v_cache, here),
-        _stream(stream)))
+        _on(positions, i32, tokens, "positions", here),
+        _on(q_start, i32, requests + 1, "q_start", here), _on(kv_len, i32, requests, "kv_len", here),
+        _on(page_table, i32, table, "page_table", here),
+        _on(q_out, dt, tokens * wide, "q_out", here), _on(k_cache, dt, cache, "k_cache", here),
+        _on(v_cache, dt, cache, "v_cache", here), handle))
 
 
 def sparoa_attention_workspace_size(desc):
@@ -824,40 +838,49 @@ def sparoa_attention_workspace_size(desc):
 def sparoa_paged_attention(desc, opts, q, k_cache, v_cache, q_start, kv_len, page_table,
                            prefix_len, first_key, slopes, out, workspace, stream=None):
     """Attention of every request's rows over its cache (see sparoa.h)."""
-    d, dt, here = desc, _DT_TORCH.get(desc.dtype), _device()
-    n = d.tokens * d.heads * d.head_dim
+    dt, tokens, wide, _, cache, requests, table, _, heads, _ = desc.of()
+    here, handle = _now(stream)
+    i32 = torch.int32
     _check(_L.sparoa_paged_attention(
-        ctypes.byref(d), ctypes.byref(opts), _on(q, dt, n, "q", here),
-        *_cache(d, dt, k_cache, v_cache, here), *_batch(d, q_start, kv_len, page_table, here),
-        _on(prefix_len, torch.int32, d.requests, "prefix_len", here),
-        _on(first_key, torch.int32, d.tokens, "first_key", here),
-        _on(slopes, torch.float32, d.heads, "slopes", here), _on(out, dt, n, "out", here),
-        *_room(workspace, here), _stream(stream)))
+        ctypes.byref(desc), ctypes.byref(opts), _on(q, dt, tokens * wide, "q", here),
+        _on(k_cache, dt, cache, "k_cache", here), _on(v_cache, dt, cache, "v_cache", here),
+        _on(q_start, i32, requests + 1, "q_start", here), _on(kv_len, i32, requests, "kv_len", here),
+        _on(page_table, i32, table, "page_table", here),
+        _on(prefix_len, i32, requests, "prefix_len", here),
+        _on(first_key, i32, tokens, "first_key", here),
+        _on(slopes, torch.float32, heads, "slopes", here),
+        _on(out, dt, tokens * wide, "out", here), *_room(workspace, here), handle))
 
 
 def sparoa_tree_attention(desc, opts, q, k_cache, v_cache, q_start, kv_len, page_table, tree_mask,
                           positions, slopes, out, workspace, stream=None):
     """Attention of drafted trees over their contexts (see sparoa.h); tree_mask: the bits in
     int64 [tokens, ceil(max_queries / 64)]."""
-    d, dt, here = desc, _DT_TORCH.get(desc.dtype), _device()
-    n = d.tokens * d.heads * d.head_dim
+    dt, tokens, wide, _, cache, requests, table, words, heads, _ = desc.of()
+    here, handle = _now(stream)
+    i32 = torch.int32
     _check(_L.sparoa_tree_attention(
-        ctypes.byref(d), ctypes.byref(opts), _on(q, dt, n, "q", here),
-        *_cache(d, dt, k_cache, v_cache, here), *_batch(d, q_start, kv_len, page_table, here),
-        _on(tree_mask, torch.int64, d.tokens * -(-d.max_queries // 64), "tree_mask", here),
-        _on(positions, torch.int32, d.tokens, "positions", here),
-        _on(slopes, torch.float32, d.heads, "slopes", here), _on(out, dt, n, "out", here),
-        *_room(workspace, here), _stream(stream)))
+        ctypes.byref(desc), ctypes.byref(opts), _on(q, dt, tokens * wide, "q", here),
+        _on(k_cache, dt, cache, "k_cache", here), _on(v_cache, dt, cache, "v_cache", here),
+        _on(q_start, i32, requests + 1, "q_start", here), _on(kv_len, i32, requests, "kv_len", here),
+        _on(page_table, i32, table, "page_table", here),
+        _on(tree_mask, torch.int64, tokens * words, "tree_mask", here),
+        _on(positions, i32, tokens, "positions", here),
+        _on(slopes, torch.float32, heads, "slopes", here),
+        _on(out, dt, tokens * wide, "out", here), *_room(workspace, here), handle))
 
 
 def sparoa_kv_keep(desc, layers, q_start, kv_len, page_table, keep, kept, k_cache, v_cache,
                    stream=None):
     """Accepted drafts' keys and values into place, in `layers` caches (see sparoa.h);
     keep int32 [requests, most]."""
-    d, here = desc, _device()
-    most = keep.shape[1] if keep.dim() == 2 else 0
+    dt, _, _, _, cache, requests, table, _, _, _ = desc.of()
+    here, handle = _now(stream)
+    i32, most = torch.int32, keep.shape[1] if keep.dim() == 2 else 0
     _check(_L.sparoa_kv_keep(
-        ctypes.byref(d), layers, *_batch(d, q_start, kv_len, page_table, here),
-        _on(keep, torch.int32, d.requests * most, "keep", here), most,
-        _on(kept, torch.int32, d.requests, "kept", here),
-        *_cache(d, _DT_TORCH.get(d.dtype), k_cache, v_cache, here, layers), _stream(stream)))
+        ctypes.byref(desc), layers, _on(q_start, i32, requests + 1, "q_start", here),
+        _on(kv_len, i32, requests, "kv_len", here), _on(page_table, i32, table, "page_table", here),
+        _on(keep, i32, requests * most, "keep", here), most,
+        _on(kept, i32, requests, "kept", here),
+        _on(k_cache, dt, layers * cache, "k_cache", here),
+        _on(v_cache, dt, layers * cache, "v_cache", here), handle))
