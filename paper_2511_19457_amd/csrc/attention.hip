@@ -232,8 +232,11 @@ struct Split {
     if (lane >= a.kv.requests) q.n = 0;
     l = load_of(a, q, keys);
     float work = (float)l.tiles * l.mean;
+    if (a.kv.requests > 1)
 #pragma unroll
-    for (int m = 32; m; m >>= 1) work += __shfl_xor(work, m);
+      for (int m = 32; m; m >>= 1) work += __shfl_xor(work, m);
+    else
+      work = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(work)));
     chunks = ranges_of(a, q, l, chunk_of(a, work), keys);
     // The requests of the longest ranges first where rows are many: 12 chunks of prompts 63
     // -> 55 us, 32 trees the same.  (Single rows are a stream, whose last ranges have the
@@ -302,10 +305,30 @@ struct Split {
   }
 };
 
+// The least (or greatest) of all lanes' numbers, by moves between lanes within the
+// vector unit (through LDS the same takes six of its latencies).
+template <bool LEAST>
+__device__ __forceinline__ int wave_limit(int v) {
+#define SPAROA_DPP_LIMIT(ctrl, rows)                                             \
+  {                                                                              \
+    const int o = __builtin_amdgcn_update_dpp(v, v, ctrl, rows, 0xF, false);     \
+    v = LEAST ? min(v, o) : max(v, o);                                           \
+  }
+  SPAROA_DPP_LIMIT(0x111, 0xF)
+  SPAROA_DPP_LIMIT(0x112, 0xF)
+  SPAROA_DPP_LIMIT(0x114, 0xF)
+  SPAROA_DPP_LIMIT(0x118, 0xF)
+  SPAROA_DPP_LIMIT(0x142, 0xA)
+  SPAROA_DPP_LIMIT(0x143, 0xC)
+#undef SPAROA_DPP_LIMIT
+  return __builtin_amdgcn_readlane(v, 63);
+}
+
 // What row (token, group head) number `row` of a request sees, and where it lies.
 struct Row {
   bool live;
   int token, head, pos, lo, hi;
+  uint64_t bits;   // a tree's first 64
 };
 __device__ __forceinline__ Row row_of(const AttnArgs &a, const Item &it, int kv_head, int row) {
   Row o;
@@ -315,7 +338,9 @@ __device__ __forceinline__ Row row_of(const AttnArgs &a, const Item &it, int kv_
   o.head = kv_head * a.kv.group + (o.live ? row : 0) - j * a.kv.group;
   o.pos = it.len - it.n + j;
   o.lo = 0, o.hi = it.len;
+  o.bits = 0;
   if (a.mask) {
+    o.bits = a.mask[(int64_t)o.token * a.mask_words];
     if (a.positions) o.pos = a.positions[o.token];
   } else if (a.causal) {
     o.hi = min(it.len, max(o.pos + 1, a.prefix ? a.prefix[it.r] : 0));
@@ -339,8 +364,9 @@ __device__ __forceinline__ uint64_t seen_keys(const AttnArgs &a, const Item &it,
   const uint64_t *words = a.mask + (int64_t)row.token * a.mask_words;
   const int w = first >> 6, shift = first & 63;   // (w may be -1)
   uint64_t nodes = 0;
-  if (w >= 0 && w < a.mask_words) nodes = words[w] >> shift;
-  if (shift && w + 1 < a.mask_words) nodes |= words[w + 1] << (64 - shift);
+  // (the first word lies in registers: a load here waits for the tiles sent for before)
+  if (w >= 0 && w < a.mask_words) nodes = (w ? words[w] : row.bits) >> shift;
+  if (shift && w + 1 < a.mask_words) nodes |= (w + 1 ? words[w + 1] : row.bits) << (64 - shift);
   nodes &= low_bits(it.n - first) & ~low_bits(-first);
   if (a.window)   // nodes that lie too far back
 #pragma nounroll
@@ -467,17 +493,12 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
 
   const Row row = row_of(a, it, kv_head, it.row0 + wave * kWaveRows + rl);
   // the wave's range of keys, and the part that all its rows see
-  int lo = row.live && row.lo < row.hi ? row.lo : INT32_MAX, hi = lo < INT32_MAX ? row.hi : 0;
-  int all_lo = row.live ? row.lo : 0;
-  int all_hi = row.live ? (a.mask ? it.len - it.n : row.hi) : INT32_MAX;
-#pragma unroll
-  for (int m = 32; m; m >>= 1) {
-    lo = min(lo, __shfl_xor(lo, m)), hi = max(hi, __shfl_xor(hi, m));
-    all_lo = max(all_lo, __shfl_xor(all_lo, m)), all_hi = min(all_hi, __shfl_xor(all_hi, m));
-  }
-  lo = __builtin_amdgcn_readfirstlane(lo), hi = __builtin_amdgcn_readfirstlane(hi);
-  all_lo = __builtin_amdgcn_readfirstlane(all_lo);
-  all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+  const bool some = row.live && row.lo < row.hi;
+  const int lo = wave_limit<true>(some ? row.lo : INT32_MAX);
+  const int hi = wave_limit<false>(some ? row.hi : 0);
+  const int all_lo = wave_limit<false>(row.live ? row.lo : 0);
+  const int all_hi =
+      wave_limit<true>(!row.live ? INT32_MAX : a.mask ? it.len - it.n : row.hi);
   if (lane == 0) reach[wave][0] = lo, reach[wave][1] = hi;
   __syncthreads();
   int tile_lo = INT32_MAX, tile_hi = 0;
