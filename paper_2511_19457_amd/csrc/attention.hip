@@ -8,9 +8,9 @@
 //   transposing read.  So no score leaves its lane and a row's factors meet its
 //   outputs there.
 // Keys and values go from memory to a ring of two stages in LDS by the loads
-// themselves.  Work is cut into items (row tile, range of key tiles) of like
-// size by every work-group from the lengths on the device; the ranges of a row
-// tile that has several are joined by a second kernel.
+// themselves.  Work is cut into items (row tile, range of keys) of like size from the
+// lengths on the device, by every wave for itself or, above 64 requests, by a kernel in
+// front; the ranges of a row tile that has several are joined by a kernel behind.
 #include <algorithm>
 
 #include "cache.h"
@@ -130,7 +130,8 @@ __device__ __forceinline__ Load load_of(const AttnArgs &a, const KvRequest &q, i
     if (a.window) reach = min(q.len, a.window + kTileRows / a.kv.group + 1);
     mean = fminf((float)q.len - 0.5f * (float)q.n, (float)reach);
   }
-  l.spans = (reach - 1) / keys + 1 + (reach < q.len);   // (a window begins within a tile)
+  // (a window begins within a tile; no more than there are)
+  l.spans = min((reach - 1) / keys + 2, (q.len - 1) / keys + 1);
   l.mean = fmaxf(mean / (float)keys, 0.5f * (float)l.spans);
   return l;
 }
@@ -296,6 +297,8 @@ struct Split {
       it.chunks = ranges_of(a, mine, load, a.plan[0], keys);
       tiles = load.tiles, local = id - before[it.r], slot0 = slots_of[it.r];
     }
+    // (sums that passed 2^31: requests that claim each other's rows)
+    if ((uint32_t)local >= (uint32_t)(TILES ? tiles : tiles * it.chunks)) return Item{};
     // (row tiles innermost, the last rows, which see most, first)
     it.chunk = TILES ? 0 : local / tiles;
     const int tile = local - it.chunk * tiles;
@@ -489,7 +492,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
   const int kv_head = blockIdx.x % a.kv.kv_heads, id = blockIdx.x / a.kv.kv_heads;
   const Item it = Split<false>(a, KT).find(id);
   if (!it.n) return;
-  const int slot = it.slot * a.kv.kv_heads + kv_head;
+  const int64_t slot = (int64_t)it.slot * a.kv.kv_heads + kv_head;
 
   const Row row = row_of(a, it, kv_head, it.row0 + wave * kWaveRows + rl);
   // the wave's range of keys, and the part that all its rows see
@@ -753,8 +756,8 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
     for (int b = 0; b < DB; ++b) store_rows<DT, D>(a, row, b, acc[b], by);
     return;
   }
-  if (slot >= a.slots || !row.live || wave >= a.slot_waves) return;
-  const int64_t part = ((int64_t)slot * a.slot_waves + wave) * kWaveRows + rl;
+  if (slot < 0 || slot >= a.slots || !row.live || wave >= a.slot_waves) return;
+  const int64_t part = (slot * a.slot_waves + wave) * kWaveRows + rl;
   if (half == 0) reinterpret_cast<float2 *>(a.ml)[part] = make_float2(m * c, l);
   float *const o = reinterpret_cast<float *>(a.part) + part * S::pitch + 4 * half;
 #pragma unroll
@@ -801,10 +804,11 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a, int step) {
 #pragma unroll
           for (int i = 0; i < AHEAD; ++i) {
             const int ch = c0 + i * share;
-            const int slot = (it.slot + min(ch, it.chunks - 1) * tiles) * a.kv.kv_heads + kv_head;
-            has[i] = ch < it.chunks && slot < a.slots;
-            const int64_t at = (int64_t)min(slot, a.slots - 1) * a.slot_waves * kWaveRows +
-                               g * step + r;
+            const int64_t slot =
+                ((int64_t)it.slot + (int64_t)min(ch, it.chunks - 1) * tiles) * a.kv.kv_heads +
+                kv_head;
+            has[i] = ch < it.chunks && slot >= 0 && slot < a.slots;
+            const int64_t at = (has[i] ? slot : 0) * a.slot_waves * kWaveRows + g * step + r;
             ml[i] = reinterpret_cast<const float2 *>(a.ml)[at];
             o[i] = reinterpret_cast<const f32x4 *>(a.part)[at * LANES + lane];
           }

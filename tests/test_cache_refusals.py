@@ -170,3 +170,11 @@ def test_the_binding_refuses_other_tensors():
     for bad in (q.float(), q[:3], q.t(), q[:, ::2], torch.zeros(128).bfloat16()):
         with pytest.raises(abi.SparoaError):
             abi._rows(bad, torch.bfloat16, 4, 128, "q", 0)
+
+
+def test_a_changed_descriptor_is_asked_anew():
+    d = abi.kv_desc(4, 2, 8, 2, 64, 3, 16, 2, torch.bfloat16)
+    assert d.of()[1:7] == (4, 512, 128, 3 * 2 * 16 * 64, 2, 4) and d.of()[7] == 1
+    d.tokens, d.pages, d.max_queries, d.dtype = 9, 5, 65, abi.F32
+    assert d.of()[0] is torch.float32
+    assert d.of()[1] == 9 and d.of()[4] == 5 * 2 * 16 * 64 and d.of()[7] == 2

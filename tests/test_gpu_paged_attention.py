@@ -102,6 +102,15 @@ def test_options(opts, dt):
     compare(Batch([70, 1, 150], [70, 300, 411], 4, 2, 64, 20, dt, seed=5), opts)
 
 
+@pytest.mark.parametrize("dim", [64, 256])
+@pytest.mark.parametrize("keys", [2, 31, 32, 33, 63, 64, 65, 96, 128, 129, 200])
+def test_windows_within_few_tiles(keys, dim):
+    """Windows shorter than the cache, caches of one tile or a few, bounds that just hold."""
+    for rows in (1, 2, min(keys, 40)):
+        for window in (1, 10, 31, 33, 63, 100):
+            compare(Batch([rows], [keys], 4, 1, dim, 16, "f32", seed=keys), dict(window=window))
+
+
 @pytest.mark.parametrize("dt", TYPES)
 @pytest.mark.parametrize("opts", [{}, dict(cap=10.0), dict(window=90), dict(causal=False)])
 def test_prefix_documents_slopes(opts, dt):
