@@ -822,8 +822,8 @@ sparoa_status sparoa_kv_append(const sparoa_kv_desc *desc, int64_t rot_dim, int 
  *   Equal inputs give equal bits.  Workspace: sparoa_attention_workspace_size
  *   bytes, contents on entry do not matter; it may not be shared by calls that
  *   overlap in time.
- * Errors: also INVALID_ARG for null options, a scale or cap that is not finite,
- * scale <= 0, cap < 0, window < 0; UNSUPPORTED for 2^30 or more rows (token, head);
+ * Errors: also INVALID_ARG for null options, a scale or a cap other than 0 outside
+ * [2^-60, 2^60], window < 0; UNSUPPORTED for 2^30 or more rows (token, head);
  * WORKSPACE. */
 typedef struct {
   float scale, cap;

@@ -390,13 +390,22 @@ __device__ __forceinline__ float distance(const AttnArgs &a, const Item &it, con
   return fabsf((float)(row.pos - at));
 }
 
-// cap tanh(s / cap)
-template <int DT>
+// cap tanh(x), x = by s.  16-bit types: 1 - 2 / (1 + e^2x), off by about 2^-23 of the cap.
+// That is less than 2^-14 in a score for caps up to kFewCap; above it, the series
+// x - x^3 / 3 + 2 x^5 / 15 where |x| < 1/8 (off by 17 x^7 / 315, less than 2^-22 of x), so that
+// the error is one of 2^-20 of the score, whatever the cap.
+// (The series for every cap: 75 us against 60 for the capped chunks of prompts.)
+constexpr float kFewCap = 256.f;
+
+template <int DT, bool LARGE>
 __device__ __forceinline__ float capped(float s, float cap, float by) {
-  // (16-bit types: 1 - 2 / (1 + e^2x), off by 2^-23 of the cap)
   if constexpr (DT == SPAROA_F32) return cap * tanhf(s * by);
-  return cap - 2.f * cap * __builtin_amdgcn_rcpf(
-                               1.f + __builtin_amdgcn_exp2f(2.f * kLog2e * by * s));
+  const float far = cap - 2.f * cap * __builtin_amdgcn_rcpf(
+                                    1.f + __builtin_amdgcn_exp2f(2.f * kLog2e * by * s));
+  if (!LARGE) return far;
+  const float x = by * s, x2 = x * x;
+  const float near = cap * fmaf(x * x2, fmaf(x2, 2.f / 15.f, -1.f / 3.f), x);
+  return fabsf(x) < 0.125f ? near : far;
 }
 
 // Outputs of one row tile's wave: lane l has row l & 31; register 16 b + r has
@@ -432,12 +441,25 @@ __device__ __forceinline__ bool holds_bad(const char *tile, int bytes) {
   return __any((top & (DT == SPAROA_F32 ? 0x80000000u : 0x80008000u)) != 0);
 }
 
+// Weights are 2^(c s - c m) as one fma of s, c and the rounded c m: a row's weights all have
+// the same error, its sum of them too.  Behind 2^24 that rounding could pass the largest
+// exponent there is: m is taken off first there.
+struct Base {
+  float shift, by;   // 2^(c (s - shift) - by)
+  __device__ Base(float m, float c) {
+    const float at = m == -__builtin_inff() ? 0.f : m * c;
+    const bool large = fabsf(at) > 0x1p24f;
+    shift = large ? m : 0.f, by = large ? 0.f : at;
+  }
+};
+
 // acc += weights x values over the keys from .. to that each row sees, one by one.
 template <int DT, int D>
 __device__ __forceinline__ void add_seen(const AttnArgs &a, const Item &it, const Row &row,
                                          int kv_head, int from, int to, float c, float cap_by,
-                                         float slope, float base, f32x16 (&acc)[D / 32]) {
+                                         float slope, float m, f32x16 (&acc)[D / 32]) {
   const int half = (threadIdx.x & 63) >> 5;
+  const Base base(m, c);
   const int64_t q0 = ((int64_t)row.token * a.kv.heads + row.head) * a.kv.dim;
 #pragma nounroll
   for (int k = from; k < min(to, it.len); ++k) {
@@ -453,9 +475,11 @@ __device__ __forceinline__ void add_seen(const AttnArgs &a, const Item &it, cons
 #pragma unroll
       for (int e = 0; e < 4; ++e) x = fmaf(qv[e], kv[e], x);
     }
-    if (a.cap > 0.f) x = capped<DT>(x, a.cap, cap_by);
+    if (a.cap > 0.f) x = capped<DT, true>(x, a.cap, cap_by);
     if (a.slopes) x = fmaf(-slope, distance(a, it, row, k), x);
-    const float p = __builtin_amdgcn_exp2f(fmaf(x, c, -base));
+    // (this sum's roundings are other than those that found the maximum; NaN stays)
+    const float at2 = fmaf(x - base.shift, c, -base.by);
+    const float p = __builtin_amdgcn_exp2f(at2 > 2.f * kSlack ? 2.f * kSlack : at2);
 #pragma unroll
     for (int b = 0; b < D / 32; ++b)
 #pragma unroll
@@ -579,6 +603,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
   float m = -__builtin_inff(), l = 0.f;   // (l: the lane's own keys)
+  bool far = false;   // a row of the wave has a maximum behind 2^24
   // Tiles that hold an infinity or NaN beside keys that some row does not see are left to
   // the end (behind the 64th with all that follow): their values are added key by key.
   uint64_t put_off = 0;
@@ -626,11 +651,16 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
         s[n] = mma32<DT>(k[(i - KA) % (KA + 1)], q[st], s[n]);
       }
     }
-    if (a.cap > 0.f) {
+    if (a.cap > kFewCap) {
 #pragma unroll
       for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[n][i] = capped<DT>(s[n][i], a.cap, cap_by);
+        for (int i = 0; i < 16; ++i) s[n][i] = capped<DT, true>(s[n][i], a.cap, cap_by);
+    } else if (a.cap > 0.f) {
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[n][i] = capped<DT, false>(s[n][i], a.cap, cap_by);
     }
     if (a.slopes) {   // (scores are in units of 1 / c here)
       if (!a.mask || k0 + KT <= it.len - it.n) {
@@ -669,17 +699,27 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
     top = fmaxf(top, other_half(top));
-    if (__any(top * c > m * c + kSlack)) {
+    // (far: the two products can be alike where the scores are not)
+    if (__any(top * c > m * c + kSlack || (far && top > m))) {
       const float to = fmaxf(m, top);
       const float by = to == m ? 1.f : __builtin_amdgcn_exp2f((m - to) * c);
       m = to;
+      far = __any(Base(m, c).shift != 0.f);
       l *= by;
 #pragma unroll
       for (int b = 0; b < DB; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[b][i] *= by;
     }
-    const float base = m == -__builtin_inff() ? 0.f : m * c;
+    float base = m == -__builtin_inff() ? 0.f : m * c;
+    if (far) {
+      const Base large(m, c);
+      base = large.by;
+#pragma unroll
+      for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[n][i] -= large.shift;
+    }
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -743,10 +783,9 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
   }
 
   if (put_off || put_off_from < t1) {
-    const float base = m == -__builtin_inff() ? 0.f : m * c;
     for (int t = t0; t < t1; ++t)
       if (t >= put_off_from || (t - t0 < 64 && put_off >> (t - t0) & 1))
-        add_seen<DT, D>(a, it, row, kv_head, t * KT, t * KT + KT, c, cap_by, slope, base, acc);
+        add_seen<DT, D>(a, it, row, kv_head, t * KT, t * KT + KT, c, cap_by, slope, m, acc);
   }
 
   l += other_half(l);

@@ -60,10 +60,13 @@ KvArgs kv_args(const sparoa_kv_desc &d, const int32_t *q_start, const int32_t *k
 
 sparoa_status check_opts(const sparoa_attention_opts *o) {
   if (!o) return fail(SPAROA_ERR_INVALID_ARG, "null attention options");
-  if (!std::isfinite(o->scale) || !(o->scale > 0.f))
-    return fail(SPAROA_ERR_INVALID_ARG, "attention: the scale must be finite and > 0");
-  if (!std::isfinite(o->cap) || !(o->cap >= 0.f) || o->window < 0)
-    return fail(SPAROA_ERR_INVALID_ARG, "attention: cap must be finite, cap and window >= 0");
+  // (the kernel divides by both, and one by the other)
+  constexpr float least = 0x1p-60f, most = 0x1p60f;
+  if (!(o->scale >= least && o->scale <= most))
+    return fail(SPAROA_ERR_INVALID_ARG, "attention: the scale must be in [2^-60, 2^60]");
+  if (!(o->cap == 0.f || (o->cap >= least && o->cap <= most)) || o->window < 0)
+    return fail(SPAROA_ERR_INVALID_ARG,
+                "attention: cap must be 0 or in [2^-60, 2^60], window >= 0");
   return SPAROA_OK;
 }
 

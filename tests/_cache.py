@@ -84,7 +84,7 @@ def attention(b, sees_of, far_of, scale, cap=0.0, slopes=None, skip=()):
     """(out, error bound) [tokens, heads, dim]; rows of no request: NaN and infinity.
 
     Bound: a score is off by dim + 16 roundings of 2^-24 of sum |q k| scale, and by
-    16 of them of itself, the cap and the bias; twice that is a weight's relative error
+    16 of them of itself, the cap (at most 256 of it: above, 64 of itself) and the bias; twice that is a weight's relative error
     (its own and the sum's).  Weights are rounded to the type (u, and half a step below
     its normal range, 2^8 of it at most since the running maximum may lag by 2^8 - the
     sum is at least 1), sums of n terms take n + 64 roundings of 2^-24, the output u."""
@@ -106,7 +106,7 @@ def attention(b, sees_of, far_of, scale, cap=0.0, slopes=None, skip=()):
             off = (b.dim + 16) * 2.0 ** -24 * size + 2.0 ** -20 * x.abs()
             if cap:
                 x = cap * torch.tanh(x / cap)
-                off = off + 2.0 ** -20 * cap
+                off = off + (2.0 ** -20 * cap if cap <= 256 else 2.0 ** -18 * x.abs())
             if slopes is not None:
                 x = x - float(slopes[h]) * far
                 off = off + 2.0 ** -20 * (float(slopes[h]) * far).abs()

@@ -91,8 +91,9 @@ def test_append(status, args):
     assert _append(**args) == status and abi.sparoa_last_error()
 
 
-OPTS = [(INVALID, dict(opts=dict(scale=s))) for s in (0.0, -1.0, NAN, INF)] + [
-    (INVALID, dict(opts=dict(cap=c))) for c in (-1.0, NAN, INF)] + [
+OPTS = [(INVALID, dict(opts=dict(scale=s))) for s in (0.0, -1.0, NAN, INF,
+                                                        2.0 ** -61, 2.0 ** 61)] + [
+    (INVALID, dict(opts=dict(cap=c))) for c in (-1.0, NAN, INF, 2.0 ** -61, 2.0 ** 61)] + [
     (INVALID, dict(opts=dict(window=-1))), (WORKSPACE, dict(ws=0)),
     (WORKSPACE, dict(ptrs=dict(ws=None))), (UNSUPPORTED, dict(ptrs=dict(ws=ODD)))] + [
     (INVALID, dict(ptrs={k: None})) for k in ("q", "kc", "vc", "q_start", "kv_len", "table",

@@ -102,6 +102,44 @@ def test_options(opts, dt):
     compare(Batch([70, 1, 150], [70, 300, 411], 4, 2, 64, 20, dt, seed=5), opts)
 
 
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("cap", [2.0 ** -60, 1e-3, 256.0, 257.0, 1e4, 1e6, 2.0 ** 60])
+def test_caps_of_any_size(cap, dt):
+    """A cap far above the scores changes nothing in them; a tiny one leaves equal weights."""
+    b = Batch([40, 1], [100, 300], 4, 2, 64, 16, dt, seed=8)
+    compare(b, dict(cap=cap))
+    compare(b, dict(cap=cap, scale=20.0))
+    compare(b, dict(cap=cap), slopes=2.0 ** -torch.arange(1.0, 5.0))
+
+
+def test_least_scale():
+    """All visible keys alike; with slopes, as their distances alone."""
+    b = Batch([1], [200], 2, 2, 64, 16, "f32", seed=9)
+    compare(b, dict(scale=2.0 ** -60))
+    compare(b, dict(scale=2.0 ** -60), slopes=torch.tensor([0.5, 0.25]))
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("keys", [1, 200, 3000])
+@pytest.mark.parametrize("scale,size", [(2.0 ** 60, 1.0), (1.0, 2.0 ** 15), (2.0 ** 40, 2.0 ** 15)])
+def test_scores_far_above_one(scale, size, keys, dt):
+    """The best key alone: one that stands out, or the last of rising ones, which an eighth
+    of a step or more parts from the next (their products are exact)."""
+    b = Batch([1], [keys], 2, 2, 64, 16, dt, seed=9)
+    sign = torch.sign(b.q[0].float())
+    b.q[0] = (size * sign).to(b.q.dtype)
+    for rising in (False, True):
+        k = torch.zeros(keys, 2, 64)
+        if rising:
+            k[:] = size * sign * (torch.arange(keys) * 16 // keys / 16 - 0.5)[:, None, None]
+            k[-1] = size * sign
+        else:
+            k[keys // 3] = size * sign
+        b.put(b.k, 0, k)
+        best = keys - 1 if rising else keys // 3
+        assert torch.equal(run(b, dict(scale=scale))[0].cpu(), b.get(b.v, 0)[best])
+
+
 @pytest.mark.parametrize("dim", [64, 256])
 @pytest.mark.parametrize("keys", [2, 31, 32, 33, 63, 64, 65, 96, 128, 129, 200])
 def test_windows_within_few_tiles(keys, dim):
