@@ -11,29 +11,35 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxHalf = 128;   // pairs of a head
+constexpr int kLeftOver = 128;
 
-// The request of row t, by the whole wave (a search of 64 ways: one round trip to
-// memory for up to 64 requests, two for 4096).  n 0: none.
+// The request of row t.  n 0: none.
 struct RowOf {
   int r;
   KvRequest q;
 };
-__device__ __forceinline__ RowOf request_of(const KvArgs &a, int t) {
+
+// Of up to 64 requests, by the whole wave: one round trip to memory.
+__device__ __forceinline__ RowOf request_of_few(const KvArgs &a, int t) {
+  const int lane = threadIdx.x & 63, l = min(lane, a.requests - 1);
+  RowOf f{0, {0, 0, 0}};
+  const KvRequest mine = kv_request(a, l);
+  const uint64_t has = __ballot(lane < a.requests && mine.n && mine.start <= t &&
+                                t - mine.start < mine.n);
+  if (!has) return f;
+  f.r = __builtin_ctzll(has);
+  f.q = KvRequest{__builtin_amdgcn_readlane(mine.start, f.r),
+                  __builtin_amdgcn_readlane(mine.n, f.r),
+                  __builtin_amdgcn_readlane(mine.len, f.r)};
+  return f;
+}
+
+// Of more, by the whole wave: the last request that starts at t or before (64 ways a step,
+// two round trips for 4096 requests).  Starts that decrease, which entries that break
+// their bounds bring about, may lead it past the row's.
+__device__ __forceinline__ RowOf request_of_many(const KvArgs &a, int t) {
   const int lane = threadIdx.x & 63;
   RowOf f{0, {0, 0, 0}};
-  if (a.requests <= 64) {
-    const int l = min(lane, a.requests - 1);
-    const KvRequest mine = kv_request(a, l);
-    const uint64_t has = __ballot(lane < a.requests && mine.n && mine.start <= t &&
-                                  t - mine.start < mine.n);
-    if (!has) return f;
-    f.r = __builtin_ctzll(has);
-    f.q = KvRequest{__builtin_amdgcn_readlane(mine.start, f.r),
-                    __builtin_amdgcn_readlane(mine.n, f.r),
-                    __builtin_amdgcn_readlane(mine.len, f.r)};
-    return f;
-  }
-  // the last request that starts at t or before
   int at = 0, left = a.requests;
   while (left > 1) {
     const int step = (left + 63) / 64, probe = at + lane * step;
@@ -46,6 +52,29 @@ __device__ __forceinline__ RowOf request_of(const KvArgs &a, int t) {
   f.q = kv_request(a, f.r);
   if (t < f.q.start || t - f.q.start >= f.q.n) f.q.n = 0;
   return f;
+}
+
+// Of any number, whatever the others' entries, by the whole work-group: the first that
+// holds t.
+__device__ __forceinline__ RowOf request_of_all(const KvArgs &a, int t) {
+  __shared__ int first;
+  if (threadIdx.x == 0) first = a.requests;
+  __syncthreads();
+  for (int r = threadIdx.x; r < a.requests; r += kThreads)
+    if (a.q_start[r] <= t && t < a.q_start[r + 1] && kv_request(a, r).n) atomicMin(&first, r);
+  __syncthreads();
+  RowOf f{first, {0, 0, 0}};
+  __syncthreads();   // (read, before another row's)
+  if (f.r < a.requests) f.q = kv_request(a, f.r);
+  return f;
+}
+// Whether no start decreases: what request_of_many does not find is not there.
+__device__ __forceinline__ bool starts_rise(const KvArgs &a) {
+  bool falls = false;
+#pragma unroll 8
+  for (int r = threadIdx.x; r < a.requests; r += kThreads)
+    falls |= a.q_start[r + 1] < a.q_start[r];
+  return !__syncthreads_or(falls);
 }
 
 template <int DT, int V, bool ALIGNED>
@@ -69,11 +98,14 @@ __device__ __forceinline__ void write(void *p, int64_t at, const float (&v)[V]) 
   }
 }
 
-// A work-group a row (token): its heads' pieces of V elements.  Rotated pieces come
-// in pairs half a rotation apart (PAIRS), or hold their pairs side by side.  Bound by
-// memory: 8500 rows of 32 + 2 x 8 heads of 128, bf16, 31 us with the rows in the cache of
-// the last pass, 44 us cold (4.3 TB/s); one row 3 us.
-template <int DT, int V, bool PAIRS, bool ALIGNED>
+// A work-group a row (token): its heads' pieces of V elements.  Rotated pieces come in
+// pairs half a rotation apart (PAIRS), or hold their pairs side by side.  Bound by memory:
+// 7660 rows of 32 + 2 x 8 heads of 128, bf16, 44 us (4.3 TB/s); one row 3 us.
+// With MANY (above 64 requests) kLeftOver work-groups in front look whether a start
+// decreases, and only then for the rows that the search missed: 300 rows of 300 requests
+// take 4.8 us (4.7 without), with a start that decreases 7; rows that each looked for
+// themselves made padding cost its scan (8000 rows 9.5 -> 12 us).
+template <int DT, int V, bool PAIRS, bool ALIGNED, bool MANY>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, KvDiv by_units,
                                                           int units) {
   __shared__ float2 turn[kMaxHalf];
@@ -82,10 +114,18 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, KvDiv by
   const int heads = a.q ? a.kv.heads : 0;
   const int rotated = (heads + a.kv.kv_heads) * units;
   const int total = rotated + a.kv.kv_heads * (dim / V);
-  for (int64_t at_row = blockIdx.x; at_row < a.kv.tokens; at_row += gridDim.x) {
+  const bool left_over = MANY && blockIdx.x < kLeftOver;
+  if (left_over && starts_rise(a.kv)) return;
+  const int first_row = MANY && !left_over ? blockIdx.x - kLeftOver : blockIdx.x;
+  const int row_step = !MANY ? gridDim.x : left_over ? kLeftOver : gridDim.x - kLeftOver;
+  for (int64_t at_row = first_row; at_row < a.kv.tokens; at_row += row_step) {
     const int t = (int)at_row;
-    const RowOf row = request_of(a.kv, t);
-    if (!row.q.n) continue;   // (alike in every wave)
+    RowOf row = MANY ? request_of_many(a.kv, t) : request_of_few(a.kv, t);
+    if (left_over) {
+      if (row.q.n) continue;   // (alike in every wave)
+      row = request_of_all(a.kv, t);
+    }
+    if (!row.q.n) continue;
     const int at = row.q.len - row.q.n + (t - row.q.start);
     if (tid < half) {
       // p freqs[i] in turns, reduced in fp64: far positions keep their angle
@@ -154,27 +194,35 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, KvDiv by
   }
 }
 
-template <int DT>
+template <int DT, bool MANY>
 void append(const AppendArgs &a, hipStream_t stream) {
   constexpr int V = 16 / Elem<DT>::size;
-  const unsigned grid = (unsigned)std::min(a.kv.tokens, 1 << 20);
+  const unsigned grid = (unsigned)std::min(a.kv.tokens, 1 << 20) + (MANY ? kLeftOver : 0);
   const int dim = a.kv.dim;
   bool whole = a.k_stride % V == 0 && a.v_stride % V == 0 && (!a.q || a.q_stride % V == 0);
+  auto run = [&](auto kernel, int units) {
+    kernel<<<grid, kThreads, 0, stream>>>(a, kv_div(units), units);
+  };
   if (a.interleaved) {
     whole = whole && a.rot % V == 0;
-    const int units = whole ? dim / V : dim / 2;
     if (whole)
-      append_kernel<DT, V, false, true><<<grid, kThreads, 0, stream>>>(a, kv_div(units), units);
+      run(append_kernel<DT, V, false, true, MANY>, dim / V);
     else
-      append_kernel<DT, 2, false, false><<<grid, kThreads, 0, stream>>>(a, kv_div(units), units);
+      run(append_kernel<DT, 2, false, false, MANY>, dim / 2);
     return;
   }
   whole = whole && a.rot % (2 * V) == 0;
-  const int v = whole ? V : 1, units = a.rot / 2 / v + (dim - a.rot) / v;
   if (whole)
-    append_kernel<DT, V, true, true><<<grid, kThreads, 0, stream>>>(a, kv_div(units), units);
+    run(append_kernel<DT, V, true, true, MANY>, a.rot / 2 / V + (dim - a.rot) / V);
   else
-    append_kernel<DT, 1, true, false><<<grid, kThreads, 0, stream>>>(a, kv_div(units), units);
+    run(append_kernel<DT, 1, true, false, MANY>, a.rot / 2 + (dim - a.rot));
+}
+template <int DT>
+void append(const AppendArgs &a, hipStream_t stream) {
+  if (a.kv.requests > 64)
+    append<DT, true>(a, stream);
+  else
+    append<DT, false>(a, stream);
 }
 
 // Accepted drafts of one (request, kv head) in the keys or values of `per` layers:
