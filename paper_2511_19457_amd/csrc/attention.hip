@@ -452,6 +452,17 @@ struct Base {
     shift = large ? m : 0.f, by = large ? 0.f : at;
   }
 };
+// What the rounding of c m left out of a row's weights: they are 2^(c (s - m) + left).
+// Sums of weights by different maxima meet without it, or keys of like scores would weigh
+// by the tile or range that they lie in (near 2^23 by up to half as much again).
+__device__ __forceinline__ float left_out(float m, float c) {
+  const Base base(m, c);
+  return base.shift != 0.f || m == -__builtin_inff() ? 0.f : fmaf(m, c, -base.by);
+}
+// Scores to log2: 2^(c s), s the product, or cap tanh(scale product / cap).
+__device__ __forceinline__ float score_unit(const AttnArgs &a) {
+  return a.cap > 0.f ? kLog2e : a.scale * kLog2e;
+}
 
 // acc += weights x values over the keys from .. to that each row sees, one by one.
 template <int DT, int D>
@@ -591,9 +602,8 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
         q[s].v[e] = v < vectors ? reinterpret_cast<const u32x4 *>(from)[v] : u32x4{0, 0, 0, 0};
       }
   }
-  // scores to log2: 2^(c s), s the product, or cap tanh(scale product / cap); the bias
-  // by distance in units of 1 / c
-  const float c = a.cap > 0.f ? kLog2e : a.scale * kLog2e;
+  // (the bias by distance in units of 1 / c)
+  const float c = score_unit(a);
   const float cap_by = a.cap > 0.f ? a.scale / a.cap : 0.f;
   const float slope = a.slopes ? a.slopes[row.head] / (a.cap > 0.f ? 1.f : a.scale) : 0.f;
 
@@ -702,7 +712,8 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
     // (far: the two products can be alike where the scores are not)
     if (__any(top * c > m * c + kSlack || (far && top > m))) {
       const float to = fmaxf(m, top);
-      const float by = to == m ? 1.f : __builtin_amdgcn_exp2f((m - to) * c);
+      const float by = to == m ? 1.f : __builtin_amdgcn_exp2f(
+          fmaf(m - to, c, left_out(to, c) - left_out(m, c)));
       m = to;
       far = __any(Base(m, c).shift != 0.f);
       l *= by;
@@ -797,17 +808,19 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
   }
   if (slot < 0 || slot >= a.slots || !row.live || wave >= a.slot_waves) return;
   const int64_t part = (slot * a.slot_waves + wave) * kWaveRows + rl;
-  if (half == 0) reinterpret_cast<float2 *>(a.ml)[part] = make_float2(m * c, l);
+  const float whole = __builtin_amdgcn_exp2f(-left_out(m, c));
+  if (half == 0) reinterpret_cast<float2 *>(a.ml)[part] = make_float2(m, l * whole);
   float *const o = reinterpret_cast<float *>(a.part) + part * S::pitch + 4 * half;
 #pragma unroll
   for (int b = 0; b < DB; ++b)
 #pragma unroll
     for (int g = 0; g < 4; ++g)
       *reinterpret_cast<f32x4 *>(o + 32 * b + 8 * g) =
-          f32x4{acc[b][4 * g], acc[b][4 * g + 1], acc[b][4 * g + 2], acc[b][4 * g + 3]};
+          f32x4{acc[b][4 * g] * whole, acc[b][4 * g + 1] * whole, acc[b][4 * g + 2] * whole,
+                acc[b][4 * g + 3] * whole};
 }
 
-// Joins the ranges of a row tile: out = sum_c 2^(m_c - m) o_c / sum_c 2^(m_c - m) l_c.
+// Joins the ranges of a row tile: out = sum_r 2^(c (m_r - m)) o_r / sum_r 2^(c (m_r - m)) l_r.
 // D / 4 lanes have a row; where a row has many ranges several such groups share them
 // and meet in LDS, since the chain of loads is all that such a call takes.
 template <int DT, int D>
@@ -819,6 +832,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a, int step) {
   __shared__ float2 stats[GROUPS];
   const int tid = threadIdx.x, group = tid / LANES, lane = tid % LANES;
   const Split<true> split(a, KT);
+  const float c = score_unit(a);
   const int row_groups = (a.tile_rows + step - 1) / step;
   const int per = a.kv.kv_heads * row_groups;
   for (int u = blockIdx.x;; u += gridDim.x) {
@@ -855,8 +869,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a, int step) {
           for (int i = 0; i < AHEAD; ++i) {
             if (!has[i] || ml[i].y == 0.f) continue;   // (the range held nothing for this row)
             const float to = fmaxf(m, ml[i].x);
-            const float old = m == to ? 1.f : __builtin_amdgcn_exp2f(m - to);
-            const float by = ml[i].x == to ? 1.f : __builtin_amdgcn_exp2f(ml[i].x - to);
+            const float old = m == to ? 1.f : __builtin_amdgcn_exp2f((m - to) * c);
+            const float by = ml[i].x == to ? 1.f : __builtin_amdgcn_exp2f((ml[i].x - to) * c);
             m = to;
             l = fmaf(by, ml[i].y, l * old);
 #pragma unroll
@@ -873,8 +887,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a, int step) {
             const f32x4 x = sums[group + p][lane];
             if (v.y == 0.f) continue;
             const float to = fmaxf(m, v.x);
-            const float old = m == to ? 1.f : __builtin_amdgcn_exp2f(m - to);
-            const float by = v.x == to ? 1.f : __builtin_amdgcn_exp2f(v.x - to);
+            const float old = m == to ? 1.f : __builtin_amdgcn_exp2f((m - to) * c);
+            const float by = v.x == to ? 1.f : __builtin_amdgcn_exp2f((v.x - to) * c);
             m = to;
             l = fmaf(by, v.y, l * old);
 #pragma unroll
