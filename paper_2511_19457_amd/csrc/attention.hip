@@ -464,13 +464,13 @@ __device__ __forceinline__ float score_unit(const AttnArgs &a) {
   return a.cap > 0.f ? kLog2e : a.scale * kLog2e;
 }
 
-// acc += weights x values over the keys from .. to that each row sees, one by one.
+// The keys from .. to that each row sees, one by one, added to its sums (a weight by one
+// score in both): m, l and acc, which are of weights 2^(c (s - m)) here.
 template <int DT, int D>
 __device__ __forceinline__ void add_seen(const AttnArgs &a, const Item &it, const Row &row,
                                          int kv_head, int from, int to, float c, float cap_by,
-                                         float slope, float m, f32x16 (&acc)[D / 32]) {
+                                         float slope, float &m, float &l, f32x16 (&acc)[D / 32]) {
   const int half = (threadIdx.x & 63) >> 5;
-  const Base base(m, c);
   const int64_t q0 = ((int64_t)row.token * a.kv.heads + row.head) * a.kv.dim;
 #pragma nounroll
   for (int k = from; k < min(to, it.len); ++k) {
@@ -488,9 +488,18 @@ __device__ __forceinline__ void add_seen(const AttnArgs &a, const Item &it, cons
     }
     if (a.cap > 0.f) x = capped<DT, true>(x, a.cap, cap_by);
     if (a.slopes) x = fmaf(-slope, distance(a, it, row, k), x);
-    // (this sum's roundings are other than those that found the maximum; NaN stays)
-    const float at2 = fmaf(x - base.shift, c, -base.by);
-    const float p = __builtin_amdgcn_exp2f(at2 > 2.f * kSlack ? 2.f * kSlack : at2);
+    const float top = fmaxf(m, x);   // (m, where x is NaN)
+    if (top > m) {
+      const float by = __builtin_amdgcn_exp2f((m - top) * c);
+      m = top;
+      l *= by;
+#pragma unroll
+      for (int b = 0; b < D / 32; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[b][i] *= by;
+    }
+    const float p = __builtin_amdgcn_exp2f((x - (m == -__builtin_inff() ? 0.f : m)) * c);
+    if (half == 0) l += p;   // (l: the lane's own)
 #pragma unroll
     for (int b = 0; b < D / 32; ++b)
 #pragma unroll
@@ -614,8 +623,10 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
     for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
   float m = -__builtin_inff(), l = 0.f;   // (l: the lane's own keys)
   bool far = false;   // a row of the wave has a maximum behind 2^24
-  // Tiles that hold an infinity or NaN beside keys that some row does not see are left to
-  // the end (behind the 64th with all that follow): their values are added key by key.
+  // Tiles that hold an infinity or NaN beside keys that some row does not see (a weight of
+  // 0 times it is NaN) are left to the end (behind the 64th with all that follow) and added
+  // key by key: weight and value, since a score that is summed in another order is another
+  // (by whole units behind 2^24).
   uint64_t put_off = 0;
   int put_off_from = INT32_MAX;
 
@@ -639,6 +650,14 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
     if (k0 >= hi || k0 + KT <= lo) continue;   // none of this wave's rows
 
     const char *keys = smem + stage * S::stage, *values = keys + S::tile;
+    const bool hidden = k0 < all_lo || k0 + KT > all_hi || pageless;   // from some row
+    if (t >= put_off_from || (hidden && holds_bad<DT>(values, S::tile))) {
+      if (t - t0 < 64)
+        put_off |= (uint64_t)1 << (t - t0);
+      else
+        put_off_from = min(put_off_from, t);
+      continue;
+    }
     constexpr int KA = 2, VA = 2;   // pieces that are read before their product
     f32x16 s[NB];
     {
@@ -690,7 +709,6 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
                            s[n][i]);
       }
     }
-    const bool hidden = k0 < all_lo || k0 + KT > all_hi || pageless;   // from some row
     if (hidden) {
       const uint64_t seen = (seen_keys(a, it, row, k0) & ~pageless) >> (4 * half);
 #pragma unroll
@@ -738,15 +756,6 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
         s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -base));
         l += s[n][i];
       }
-    // (a weight of 0 times a hidden key's infinity or NaN is NaN)
-    if (t >= put_off_from) continue;
-    if (hidden && holds_bad<DT>(values, S::tile)) {
-      if (t - t0 < 64)
-        put_off |= (uint64_t)1 << (t - t0);
-      else
-        put_off_from = t;
-      continue;
-    }
     Piece<DT> v[VA + 1], p;
 #pragma unroll
     for (int i = 0; i < 2 * NB * DB + VA; ++i) {   // 16 keys of 32 dimensions
@@ -793,10 +802,17 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
     }
   }
 
+  float whole = __builtin_amdgcn_exp2f(-left_out(m, c));   // (to weights 2^(c (s - m)))
   if (put_off || put_off_from < t1) {
+    l *= whole;
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[b][i] *= whole;
+    whole = 1.f;
     for (int t = t0; t < t1; ++t)
       if (t >= put_off_from || (t - t0 < 64 && put_off >> (t - t0) & 1))
-        add_seen<DT, D>(a, it, row, kv_head, t * KT, t * KT + KT, c, cap_by, slope, m, acc);
+        add_seen<DT, D>(a, it, row, kv_head, t * KT, t * KT + KT, c, cap_by, slope, m, l, acc);
   }
 
   l += other_half(l);
@@ -808,7 +824,6 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
   }
   if (slot < 0 || slot >= a.slots || !row.live || wave >= a.slot_waves) return;
   const int64_t part = (slot * a.slot_waves + wave) * kWaveRows + rl;
-  const float whole = __builtin_amdgcn_exp2f(-left_out(m, c));
   if (half == 0) reinterpret_cast<float2 *>(a.ml)[part] = make_float2(m, l * whole);
   float *const o = reinterpret_cast<float *>(a.part) + part * S::pitch + 4 * half;
 #pragma unroll
