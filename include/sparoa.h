@@ -817,7 +817,8 @@ sparoa_status sparoa_kv_append(const sparoa_kv_desc *desc, int64_t rot_dim, int 
  * no key gives 0.
  *   q and out [tokens][heads][head_dim], no overlap.
  *   Scores, softmax and sums are fp32; a weight is rounded once to dtype as an
- *   operand of the second product, the output once.  An infinity or NaN in a
+ *   operand of the second product (fp16: with fewer bits below 2^-21 of the row's
+ *   largest weight, to 0 below 2^-32), the output once.  An infinity or NaN in a
  *   key or value stays with the rows that see it.
  *   Equal inputs give equal bits.  Workspace: sparoa_attention_workspace_size
  *   bytes, contents on entry do not matter; it may not be shared by calls that

@@ -441,23 +441,32 @@ __device__ __forceinline__ bool holds_bad(const char *tile, int bytes) {
   return __any((top & (DT == SPAROA_F32 ? 0x80000000u : 0x80008000u)) != 0);
 }
 
-// Weights are 2^(c s - c m) as one fma of s, c and the rounded c m: a row's weights all have
-// the same error, its sum of them too.  Behind 2^24 that rounding could pass the largest
-// exponent there is: m is taken off first there.
+// Weights are 2^(c s - c m + up) as one fma of s, c and the rounded c m - up: a row's
+// weights all have the same error, its sum of them too.  Behind 2^22 that rounding could
+// pass the largest exponent there is: m is taken off first there.
+// up: fp16 has 10 bits down to 2^-14 and none below 2^-25.  2^7 above the largest weight's
+// size a long flat tail keeps its part of the sum (2^-32 of the largest weight a key is
+// lost, half a step of an output for 2^20 keys), and a weight in front of a maximum that
+// lags by 2^8 stays a number: 2^(7 + 8 + 1/2) at most, the half for what c m and its
+// comparison are rounded by up to 2^22.
+template <int DT>
 struct Base {
+  static constexpr float up = DT == SPAROA_F16 ? 7.f : 0.f;
   float shift, by;   // 2^(c (s - shift) - by)
   __device__ Base(float m, float c) {
     const float at = m == -__builtin_inff() ? 0.f : m * c;
-    const bool large = fabsf(at) > 0x1p24f;
-    shift = large ? m : 0.f, by = large ? 0.f : at;
+    const bool large = fabsf(at) > 0x1p22f;
+    shift = large ? m : 0.f, by = large ? -up : at - up;
   }
 };
-// What the rounding of c m left out of a row's weights: they are 2^(c (s - m) + left).
+// What a row's weights, 2^(c (s - m) + left), have beside the maximum: `up`, and what the
+// rounding of c m left out.
 // Sums of weights by different maxima meet without it, or keys of like scores would weigh
 // by the tile or range that they lie in (near 2^23 by up to half as much again).
+template <int DT>
 __device__ __forceinline__ float left_out(float m, float c) {
-  const Base base(m, c);
-  return base.shift != 0.f || m == -__builtin_inff() ? 0.f : fmaf(m, c, -base.by);
+  const Base<DT> base(m, c);
+  return m == -__builtin_inff() ? 0.f : base.shift != 0.f ? Base<DT>::up : fmaf(m, c, -base.by);
 }
 // Scores to log2: 2^(c s), s the product, or cap tanh(scale product / cap).
 __device__ __forceinline__ float score_unit(const AttnArgs &a) {
@@ -622,7 +631,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[b][i] = 0.f;
   float m = -__builtin_inff(), l = 0.f;   // (l: the lane's own keys)
-  bool far = false;   // a row of the wave has a maximum behind 2^24
+  bool far = false;   // a row of the wave has a maximum behind 2^22
   // Tiles that hold an infinity or NaN beside keys that some row does not see (a weight of
   // 0 times it is NaN) are left to the end (behind the 64th with all that follow) and added
   // key by key: weight and value, since a score that is summed in another order is another
@@ -731,18 +740,18 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
     if (__any(top * c > m * c + kSlack || (far && top > m))) {
       const float to = fmaxf(m, top);
       const float by = to == m ? 1.f : __builtin_amdgcn_exp2f(
-          fmaf(m - to, c, left_out(to, c) - left_out(m, c)));
+          fmaf(m - to, c, left_out<DT>(to, c) - left_out<DT>(m, c)));
       m = to;
-      far = __any(Base(m, c).shift != 0.f);
+      far = __any(Base<DT>(m, c).shift != 0.f);
       l *= by;
 #pragma unroll
       for (int b = 0; b < DB; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[b][i] *= by;
     }
-    float base = m == -__builtin_inff() ? 0.f : m * c;
+    float base = (m == -__builtin_inff() ? 0.f : m * c) - Base<DT>::up;
     if (far) {
-      const Base large(m, c);
+      const Base<DT> large(m, c);
       base = large.by;
 #pragma unroll
       for (int n = 0; n < NB; ++n)
@@ -802,7 +811,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
     }
   }
 
-  float whole = __builtin_amdgcn_exp2f(-left_out(m, c));   // (to weights 2^(c (s - m)))
+  float whole = __builtin_amdgcn_exp2f(-left_out<DT>(m, c));   // (to weights 2^(c (s - m)))
   if (put_off || put_off_from < t1) {
     l *= whole;
 #pragma unroll
