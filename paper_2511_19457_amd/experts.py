@@ -131,7 +131,23 @@ class ExpertStack:
                         to=torch.uint8)
 
     def attend(self, b, adapter_ids, batch, tree=None, stream=None):
-        """Block b's attention on n: q, o and the block's cache keep what it made."""
+        """Block b's attention on n: q, o and the block's cache keep what it made (o is 0 in
+        rows of no request)."""
+        self._clear(stream)
+        self._attend(b, adapter_ids, batch, tree, stream)
+
+    def _clear(self, stream):
+        """o to 0: attention leaves rows of no request as they were, with what an earlier
+        batch had there.  Once a pass, since its blocks write the same rows."""
+        if stream is None:
+            self.o.zero_()
+            return
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(stream, device=self.o.device)
+        with torch.cuda.stream(stream):
+            self.o.zero_()
+
+    def _attend(self, b, adapter_ids, batch, tree, stream):
         w, d = self.blocks[b], self.kv
         abi.sparoa_fc_adapted(self.qkv_fc, abi.ACT_NONE, self.n, w["qkv"], None, w["qkv_a"],
                               w["qkv_b"], self.scale, adapter_ids, None, self.qkv, self.ws, stream)
@@ -155,9 +171,14 @@ class ExpertStack:
 
     def run_block(self, b, adapter_ids, token_mask=None, stream=None, batch=None, tree=None):
         """Block b on r and n in place; p, logits, idx, weights, plan and f keep what it made."""
+        if self.heads:
+            self._clear(stream)
+        self._run_block(b, adapter_ids, token_mask, stream, batch, tree)
+
+    def _run_block(self, b, adapter_ids, token_mask, stream, batch, tree):
         w = self.blocks[b]
         if self.heads:
-            self.attend(b, adapter_ids, batch, tree, stream)
+            self._attend(b, adapter_ids, batch, tree, stream)
         abi.sparoa_fc_adapted(self.proj, abi.ACT_NONE, self.o if self.heads else self.n, w["proj"],
                               None, w["lora_a"], w["lora_b"], self.scale, adapter_ids, None, self.p,
                               self.ws, stream)
@@ -184,8 +205,10 @@ class ExpertStack:
             raise ValueError(f"x: {tuple(self.r.shape)} of {self.dtype} is wanted")
         abi.sparoa_block_norm(self.first, None, None, None, None, x, self.first_norm, None, self.r,
                               self.n, stream)
+        if self.heads:
+            self._clear(stream)
         for b in range(len(self.blocks)):
-            self.run_block(b, adapter_ids, token_mask, stream, batch, tree)
+            self._run_block(b, adapter_ids, token_mask, stream, batch, tree)
         return self.n
 
 
