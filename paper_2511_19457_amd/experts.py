@@ -63,6 +63,12 @@ class ExpertStack:
             self.kv = abi.kv_desc(tokens, requests, heads, kv_heads, head_dim, pages, page_size,
                                   table_pages, dtype, max_queries=max_queries)
             self.attention = abi.attention_opts(head_dim ** -0.5, window=window)
+            # trees by the words of their bits: 64 nodes a word, 256 nodes at most
+            self.trees = {}
+            for words in range(1, -(-min(self.kv.max_queries, 256) // 64) + 1):
+                self.trees[words] = abi.kv_desc(tokens, requests, heads, kv_heads, head_dim, pages,
+                                                page_size, table_pages, dtype,
+                                                max_queries=min(self.kv.max_queries, 64 * words))
             half = head_dim // 2
             self.freqs = rope_base ** (-torch.arange(half, dtype=torch.float64,
                                                      device=self.dev) / half)
@@ -126,8 +132,9 @@ class ExpertStack:
                             abi.sparoa_fc_workspace_size(self.router, family | 1),
                             abi.sparoa_expert_route_workspace_size(self.route),
                             abi.sparoa_expert_ffn_workspace_size(self.ffn), 16,
-                            *([abi.sparoa_fc_adapted_workspace_size(self.qkv_fc),
-                               abi.sparoa_attention_workspace_size(self.kv)] if heads else [])),
+                            *([abi.sparoa_fc_adapted_workspace_size(self.qkv_fc)] +
+                              [abi.sparoa_attention_workspace_size(d)
+                               for d in (self.kv, *self.trees.values())] if heads else [])),
                         to=torch.uint8)
 
     def attend(self, b, adapter_ids, batch, tree=None, stream=None):
@@ -149,6 +156,12 @@ class ExpertStack:
 
     def _attend(self, b, adapter_ids, batch, tree, stream):
         w, d = self.blocks[b], self.kv
+        if tree is not None:
+            words, rest = divmod(tree[0].numel(), d.tokens)
+            if rest or words not in self.trees:
+                raise ValueError(f"tree_mask: [{d.tokens}, words] with 1 to {max(self.trees)} "
+                                 f"words is wanted, got {tuple(tree[0].shape)}")
+            d = self.trees[words]
         abi.sparoa_fc_adapted(self.qkv_fc, abi.ACT_NONE, self.n, w["qkv"], None, w["qkv_a"],
                               w["qkv_b"], self.scale, adapter_ids, None, self.qkv, self.ws, stream)
         wide, narrow = d.heads * d.head_dim, d.kv_heads * d.head_dim
@@ -198,7 +211,8 @@ class ExpertStack:
         """x [tokens, hidden], adapter_ids int32 [tokens] (outside [0, adapters): none),
         token_mask uint8 [tokens] or None -> the last block's normed output (a buffer of
         the stack's).  With heads: batch = (q_start, kv_len, page_table), kv_len with the
-        pass's own keys, and for drafted trees tree = (tree_mask, positions)."""
+        pass's own keys, and for drafted trees tree = (tree_mask, positions), tree_mask
+        int64 [tokens, words]: 64 nodes of a request for each word, at most 256."""
         if bool(self.heads) != (batch is not None):
             raise ValueError("batch: wanted where the stack has heads, and only there")
         if tuple(x.shape) != tuple(self.r.shape) or x.dtype != self.dtype:
