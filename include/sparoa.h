@@ -824,8 +824,8 @@ sparoa_status sparoa_kv_append(const sparoa_kv_desc *desc, int64_t rot_dim, int 
  *   bytes, contents on entry do not matter; it may not be shared by calls that
  *   overlap in time.
  * Errors: also INVALID_ARG for null options, a scale or a cap other than 0 outside
- * [2^-60, 2^60], window < 0; UNSUPPORTED for 2^30 or more rows (token, head);
- * WORKSPACE. */
+ * [2^-60, 2^60], window < 0; UNSUPPORTED for 2^31 or more row tiles (of 128 rows
+ * (token, head of the group) of a request) and ranges; WORKSPACE. */
 typedef struct {
   float scale, cap;
   int64_t window;   /* keys a row sees up to its own, 0: all */

@@ -533,7 +533,8 @@ __device__ __forceinline__ void add_seen(const AttnArgs &a, const Item &it, cons
 // stages (325), a kernel for up to 32 rows with a ring a wave and no barrier (decoding
 // 216 us against 221 then, one token 15.4 against 13.8).
 template <int DT, int D>
-__global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_kernel(AttnArgs a,
+                                                                                int id0) {
   using S = Shape<DT, D>;
   using E = Elem<DT>;
   constexpr int KT = S::keys, NB = KT / 32, DB = D / 32, NV = S::vectors;
@@ -542,7 +543,7 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
 
   const int lane = threadIdx.x & 63, rl = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kv_head = blockIdx.x % a.kv.kv_heads, id = blockIdx.x / a.kv.kv_heads;
+  const int kv_head = blockIdx.x % a.kv.kv_heads, id = id0 + blockIdx.x / a.kv.kv_heads;
   const Item it = Split<false>(a, KT).find(id);
   if (!it.n) return;
   const int64_t slot = (int64_t)it.slot * a.kv.kv_heads + kv_head;
@@ -932,12 +933,13 @@ __global__ __launch_bounds__(kThreads) void join_kernel(AttnArgs a, int step) {
   }
 }
 
-// Row tiles that the descriptor allows.
+// Row tiles that the descriptor allows (a request that has some has a token).
 int64_t most_tiles(const sparoa_kv_desc &d) {
   const int64_t group = d.heads / d.kv_heads;
   const int64_t queries = std::min(d.max_queries, d.tokens);
-  return std::min(d.requests * cdiv(queries * group, kTileRows),
-                  d.tokens * group / kTileRows + d.requests);
+  const int64_t requests = std::min(d.requests, d.tokens);
+  return std::min(requests * cdiv(queries * group, kTileRows),
+                  d.tokens * group / kTileRows + requests);
 }
 
 struct Parts {
@@ -974,16 +976,20 @@ template <int DT, int D>
 sparoa_status launch(const AttnArgs &a, int64_t tiles, hipStream_t stream) {
   // (by the work that they share, or by the ranges that a row tile can have)
   const int64_t ranges = std::min<int64_t>(kMaxRanges, cdiv(a.kv.max_keys, Shape<DT, D>::keys) + 1);
-  const int64_t items = std::min(tiles + cdiv(2 * a.target, a.kv.kv_heads) + 2, tiles * ranges) *
-                        a.kv.kv_heads;
-  if (items > 1 << 23)
-    return fail(SPAROA_ERR_UNSUPPORTED, "attention: 2^30 or more rows (token, head)");
+  const int64_t items = std::min(tiles + cdiv(2 * a.target, a.kv.kv_heads) + 2, tiles * ranges);
+  if (items > INT32_MAX)
+    return fail(SPAROA_ERR_UNSUPPORTED, "attention: 2^31 or more row tiles and ranges");
   if (a.plan) {
     plan_kernel<<<1, kPlanThreads, 0, stream>>>(a, Shape<DT, D>::keys);
     SPAROA_LAUNCH_CHECK("attention: plan");
   }
-  attention_kernel<DT, D><<<(unsigned)items, kThreads, 0, stream>>>(a);
-  SPAROA_LAUNCH_CHECK("attention");
+  // (2^31 threads a launch: a request of its own for every token makes an item of each)
+  const int64_t most = (1 << 23) / a.kv.kv_heads;
+  for (int64_t id0 = 0; id0 < items; id0 += most) {
+    const unsigned grid = (unsigned)(std::min(items - id0, most) * a.kv.kv_heads);
+    attention_kernel<DT, D><<<grid, kThreads, 0, stream>>>(a, (int)id0);
+    SPAROA_LAUNCH_CHECK("attention");
+  }
   if (a.slots) {
     // (a work-group a row where they are few altogether; else the lookups are made for
     // several: 64 requests of 4 rows a kv head 221 us with 1 each, 217 with 4)
