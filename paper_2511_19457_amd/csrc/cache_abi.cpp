@@ -34,7 +34,7 @@ sparoa_status check_kv(const sparoa_kv_desc *d) {
   if (d->head_dim > 256 || d->head_dim % 8)
     return fail(SPAROA_ERR_UNSUPPORTED, "kv: head_dim above 256 or no multiple of 8");
   // (a row tile's and a key tile's last index stay below 2^31, too)
-  if (!below_2g(d->tokens + 1024, d->heads) || d->tokens > kMax31 - 1024 ||
+  if (d->tokens > kMax31 - 1024 || !below_2g(d->tokens + 1024, d->heads) ||
       !below_2g(d->requests, d->table_pages) || d->requests >= kMax31 ||
       !below_2g(d->pages, d->kv_heads, d->page_size) || d->max_keys > kMax31 - 1024 ||
       d->page_size > kMax31)
