@@ -114,32 +114,43 @@ struct Item {
   int slot, chunk, chunks;   // number `chunk` of the row tile's ranges of keys
 };
 
-// Row tiles of a request, key tiles that one of them reaches at most, and on average
-// (as far as lengths tell; not below half of the most).
+// Row tiles of a request, key tiles that one of them reaches at most, and its work: half
+// keys that its row tiles reach (on average, as far as lengths tell; not below half of the
+// most).  Whole numbers: the kernels that find the split each for themselves add them in
+// any order to the same sum.
 struct Load {
   int tiles, spans;
-  float mean;
+  int64_t work;
 };
 __device__ __forceinline__ Load load_of(const AttnArgs &a, const KvRequest &q, int keys) {
-  Load l{0, 0, 0.f};
+  Load l{0, 0, 0};
   if (!q.n) return l;
   l.tiles = (q.n * a.kv.group + kTileRows - 1) / kTileRows;
   int reach = q.len;
-  float mean = (float)q.len;
+  uint32_t mean2 = 2 * (uint32_t)q.len;
   if (a.causal && !a.mask) {
     if (a.window) reach = min(q.len, a.window + kTileRows / a.kv.group + 1);
-    mean = fminf((float)q.len - 0.5f * (float)q.n, (float)reach);
+    mean2 = min(mean2 - (uint32_t)q.n, 2 * (uint32_t)reach);
   }
   // (a window begins within a tile; no more than there are)
   l.spans = min((reach - 1) / keys + 2, (q.len - 1) / keys + 1);
-  l.mean = fmaxf(mean / (float)keys, 0.5f * (float)l.spans);
+  l.work = (int64_t)l.tiles * max(mean2, (uint32_t)(l.spans * keys));
   return l;
 }
 
+// The sum of all lanes' work (at most 2^51 of a lane's: there every row tile is one range),
+// by moves between lanes; where one passes 26 bits, those and the rest by themselves.
+__device__ __forceinline__ int64_t wave_work(int64_t work) {
+  const uint32_t low =
+      __builtin_amdgcn_readlane(wave_prefix((int)(work & ((1 << 26) - 1))), 63);
+  if (!__any(work >> 26)) return low;
+  const int high = wave_prefix((int)(min(work, (int64_t)1 << 51) >> 26));
+  return ((int64_t)(uint32_t)__builtin_amdgcn_readlane(high, 63) << 26) + low;
+}
 // Key tiles of an item: the whole work over the wanted items.
-__device__ __forceinline__ int chunk_of(const AttnArgs &a, float work) {
-  work = work * (float)a.kv.kv_heads / (float)a.target;
-  return work < 1e9f ? max(1, (int)ceilf(work)) : 1 << 30;
+__device__ __forceinline__ int chunk_of(const AttnArgs &a, int64_t work, int keys) {
+  const float each = (float)work * (float)a.kv.kv_heads / (2.f * (float)keys * (float)a.target);
+  return each < 1e9f ? max(1, (int)ceilf(each)) : 1 << 30;
 }
 
 // Ranges of a request's row tiles.  A range's outputs pass through memory twice (4
@@ -169,21 +180,18 @@ __device__ __forceinline__ Share share_of(const Load &l, int chunks) {
 constexpr int kLaneRequests = 64;
 constexpr int kPlanThreads = 1024;
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttnArgs a, int keys) {
-  __shared__ float work_of[kPlanThreads / 64];
+  __shared__ int64_t work_of[kPlanThreads / 64];
   __shared__ int before[kPlanThreads / 64][3];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = a.kv.requests;
-  float work = 0.f;
-  for (int r = tid; r < n; r += kPlanThreads) {
-    const Load l = load_of(a, kv_request(a.kv, r), keys);
-    work += (float)l.tiles * l.mean;
-  }
-#pragma unroll
-  for (int m = 32; m; m >>= 1) work += __shfl_xor(work, m);
+  int64_t work = 0;
+  for (int r = tid; r < n; r += kPlanThreads)
+    work = min(work + load_of(a, kv_request(a.kv, r), keys).work, (int64_t)1 << 51);
+  work = wave_work(work);
   if (lane == 0) work_of[wave] = work;
   __syncthreads();
-  work = 0.f;
+  work = 0;
   for (int w = 0; w < kPlanThreads / 64; ++w) work += work_of[w];
-  const int chunk = chunk_of(a, work);
+  const int chunk = chunk_of(a, work, keys);
   int32_t *const items = a.plan + 1, *const slots = items + n + 1, *const splits = slots + n + 1;
   int sum[3] = {0, 0, 0};
   for (int r0 = 0; r0 < n; r0 += kPlanThreads) {
@@ -232,13 +240,7 @@ struct Split {
     q = kv_request(a.kv, min(lane, a.kv.requests - 1));
     if (lane >= a.kv.requests) q.n = 0;
     l = load_of(a, q, keys);
-    float work = (float)l.tiles * l.mean;
-    if (a.kv.requests > 1)
-#pragma unroll
-      for (int m = 32; m; m >>= 1) work += __shfl_xor(work, m);
-    else
-      work = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(work)));
-    chunks = ranges_of(a, q, l, chunk_of(a, work), keys);
+    chunks = ranges_of(a, q, l, chunk_of(a, wave_work(l.work), keys), keys);
     // The requests of the longest ranges first where rows are many: 12 chunks of prompts 63
     // -> 55 us, 32 trees the same.  (Single rows are a stream, whose last ranges have the
     // memory to themselves: 64 requests 224 us in their order, 238 by length.)
@@ -955,7 +957,7 @@ Parts attention_split(const sparoa_kv_desc &d) {
                                      : kTargetMany;
   // A request's row tiles that are split have ceil(spans / chunk) < 2 spans / chunk
   // ranges each, spans are at most twice their mean, and all means at most `target`
-  // chunks.  (+ kv_heads: the work's sum is rounded.)
+  // chunks.  (+ kv_heads: their quotient is rounded.)
   const int64_t chunks = cdiv(d.max_keys, tile_keys(d.head_dim, d.dtype));
   const int64_t most = most_tiles(d);
   const int64_t cap = 4 * s.target + 4 * d.kv_heads;
