@@ -739,8 +739,9 @@ __global__ __launch_bounds__(kThreads, (Shape<DT, D>::groups)) void attention_ke
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
     top = fmaxf(top, other_half(top));
-    // (far: the two products can be alike where the scores are not)
-    if (__any(top * c > m * c + kSlack || (far && top > m))) {
+    // (far: the two products can be alike where the scores are not; the first: its product
+    // can be -infinity)
+    if (__any(top * c > m * c + kSlack || ((far || m == -__builtin_inff()) && top > m))) {
       const float to = fmaxf(m, top);
       const float by = to == m ? 1.f : __builtin_amdgcn_exp2f(
           fmaf(m - to, c, left_out<DT>(to, c) - left_out<DT>(m, c)));

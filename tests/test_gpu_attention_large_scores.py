@@ -50,3 +50,22 @@ def test_scales(dt):
         b = Exact(3000, 2, 64, 16, dt, scores((10, 700, 1400, 2100, 2990), (0, 1, 3, 2, 1), exponent))
         b.scores = b.scores * scale
         b.compare(run(b, dict(scale=scale)))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("keys,heads,dim", [(200, 2, 64), (3000, 2, 64), (640, 1024, 8)])
+def test_products_whose_scores_pass_fp32(keys, heads, dim, dt):
+    """Products of 2^68 and more with a scale of 2^60, of either sign: the largest alone
+    (the others' weights are e^-(2^100))."""
+    for sign in (1.0, -1.0):
+        for best in (0, keys // 2, keys - 1):
+            b = Exact(keys, heads, dim, 16, dt, {0: (2, 1)})
+            b.q[:, :, 0], b.q[:, :, 1] = 2.0 ** 34, 0.0
+            k = torch.zeros(keys, heads, dim)
+            k[:, :, 0] = sign * 2.0 ** (36 if sign < 0 else 34)
+            k[best, :, 0] = sign * 2.0 ** (34 if sign < 0 else 36)
+            b.put(b.k, 0, k)
+            got = run(b, dict(scale=2.0 ** 60))[0].cpu()
+            want = b.get(b.v, 0)[best].double()
+            # (the weight is 1, or 2^7 in fp32 sums of products: exact but for 3 roundings of 2^-24)
+            assert ((got.double() - want).abs() <= 4 * 2.0 ** -24 * want.abs()).all(), (sign, best)
