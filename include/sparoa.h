@@ -768,6 +768,8 @@ sparoa_status sparoa_block_norm(const sparoa_block_norm_desc *desc, const void *
  * request) and `max_keys` (kv_len of a request) are what they may reach.  A
  * request without rows, or whose numbers break these bounds (rows outside
  * [0, tokens), n_r > max_queries, kv_len < n_r or > max_keys), is left out.
+ * No row may be claimed by two requests that are not left out (which takes a
+ * start that falls back): outputs of such a batch are any, within its tensors.
  *
  * Query head h reads the keys of head h / (heads / kv_heads).
  * Errors of every call: INVALID_ARG for a null descriptor or required pointer,

@@ -530,7 +530,7 @@ __device__ __forceinline__ void add_seen(const AttnArgs &a, const Item &it, cons
 // wave 1024 cycles of the one and some 1100 of the other, 2400 together): two work-groups
 // a CU, one's products beside the other's weights.  2 x 4096 causal rows, 32 heads of 128,
 // 8 kv heads, bf16: 305-335 us, 0.82-0.90 PFLOP/s; 64 single rows over 200 to 8000 keys:
-// 219 us, the kernel 5.3 TB/s.  Built and dropped: the next tile's scores beside this
+// 218 us, the kernel 5.1 TB/s (256 of them, planned in front: 820 us, 5.3).  Built and dropped: the next tile's scores beside this
 // one's weights (313 us against 305 then; fp32 42 against 35), 8 waves with rings of 4
 // stages (325), a kernel for up to 32 rows with a ring a wave and no barrier (decoding
 // 216 us against 221 then, one token 15.4 against 13.8).
