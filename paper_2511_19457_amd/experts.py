@@ -149,9 +149,11 @@ class ExpertStack:
         if stream is None:
             self.o.zero_()
             return
-        if not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(stream, device=self.o.device)
-        with torch.cuda.stream(stream):
+        handle = stream if isinstance(stream, int) else stream.cuda_stream
+        # (ExternalStream takes 0, the default stream, for none and makes one)
+        on = torch.cuda.ExternalStream(handle, device=self.o.device) if handle else \
+            torch.cuda.default_stream(self.o.device)
+        with torch.cuda.stream(on):
             self.o.zero_()
 
     def _attend(self, b, adapter_ids, batch, tree, stream):

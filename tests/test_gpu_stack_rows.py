@@ -66,6 +66,23 @@ def test_on_another_stream():
         assert not s.o[7:].any() and torch.equal(s.n, want)
 
 
+def test_the_default_stream_by_its_handle():
+    """Handle 0, with another stream current that is busy: the rows are cleared in order."""
+    s = _stack(60, 2, 20, 41, "bf16")
+    s.o.fill_(1.0)
+    busy = torch.zeros(1 << 27, device="cuda")
+    before = torch.empty_like(s.o)
+    other = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        busy.add_(1.0)
+    before.copy_(s.o)                  # (behind the busy kernels of the default stream)
+    with torch.cuda.stream(other):
+        s._clear(0)
+    torch.cuda.synchronize()
+    assert not s.o.any() and (before == 1.0).all()
+
+
 def test_captured():
     table = torch.arange(40, dtype=torch.int32).reshape(2, 20).contiguous()
     s = _stack(60, 2, 20, 41, "bf16")
